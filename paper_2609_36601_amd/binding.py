@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "libsaki.so")
 
 SAKI_F32, SAKI_BF16 = 0, 1
 SAKI_OP_COUPLE, SAKI_OP_ROUTE, SAKI_OP_VERIFY, SAKI_OP_SELECT = 0, 1, 2, 3
+SAKI_OP_KV_RESERVE, SAKI_OP_KV_COMPACT, SAKI_OP_KV_ATTENTION = 4, 5, 6
 SAKI_TARGET_MODE, SAKI_TARGET_SAMPLE = 0, 1
 SAKI_SELECT_RANDOM, SAKI_SELECT_TV_WEIGHTED = 0, 1
 SAKI_MAX_VOCAB = 1 << 21
@@ -28,7 +29,9 @@ STATUS = {0: "SAKI_OK", 1: "SAKI_E_NULLPTR", 2: "SAKI_E_SHAPE", 3: "SAKI_E_VALUE
 
 EXPORTED = ["saki_workspace_bytes", "saki_couple", "saki_couple_static", "saki_route_loss", "saki_spec_verify",
             "saki_select_positions", "saki_probe_metrics", "saki_sample", "saki_commit",
+            "saki_kv_reserve", "saki_kv_commit", "saki_kv_fork", "saki_kv_compact", "saki_kv_append", "saki_kv_attention",
             "saki_status_str", "saki_last_error"]
+KV_OK, KV_NO_PAGES, KV_TOO_LONG, KV_BAD = 0, 1, 2, 3
 SEQ_RUNNING, SEQ_FINISHED, SEQ_STOPPED = 0, 1, 2
 SAKI_MAX_PROBE_K = 64
 
@@ -69,6 +72,33 @@ TRAJ_DTYPES = dict(tokens=torch.int32, corrected=torch.uint8, teacher_argmax=tor
 class SakiTraj(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int64), ("max_len", ctypes.c_int64)] + \
                [(n, ctypes.c_void_p) for n in TRAJ_FIELDS]
+
+
+class SakiKVTable(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("pages", "length", "held", "refs")]
+
+
+class SakiKVPool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("n_layers", "layer_stride", "page_stride", "head_stride",
+                                              "token_stride")]
+
+
+class SakiKVTokens(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("n_tokens", ctypes.c_int64), ("n_new", ctypes.c_int32),
+                ("shift", ctypes.c_int32)]
+
+
+class SakiKVHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class SakiKVRope(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float)]
 
 
 class SakiError(RuntimeError):
@@ -127,6 +157,19 @@ def load(path=LIB_PATH):
     lib.saki_commit.argtypes = [ctypes.POINTER(SakiTraj), ctypes.c_int32, ctypes.c_int32,
                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(SakiCoupleOut),
                                 ctypes.c_void_p, ctypes.c_void_p]
+    P, I32, I64 = ctypes.POINTER, ctypes.c_int32, ctypes.c_int64
+    ptr, size = ctypes.c_void_p, ctypes.c_size_t
+    for name, args in (
+            ("reserve", [P(SakiKVTable), P(SakiKVPool), ptr, I32, ptr, ptr, size, ptr]),
+            ("commit", [P(SakiKVTable), ptr, ptr, ptr, ptr]),
+            ("fork", [P(SakiKVTable), I64, ptr, ptr, ptr, ptr]),
+            ("compact", [P(SakiKVTable), P(SakiKVPool), ptr, ptr, size, ptr]),
+            ("append", [P(SakiKVTable), P(SakiKVPool), I64, P(SakiKVTokens), P(SakiKVRope), I32] +
+             [P(SakiKVHeads)] * 4 + [ptr]),
+            ("attention", [P(SakiKVTable), P(SakiKVPool), I64, P(SakiKVTokens), I32, P(SakiKVHeads), P(SakiKVHeads), ptr,
+                           ctypes.c_float, I32, I32, ptr, size, ptr])):
+        f = getattr(lib, "saki_kv_" + name)
+        f.restype, f.argtypes = ctypes.c_int, args
     lib.saki_status_str.restype = ctypes.c_char_p
     lib.saki_status_str.argtypes = [ctypes.c_int]
     lib.saki_last_error.restype = ctypes.c_char_p
@@ -427,3 +470,94 @@ def saki_commit(traj, max_len, k, eos_id, accepted_len, correction, per_pos, n_c
     st = _lib.saki_commit(ctypes.byref(tr), int(k), int(eos_id), _ptr(accepted_len),
                           _ptr(correction), ctypes.byref(pp), _ptr(n_commit), _stream(stream))
     _check(st)
+
+
+# ---------------------------------------------------------------------------
+# Paged key-value caches.  Tables and pools are described once (kv_table, kv_pool)
+# and used by many calls; cache.PagedKV holds both and allocates outputs and workspaces.
+# ---------------------------------------------------------------------------
+def _want(name, t, dtype, shape, device):
+    """A dense tensor of this type, shape and device."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}: got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+
+
+def kv_table(pages, length, held, refs, page_size):
+    """Descriptor of a table (int32 tensors pages [n_seq, max_pages], length and held [n_seq], refs [n_pages])."""
+    n_seq, max_pages = pages.shape
+    for name, t, shape in (("pages", pages, (n_seq, max_pages)), ("length", length, (n_seq,)), ("held", held, (n_seq,)),
+                           ("refs", refs, (refs.numel(),))):
+        _want(name, t, torch.int32, shape, pages.device)
+    return SakiKVTable(n_seq, max_pages, refs.numel(), page_size, 0, _ptr(pages), _ptr(length), _ptr(held), _ptr(refs))
+
+
+def kv_pool(k, v):
+    """Descriptor of a pool: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] of equal strides."""
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
+        raise ValueError("k and v must be [n_layers, n_pages, n_kv_heads, page_size, head_dim] tensors alike")
+    if k.stride(4) != 1:
+        raise ValueError("the elements of a head must be consecutive")
+    s = k.stride()
+    return SakiKVPool(_ptr(k), _ptr(v), _dtype_code(k.dtype), k.shape[2], k.shape[4], 0, k.shape[0], s[0], s[1], s[2], s[3])
+
+
+def _heads(t):
+    if t is None:
+        return None
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("token arrays must be [n_tokens, heads, head_dim] with consecutive elements of a head")
+    return SakiKVHeads(_ptr(t), t.stride(0), t.stride(1))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def _ws_bytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def saki_kv_reserve(table, pool, n_new, status=None, workspace=None, stream=None):
+    """Call saki_kv_reserve; n_new: an int32 tensor [n_seq], or one number for every sequence."""
+    load()
+    each = isinstance(n_new, torch.Tensor)
+    if not each and not 0 <= n_new < 2**31:
+        raise ValueError("n_new outside [0, 2^31)")
+    _check(_lib.saki_kv_reserve(_ref(table), _ref(pool), _ptr(n_new) if each else None, 0 if each else int(n_new),
+                                _ptr(status), _ptr(workspace), _ws_bytes(workspace), _stream(stream)))
+
+
+def saki_kv_commit(table, delta, done=None, status=None, stream=None):
+    load()
+    _check(_lib.saki_kv_commit(_ref(table), _ptr(delta), _ptr(done), _ptr(status), _stream(stream)))
+
+
+def saki_kv_fork(table, src, dst, status=None, stream=None):
+    load()
+    _check(_lib.saki_kv_fork(_ref(table), src.numel(), _ptr(src), _ptr(dst), _ptr(status), _stream(stream)))
+
+
+def saki_kv_compact(table, pool, n_live=None, workspace=None, stream=None):
+    load()
+    _check(_lib.saki_kv_compact(_ref(table), _ref(pool), _ptr(n_live), _ptr(workspace), _ws_bytes(workspace),
+                                _stream(stream)))
+
+
+def saki_kv_append(table, pool, layer, tokens, k, v, q=None, q_out=None, rope=None, stream=None):
+    """Call saki_kv_append; tokens: a SakiKVTokens, rope: a SakiKVRope or None."""
+    load()
+    _check(_lib.saki_kv_append(_ref(table), _ref(pool), int(layer), _ref(tokens), _ref(rope),
+                               0 if q is None else q.shape[1], _ref(_heads(q)), _ref(_heads(q_out)), _ref(_heads(k)),
+                               _ref(_heads(v)), _stream(stream)))
+
+
+def saki_kv_attention(table, pool, layer, tokens, q, out, lse=None, scale=1.0, window=0, sinks=0, workspace=None,
+                      stream=None):
+    load()
+    for name, x in (("window", window), ("sinks", sinks)):
+        if not 0 <= x < 2**31:
+            raise ValueError(f"{name} outside [0, 2^31)")
+    _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _ref(_heads(q)),
+                                  _ref(_heads(out)), _ptr(lse), float(scale), int(window), int(sinks), _ptr(workspace),
+                                  _ws_bytes(workspace), _stream(stream)))

@@ -10,7 +10,8 @@ LIB = os.path.join(HERE, "libsaki.so")
 CSRC = os.path.join(HERE, "csrc")
 # (source, defines): the units of the library, compiled in parallel
 UNITS = [("saki.hip", [])] + [("couple.hip", [f"-DSAKI_PART={p}"]) for p in range(4)] + \
-        [("verify.hip", [f"-DSAKI_PART={p}"]) for p in range(2)]
+        [("verify.hip", [f"-DSAKI_PART={p}"]) for p in range(2)] + \
+        [("kv_cache.hip", [])] + [("kv_attention.hip", [f"-DSAKI_PART={p}"]) for p in range(6)]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

@@ -1,0 +1,454 @@
+// The entry points of the paged key-value cache: argument checks and launches.
+#include <algorithm>
+
+#include "abi.hpp"
+#include "kv_attention.hpp"
+#include "kv_pages.hpp"
+
+namespace saki {
+
+namespace {
+
+constexpr int64_t MAX_SEQ = int64_t{1} << 24;
+constexpr int64_t MAX_TOKENS = int64_t{1} << 30;  // of a sequence's pages, and of `shift`
+
+int64_t up16(int64_t b) { return (b + 15) & ~int64_t{15}; }
+int elem_bytes(int32_t dtype) { return dtype == SAKI_BF16 ? 2 : 4; }
+bool off(const void* p, unsigned align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
+
+saki_status check_table(const saki_kv_table* t) {
+  if (!t) return abi_fail(SAKI_E_NULLPTR, "table descriptor is NULL");
+  if (t->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_kv_table.reserved must be 0");
+  if (t->n_seq < 0 || t->n_seq > MAX_SEQ) return abi_fail(SAKI_E_SHAPE, "n_seq outside [0, 2^24]");
+  if (t->n_pages < 1 || t->n_pages > MAX_TOKENS) return abi_fail(SAKI_E_SHAPE, "n_pages outside [1, 2^30]");
+  if (t->page_size < 8 || t->page_size > 1024 || (t->page_size & (t->page_size - 1)) != 0)
+    return abi_fail(SAKI_E_SHAPE, "page_size must be a power of two, 8 .. 1024");
+  if (t->max_pages < 1 || t->max_pages > MAX_TOKENS / t->page_size)
+    return abi_fail(SAKI_E_SHAPE, "max_pages < 1, or max_pages * page_size > 2^30");
+  if (t->n_seq == 0) return SAKI_OK;
+  if (!t->pages || !t->length || !t->held || !t->refs)
+    return abi_fail(SAKI_E_NULLPTR, "pages, length, held and refs are required");
+  if (off(t->pages, 4) || off(t->length, 4) || off(t->held, 4) || off(t->refs, 4))
+    return abi_fail(SAKI_E_ALIGN, "table arrays must be 4-byte aligned");
+  return SAKI_OK;
+}
+
+// Whether an array of rows of `dim` elements with these extents and strides (in
+// elements) has rows that overlap, strides off 16 bytes or an extent past 2^62
+// bytes.  Strides along an extent of 1 do not matter.
+struct Axis {
+  int64_t extent, stride;
+};
+const char* bad_layout(Axis* axes, int n, int64_t dim, int elem) {
+  std::sort(axes, axes + n, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  __int128 span = dim;
+  for (int i = 0; i < n; ++i) {
+    if (axes[i].extent <= 1) continue;
+    if (axes[i].stride < 0 || (axes[i].stride * static_cast<__int128>(elem)) % 16 != 0) return "strides must be multiples of 16 bytes, >= 0";
+    if (axes[i].stride < span) return "rows overlap";
+    span += static_cast<__int128>(axes[i].stride) * (axes[i].extent - 1);
+    if (span * elem > (static_cast<__int128>(1) << 62)) return "strides too large";
+  }
+  return nullptr;
+}
+
+saki_status check_pool(const saki_kv_pool* p, const saki_kv_table* t) {
+  if (!p) return abi_fail(SAKI_E_NULLPTR, "pool descriptor is NULL");
+  if (p->dtype != SAKI_F32 && p->dtype != SAKI_BF16) return abi_fail(SAKI_E_DTYPE, "unknown pool dtype");
+  if (p->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_kv_pool.reserved must be 0");
+  if (p->n_kv_heads < 1 || p->n_kv_heads > 1024) return abi_fail(SAKI_E_SHAPE, "n_kv_heads outside [1, 1024]");
+  if (p->head_dim < 8 || p->head_dim > 256 || p->head_dim % 8 != 0)
+    return abi_fail(SAKI_E_SHAPE, "head_dim must be a multiple of 8, 8 .. 256");
+  if (p->n_layers < 1 || p->n_layers > 65536) return abi_fail(SAKI_E_SHAPE, "n_layers outside [1, 65536]");
+  if (!p->k || !p->v) return abi_fail(SAKI_E_NULLPTR, "pool k and v are required");
+  if (off(p->k, 16) || off(p->v, 16)) return abi_fail(SAKI_E_ALIGN, "pool bases must be 16-byte aligned");
+  Axis axes[4] = {{p->n_layers, p->layer_stride},
+                  {t->n_pages, p->page_stride},
+                  {p->n_kv_heads, p->head_stride},
+                  {t->page_size, p->token_stride}};
+  if (const char* why = bad_layout(axes, 4, p->head_dim, elem_bytes(p->dtype)))
+    return abi_fail(why[0] == 's' ? SAKI_E_ALIGN : SAKI_E_SHAPE, why);
+  return SAKI_OK;
+}
+
+saki_status check_tokens(const saki_kv_tokens* n, const saki_kv_table* t) {
+  if (!n) return abi_fail(SAKI_E_NULLPTR, "tokens descriptor is NULL");
+  if (n->n_tokens < 0 || n->n_tokens > INT32_MAX) return abi_fail(SAKI_E_SHAPE, "n_tokens outside [0, 2^31 - 1]");
+  if (n->shift < 0 || n->shift > MAX_TOKENS) return abi_fail(SAKI_E_VALUE, "shift outside [0, 2^30]");
+  if (n->offsets) {
+    if (off(n->offsets, 4)) return abi_fail(SAKI_E_ALIGN, "offsets must be 4-byte aligned");
+  } else if (n->n_new < 0 || n->n_tokens != t->n_seq * n->n_new) {
+    return abi_fail(SAKI_E_SHAPE, "without offsets, n_tokens must be n_seq * n_new, n_new >= 0");
+  }
+  return SAKI_OK;
+}
+
+saki_status check_heads(const saki_kv_heads* x, int64_t n_tokens, int64_t heads, const saki_kv_pool* p, bool out,
+                        const char* name) {
+  (void)name;
+  if (!x || !x->data) return abi_fail(SAKI_E_NULLPTR, "q, q_out, k, v, out: data is required");
+  if (off(x->data, 16)) return abi_fail(SAKI_E_ALIGN, "token arrays must be 16-byte aligned");
+  const int e = elem_bytes(p->dtype);
+  const int64_t lim = int64_t{1} << 56;
+  if ((n_tokens > 1 && (x->token_stride < 0 || x->token_stride > lim / n_tokens || x->token_stride * e % 16 != 0)) ||
+      (heads > 1 && (x->head_stride < 0 || x->head_stride > lim / heads || x->head_stride * e % 16 != 0)))
+    return abi_fail(SAKI_E_ALIGN, "token array strides must be multiples of 16 bytes, >= 0");
+  if (out) {
+    Axis axes[2] = {{n_tokens, x->token_stride}, {heads, x->head_stride}};
+    if (const char* why = bad_layout(axes, 2, p->head_dim, e)) return abi_fail(SAKI_E_SHAPE, why);
+  }
+  return SAKI_OK;
+}
+
+saki_status check_ws(const void* ws, size_t have, int op, int64_t n, int64_t m) {
+  if (!ws) return abi_fail(SAKI_E_WORKSPACE, "workspace is NULL");
+  if (have < kv_workspace_bytes(op, n, m)) return abi_fail(SAKI_E_WORKSPACE, "workspace too small");
+  if (off(ws, 16)) return abi_fail(SAKI_E_ALIGN, "workspace must be 16-byte aligned");
+  return SAKI_OK;
+}
+
+KvTable device_table(const saki_kv_table* t) {
+  return KvTable{t->pages, t->length, t->held, t->refs, static_cast<int>(t->n_seq), static_cast<int>(t->max_pages),
+                 static_cast<int>(t->n_pages), __builtin_ctz(static_cast<unsigned>(t->page_size))};
+}
+
+KvPool device_pool(const saki_kv_pool* p, int64_t layer) {
+  const int64_t e = elem_bytes(p->dtype);
+  const int64_t base = p->n_layers > 1 ? layer * p->layer_stride * e : 0;
+  return KvPool{static_cast<char*>(p->k) + base,
+                static_cast<char*>(p->v) + base,
+                p->n_layers > 1 ? p->layer_stride * e : 0,
+                p->page_stride * e,
+                p->n_kv_heads > 1 ? p->head_stride * e : 0,
+                p->token_stride * e,
+                static_cast<int>(p->n_layers),
+                p->n_kv_heads,
+                p->head_dim};
+}
+
+KvTokens device_tokens(const saki_kv_tokens* n) {
+  return KvTokens{n->offsets, static_cast<int>(n->n_tokens), n->n_new, n->shift};
+}
+
+KvStrides device_heads(const saki_kv_heads* x, const saki_kv_pool* p) {
+  const int64_t e = elem_bytes(p->dtype);
+  return x ? KvStrides{static_cast<char*>(x->data), x->token_stride * e, x->head_stride * e} : KvStrides{nullptr, 0, 0};
+}
+
+int pow2_dim(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// Slots for partial sums: items of units that are split, at most twice the items
+// aimed at (a unit of more than one item has at least half of each of them full).
+constexpr int64_t SLOTS = 2 * KV_ATT_ITEMS;
+
+struct ReserveWs {
+  int64_t want, moves, n_moves, writers, last, list, bytes;
+};
+ReserveWs reserve_ws(int64_t n_seq, int64_t n_pages) {
+  ReserveWs w{};
+  w.want = 16;  // after the count of moves
+  w.moves = w.want + up16(n_seq * static_cast<int64_t>(sizeof(KvWant)));
+  w.writers = w.moves + up16(n_seq * static_cast<int64_t>(sizeof(KvMove)));
+  w.last = w.writers + up16(n_pages * 4);
+  w.list = w.last + up16(n_pages * 4);
+  w.bytes = w.list + up16(n_pages * 4);
+  return w;
+}
+
+struct CompactWs {
+  int64_t to, holes, live, moves, bytes;
+};
+CompactWs compact_ws(int64_t n_pages) {
+  CompactWs w{};
+  w.to = 16;  // after n_live and the count of moves
+  w.holes = w.to + up16(n_pages * 4);
+  w.live = w.holes + up16(n_pages * 4);
+  w.moves = w.live + up16(n_pages * 4);
+  w.bytes = w.moves + up16((n_pages / 2 + 1) * static_cast<int64_t>(sizeof(KvMove)));
+  return w;
+}
+
+KvCopyParams copy_params(const saki_kv_pool* pool, const KvMove* moves, const int32_t* n_moves) {
+  KvCopyParams c{};
+  c.p = device_pool(pool, 0);
+  c.moves = moves;
+  c.n_moves = n_moves;
+  c.row_chunks = pool->head_dim * elem_bytes(pool->dtype) / 16;
+  return c;
+}
+
+// Workgroups that copy: what keeps the memory busy, and no more than units.
+int copy_groups(int64_t most_moves, const saki_kv_pool* pool, int cus) {
+  const int64_t most = 8 * static_cast<int64_t>(cus);
+  const int64_t per_page = 2 * pool->n_layers * pool->n_kv_heads;
+  return static_cast<int>(most_moves < most / per_page + 1 ? std::min(most, most_moves * per_page) : most);
+}
+
+template <typename T>
+void launch_append(const KvAppendParams& P, bool interleaved, bool vec, hipStream_t st) {
+  const auto f = interleaved ? (vec ? kv_append_kernel<T, true, true> : kv_append_kernel<T, true, false>)
+                             : (vec ? kv_append_kernel<T, false, true> : kv_append_kernel<T, false, false>);
+  hipLaunchKernelGGL(f, dim3(static_cast<unsigned>(P.n.n_tokens)), dim3(KV_APPEND_NT), 0, st, P);
+}
+
+}  // namespace
+
+size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
+  if (n <= 0 || m <= 0) return 0;
+  switch (op) {
+    case SAKI_OP_KV_RESERVE:
+      return n > MAX_SEQ || m > MAX_TOKENS ? 0 : static_cast<size_t>(reserve_ws(n, m).bytes);
+    case SAKI_OP_KV_COMPACT:
+      return m > MAX_TOKENS ? 0 : static_cast<size_t>(compact_ws(m).bytes);
+    case SAKI_OP_KV_ATTENTION: {
+      const int64_t rows = n <= 16 ? 16 : n <= 32 ? 32 : KV_ATT_ROWS;
+      return static_cast<size_t>(SLOTS * rows * (pow2_dim(m) + 2) * 4);
+    }
+    default:
+      return 0;
+  }
+}
+
+}  // namespace saki
+
+using namespace saki;
+
+extern "C" {
+
+saki_status saki_kv_reserve(const saki_kv_table* table, const saki_kv_pool* pool, const int32_t* n_new,
+                            int32_t uniform, uint8_t* status, void* ws, size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  st = check_pool(pool, table);
+  if (st != SAKI_OK) return st;
+  if (!n_new && uniform < 0) return abi_fail(SAKI_E_VALUE, "uniform < 0");
+  if (off(n_new, 4)) return abi_fail(SAKI_E_ALIGN, "n_new must be 4-byte aligned");
+  if (table->n_seq == 0) return abi_ok();
+  st = check_ws(ws, ws_bytes, SAKI_OP_KV_RESERVE, table->n_seq, table->n_pages);
+  if (st != SAKI_OK) return st;
+  int cus = 0;
+  st = abi_cus(&cus);
+  if (st != SAKI_OK) return st;
+  char* w = static_cast<char*>(ws);
+  const ReserveWs at = reserve_ws(table->n_seq, table->n_pages);
+  KvReserveParams P{};
+  P.t = device_table(table);
+  P.n_new = n_new;
+  P.uniform = uniform;
+  P.status = status;
+  P.want = reinterpret_cast<KvWant*>(w + at.want);
+  P.writers = reinterpret_cast<int32_t*>(w + at.writers);
+  P.last = reinterpret_cast<int32_t*>(w + at.last);
+  P.list = reinterpret_cast<int32_t*>(w + at.list);
+  P.moves = reinterpret_cast<KvMove*>(w + at.moves);
+  P.n_moves = reinterpret_cast<int32_t*>(w);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(kv_reserve_kernel, dim3(1), dim3(KV_PLAN_NT), 0, hs, P);
+  st = abi_launched(hipGetLastError(), "kv_reserve_kernel");
+  if (st != SAKI_OK) return st;
+  hipLaunchKernelGGL(kv_copy_kernel, dim3(copy_groups(table->n_seq, pool, cus)), dim3(KV_COPY_NT), 0, hs,
+                     copy_params(pool, P.moves, P.n_moves));
+  st = abi_launched(hipGetLastError(), "kv_copy_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+saki_status saki_kv_commit(const saki_kv_table* table, const int32_t* delta, const uint8_t* done, uint8_t* status,
+                           saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  if (!delta && !done) return abi_fail(SAKI_E_NULLPTR, "delta or done is required");
+  if (off(delta, 4)) return abi_fail(SAKI_E_ALIGN, "delta must be 4-byte aligned");
+  if (table->n_seq == 0) return abi_ok();
+  const KvCommitParams P{device_table(table), delta, done, status};
+  constexpr int PER = 256 / KV_WAVE;
+  hipLaunchKernelGGL(kv_commit_kernel, dim3(static_cast<unsigned>((table->n_seq + PER - 1) / PER)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), P);
+  st = abi_launched(hipGetLastError(), "kv_commit_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+saki_status saki_kv_fork(const saki_kv_table* table, int64_t n, const int32_t* src, const int32_t* dst,
+                         uint8_t* status, saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  if (n < 0 || n > table->n_seq) return abi_fail(SAKI_E_SHAPE, "n outside [0, n_seq]");
+  if (n == 0) return abi_ok();
+  if (!src || !dst) return abi_fail(SAKI_E_NULLPTR, "src and dst are required");
+  if (off(src, 4) || off(dst, 4)) return abi_fail(SAKI_E_ALIGN, "src and dst must be 4-byte aligned");
+  const KvForkParams P{device_table(table), src, dst, status, static_cast<int>(n)};
+  constexpr int PER = 256 / KV_WAVE;
+  hipLaunchKernelGGL(kv_fork_kernel, dim3(static_cast<unsigned>((n + PER - 1) / PER)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), P);
+  st = abi_launched(hipGetLastError(), "kv_fork_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+saki_status saki_kv_compact(const saki_kv_table* table, const saki_kv_pool* pool, int32_t* n_live, void* ws,
+                            size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  st = check_pool(pool, table);
+  if (st != SAKI_OK) return st;
+  if (off(n_live, 4)) return abi_fail(SAKI_E_ALIGN, "n_live must be 4-byte aligned");
+  if (table->n_seq == 0) return abi_ok();
+  st = check_ws(ws, ws_bytes, SAKI_OP_KV_COMPACT, table->n_seq, table->n_pages);
+  if (st != SAKI_OK) return st;
+  int cus = 0;
+  st = abi_cus(&cus);
+  if (st != SAKI_OK) return st;
+  char* w = static_cast<char*>(ws);
+  const CompactWs at = compact_ws(table->n_pages);
+  KvCompactParams P{};
+  P.t = device_table(table);
+  P.n_moves = reinterpret_cast<int32_t*>(w);
+  P.n_live = reinterpret_cast<int32_t*>(w + 4);
+  P.n_live_out = n_live;
+  P.to = reinterpret_cast<int32_t*>(w + at.to);
+  P.holes = reinterpret_cast<int32_t*>(w + at.holes);
+  P.live = reinterpret_cast<int32_t*>(w + at.live);
+  P.moves = reinterpret_cast<KvMove*>(w + at.moves);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(kv_compact_kernel, dim3(1), dim3(KV_PLAN_NT), 0, hs, P);
+  st = abi_launched(hipGetLastError(), "kv_compact_kernel");
+  if (st != SAKI_OK) return st;
+  KvMoveParams M{};
+  M.c = copy_params(pool, P.moves, P.n_moves);
+  M.t = P.t;
+  M.n_live = P.n_live;
+  M.to = P.to;
+  constexpr int PER = KV_COPY_NT / KV_WAVE;
+  M.table_groups = static_cast<int>(std::min<int64_t>((table->n_seq + PER - 1) / PER, cus));
+  const int grid = M.table_groups + copy_groups(table->n_pages / 2 + 1, pool, cus);
+  hipLaunchKernelGGL(kv_move_kernel, dim3(grid), dim3(KV_COPY_NT), 0, hs, M);
+  st = abi_launched(hipGetLastError(), "kv_move_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+saki_status saki_kv_append(const saki_kv_table* table, const saki_kv_pool* pool, int64_t layer,
+                           const saki_kv_tokens* tokens, const saki_kv_rope* rope, int32_t n_q_heads,
+                           const saki_kv_heads* q, const saki_kv_heads* q_out, const saki_kv_heads* k,
+                           const saki_kv_heads* v, saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  st = check_pool(pool, table);
+  if (st != SAKI_OK) return st;
+  if (layer < 0 || layer >= pool->n_layers) return abi_fail(SAKI_E_SHAPE, "layer outside [0, n_layers)");
+  st = check_tokens(tokens, table);
+  if (st != SAKI_OK) return st;
+  if (rope) {
+    if (rope->rotary_dim < 0 || rope->rotary_dim > pool->head_dim || rope->rotary_dim % 2 != 0)
+      return abi_fail(SAKI_E_SHAPE, "rotary_dim must be even, 0 .. head_dim");
+    if (rope->interleaved != 0 && rope->interleaved != 1) return abi_fail(SAKI_E_VALUE, "interleaved must be 0 or 1");
+    if (!isfinite(rope->amplitude)) return abi_fail(SAKI_E_VALUE, "amplitude is not finite");
+    if (rope->rotary_dim > 0 && !rope->freq) return abi_fail(SAKI_E_NULLPTR, "freq is required");
+    if (off(rope->freq, 8)) return abi_fail(SAKI_E_ALIGN, "freq must be 8-byte aligned");
+  }
+  if (n_q_heads < 0 || n_q_heads > 65536) return abi_fail(SAKI_E_SHAPE, "n_q_heads outside [0, 65536]");
+  if ((n_q_heads > 0) != (q != nullptr) || (q == nullptr) != (q_out == nullptr))
+    return abi_fail(SAKI_E_NULLPTR, "q, q_out and n_q_heads > 0 go together");
+  if (table->n_seq == 0 || tokens->n_tokens == 0) return abi_ok();
+  const int64_t n = tokens->n_tokens;
+  if (q) {
+    st = check_heads(q, n, n_q_heads, pool, false, "q");
+    if (st != SAKI_OK) return st;
+    st = check_heads(q_out, n, n_q_heads, pool, true, "q_out");
+    if (st != SAKI_OK) return st;
+  }
+  st = check_heads(k, n, pool->n_kv_heads, pool, false, "k");
+  if (st != SAKI_OK) return st;
+  st = check_heads(v, n, pool->n_kv_heads, pool, false, "v");
+  if (st != SAKI_OK) return st;
+  KvAppendParams P{};
+  P.t = device_table(table);
+  P.p = device_pool(pool, layer);
+  P.n = device_tokens(tokens);
+  P.freq = rope ? rope->freq : nullptr;
+  P.pairs = rope ? rope->rotary_dim / 2 : 0;
+  P.amplitude = rope ? rope->amplitude : 1.0f;
+  P.n_q_heads = n_q_heads;
+  P.q = device_heads(q, pool);
+  P.q_out = device_heads(q_out, pool);
+  P.k = device_heads(k, pool);
+  P.v = device_heads(v, pool);
+  const bool inter = P.pairs > 0 && rope->interleaved != 0;
+  const bool vec = P.pairs % (inter ? 4 : 8) == 0;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (pool->dtype == SAKI_BF16)
+    launch_append<uint16_t>(P, inter, vec, hs);
+  else
+    launch_append<float>(P, inter, vec, hs);
+  st = abi_launched(hipGetLastError(), "kv_append_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* pool, int64_t layer,
+                              const saki_kv_tokens* tokens, int32_t n_q_heads, const saki_kv_heads* q,
+                              const saki_kv_heads* out, float* lse, float scale, int32_t window, int32_t sinks,
+                              void* ws, size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_table(table);
+  if (st != SAKI_OK) return st;
+  st = check_pool(pool, table);
+  if (st != SAKI_OK) return st;
+  if (layer < 0 || layer >= pool->n_layers) return abi_fail(SAKI_E_SHAPE, "layer outside [0, n_layers)");
+  st = check_tokens(tokens, table);
+  if (st != SAKI_OK) return st;
+  if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % pool->n_kv_heads != 0)
+    return abi_fail(SAKI_E_SHAPE, "n_q_heads must be a multiple of n_kv_heads, at most 65536");
+  if (!isfinite(scale)) return abi_fail(SAKI_E_VALUE, "scale is not finite");
+  if (window < 0 || sinks < 0) return abi_fail(SAKI_E_VALUE, "window < 0 or sinks < 0");
+  if (off(lse, 4)) return abi_fail(SAKI_E_ALIGN, "lse must be 4-byte aligned");
+  if (table->n_seq == 0 || tokens->n_tokens == 0) return abi_ok();
+  const int64_t n = tokens->n_tokens;
+  st = check_heads(q, n, n_q_heads, pool, false, "q");
+  if (st != SAKI_OK) return st;
+  st = check_heads(out, n, n_q_heads, pool, true, "out");
+  if (st != SAKI_OK) return st;
+  st = check_ws(ws, ws_bytes, SAKI_OP_KV_ATTENTION, n * n_q_heads, pool->head_dim);
+  if (st != SAKI_OK) return st;
+
+  const bool bf = pool->dtype == SAKI_BF16;
+  const int dp = pow2_dim(pool->head_dim);
+  const int group = n_q_heads / pool->n_kv_heads;
+  // rows of a tile: those of a sequence of mean length
+  const int64_t mean = n * group / table->n_seq;
+  const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
+  const int tiles = std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
+  const int64_t rows = 16 * tiles;
+  int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
+                                  : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
+  units *= pool->n_kv_heads;
+  if (units > INT32_MAX - KV_ATT_ITEMS) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  KvAttnParams P{};
+  P.t = device_table(table);
+  P.p = device_pool(pool, layer);
+  P.n = device_tokens(tokens);
+  P.q = device_heads(q, pool);
+  P.out = device_heads(out, pool);
+  P.lse = lse;
+  P.n_q_heads = n_q_heads;
+  P.group = group;
+  P.scale2 = scale * KV_LOG2E;
+  P.window = window;
+  P.sinks = sinks;
+  P.items = KV_ATT_ITEMS;
+  P.slots = static_cast<int>(SLOTS);
+  P.part = static_cast<float*>(ws);
+  P.part_ml = P.part + SLOTS * rows * dp;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  // without a second workgroup's worth of keys in any sequence nothing is split
+  const int64_t most_blocks = table->max_pages * table->page_size / (bf ? 32 : 16) + 1;
+  const bool join = most_blocks > 2 * KV_ATT_WAVES;
+  hipError_t e;
+  if (bf)
+    e = dp == 64    ? launch_kv_attention<uint16_t, 64>(P, tiles, units, join, hs)
+        : dp == 128 ? launch_kv_attention<uint16_t, 128>(P, tiles, units, join, hs)
+                    : launch_kv_attention<uint16_t, 256>(P, tiles, units, join, hs);
+  else
+    e = dp == 64    ? launch_kv_attention<float, 64>(P, tiles, units, join, hs)
+        : dp == 128 ? launch_kv_attention<float, 128>(P, tiles, units, join, hs)
+                    : launch_kv_attention<float, 256>(P, tiles, units, join, hs);
+  st = abi_launched(e, "kv_attention_kernel");
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+}  // extern "C"

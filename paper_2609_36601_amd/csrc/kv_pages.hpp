@@ -1,0 +1,460 @@
+// The pages of a key-value cache: room for new tokens with copies of shared last
+// pages, commit and rollback, forks, compaction.
+//
+// A page is free iff its reference count is 0; there is no list of free pages.
+// Giving pages back is then a decrement and sharing them an increment, whose
+// order does not matter, and the pages given out (the lowest free ids, to the
+// sequences in order) are a function of the table alone.  Taking pages has to
+// find free ones among n_pages counts: one workgroup reads them all.
+#pragma once
+
+#include "kv_common.hpp"
+
+namespace saki {
+
+constexpr int KV_PLAN_NT = 1024;
+constexpr int KV_PLAN_WAVES = KV_PLAN_NT / KV_WAVE;
+
+struct KvMove {  // a page to copy: its first `tokens` slots
+  int32_t src, dst, tokens;
+};
+
+// What reserve keeps of a sequence between its steps.
+struct KvWant {
+  int32_t slot;   // table column of the page that takes the next token; -1: no copy in question
+  int32_t page;   // that page
+  int32_t fresh;  // new pages
+  int32_t fill;   // length % page_size
+};
+
+struct KvReserveParams {
+  KvTable t;
+  const int32_t* n_new;
+  int uniform;
+  uint8_t* status;
+  KvWant* want;       // [n_seq]
+  int32_t* writers;   // [n_pages] sequences of this call that write to a shared page
+  int32_t* last;      // [n_pages] the last of them
+  int32_t* list;      // [n_pages] free pages, ascending, as many as are taken
+  KvMove* moves;      // [n_seq]
+  int32_t* n_moves;
+};
+
+// Free pages among refs[first .. first + 256): bit e of the lane's mask stands for
+// page first + 4 lane + e.
+__device__ __forceinline__ int kv_free_mask(const int32_t* refs, int n_pages, int first, bool vec) {
+  const int p = first + 4 * (threadIdx.x & (KV_WAVE - 1));
+  int m = 0;
+  if (vec && p + 4 <= n_pages) {
+    const int4 r = *reinterpret_cast<const int4*>(refs + p);
+    m = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (p + e < n_pages) m |= (refs[p + e] == 0) << e;
+  }
+  return m;
+}
+
+// Pages of each wave: whole groups of 256, in order.
+__device__ __forceinline__ int kv_pages_per_wave(int n_pages) {
+  return ((n_pages + KV_PLAN_WAVES * 256 - 1) / (KV_PLAN_WAVES * 256)) * 256;
+}
+
+// Free pages of this wave's part of the pool.
+__device__ __forceinline__ int kv_count_free(const int32_t* refs, int n_pages, bool vec) {
+  const int per = kv_pages_per_wave(n_pages);
+  const int first = (threadIdx.x / KV_WAVE) * per;
+  int mine = 0;
+#pragma unroll 8
+  for (int g = 0; g < per; g += 256) mine += __popc(kv_free_mask(refs, n_pages, first + g, vec));
+  return kv_wave_sum(mine);
+}
+
+__global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams P) {
+  const KvTable& t = P.t;
+  const int tid = threadIdx.x, wave = tid / KV_WAVE, lane = tid & (KV_WAVE - 1);
+  const int page_mask = (1 << t.shift) - 1;
+  __shared__ int free_of[KV_PLAN_WAVES];
+  __shared__ long long part64[KV_PLAN_WAVES];
+  const bool vec = (reinterpret_cast<uintptr_t>(t.refs) & 15u) == 0;
+
+  const int counted = kv_count_free(t.refs, t.n_pages, vec);
+  if (lane == 0) free_of[wave] = counted;
+
+  // 1. what every sequence asks for
+  bool shares = false;
+  for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
+    const int n = P.n_new ? P.n_new[b] : P.uniform;
+    const int L = t.length[b], H = t.held[b];
+    KvWant w{-1, -1, 0, 0};
+    int st = SAKI_KV_OK;
+    if (n < 0 || L < 0 || H < 0 || H > t.max_pages || static_cast<int64_t>(L) > (static_cast<int64_t>(H) << t.shift)) {
+      st = SAKI_KV_BAD;
+    } else if (n > 0) {
+      const int64_t need = (static_cast<int64_t>(L) + n + page_mask) >> t.shift;
+      if (need > t.max_pages) {
+        st = SAKI_KV_TOO_LONG;
+      } else {
+        w.fresh = need > H ? static_cast<int>(need) - H : 0;
+        w.fill = L & page_mask;
+        if (w.fill) {
+          const int slot = L >> t.shift;
+          const int p = t.pages[static_cast<int64_t>(b) * t.max_pages + slot];
+          if (p < 0 || p >= t.n_pages) {
+            st = SAKI_KV_BAD;
+            w.fresh = 0;
+          } else if (t.refs[p] > 1) {
+            w.slot = slot;
+            w.page = p;
+            P.writers[p] = 0;
+            P.last[p] = -1;
+            shares = true;
+          }
+        }
+      }
+    }
+    P.want[b] = w;
+    if (P.status) P.status[b] = static_cast<uint8_t>(st);
+  }
+  // 2. of a shared page's writers, the last keeps it if all its holders write
+  const bool any_shares = __syncthreads_or(shares);
+  if (any_shares) {
+    for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
+      const KvWant w = P.want[b];
+      if (w.slot < 0) continue;
+      atomicAdd(&P.writers[w.page], 1);
+      atomicMax(&P.last[w.page], b);
+    }
+    __syncthreads();
+    for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
+      const KvWant w = P.want[b];
+      // (atomic reads: the counts were changed in the L2)
+      if (w.slot >= 0 && __hip_atomic_load(&P.writers[w.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == t.refs[w.page] &&
+          __hip_atomic_load(&P.last[w.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == b)
+        P.want[b].slot = -1;
+    }
+    __syncthreads();
+  }
+  // 3. how much that is: the call takes all of it or nothing
+  long long asked = 0, total64 = 0;
+  for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
+    const KvWant w = P.want[b];
+    asked += w.fresh + (w.slot >= 0);
+  }
+  kv_block_scan<KV_PLAN_NT, long long>(asked, part64, &total64);
+  int before = 0, n_free = 0;
+  for (int w = 0; w < KV_PLAN_WAVES; ++w) {
+    if (w < wave) before += free_of[w];
+    n_free += free_of[w];
+  }
+  if (total64 > n_free) {
+    if (P.status)
+      for (int b = tid; b < t.n_seq; b += KV_PLAN_NT)
+        if ((P.n_new ? P.n_new[b] : P.uniform) > 0 && P.status[b] == SAKI_KV_OK) P.status[b] = SAKI_KV_NO_PAGES;
+    if (tid == 0) *P.n_moves = 0;
+    return;
+  }
+  const int total = static_cast<int>(total64);
+  if (total == 0) {
+    if (tid == 0) *P.n_moves = 0;
+    return;
+  }
+  // 4. the lowest `total` free pages, ascending
+  {
+    const int per = kv_pages_per_wave(t.n_pages);
+    const int first = wave * per;
+    int rank = before;
+    for (int g = 0; g < per && rank < total; g += 256) {
+      const int m = kv_free_mask(t.refs, t.n_pages, first + g, vec);
+      const int c = __popc(m);
+      const int in = kv_wave_scan(c);
+      int at = rank + in - c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((m >> e) & 1) {
+          if (at < total) P.list[at] = first + g + 4 * lane + e;
+          ++at;
+        }
+      rank += __shfl(in, KV_WAVE - 1);
+    }
+  }
+  __syncthreads();
+  // 5. each sequence its share, in order; long shares by whole waves
+  int base = 0, n_moves = 0;
+  __shared__ int long_from[KV_PLAN_NT];
+  for (int b0 = 0; b0 < t.n_seq; b0 += KV_PLAN_NT) {
+    const int b = b0 + tid;
+    const KvWant w = b < t.n_seq ? P.want[b] : KvWant{-1, -1, 0, 0};
+    const bool copy = w.slot >= 0;
+    // (both prefix sums in one: copies in the upper half)
+    long long sum = 0;
+    const long long mine = (static_cast<long long>(copy) << 32) | static_cast<unsigned>(w.fresh + copy);
+    const long long at = kv_block_scan<KV_PLAN_NT, long long>(mine, part64, &sum);
+    int from = base + static_cast<int>(at & 0xffffffff);
+    if (copy) {
+      const int to = P.list[from];
+      P.moves[n_moves + static_cast<int>(at >> 32)] = KvMove{w.page, to, w.fill};
+      t.pages[static_cast<int64_t>(b) * t.max_pages + w.slot] = to;
+      t.refs[to] = 1;
+      atomicSub(&t.refs[w.page], 1);
+      ++from;
+    }
+    const bool is_long = w.fresh > 8;
+    if (w.fresh > 0) {
+      const int H = t.held[b];
+      if (!is_long)
+        for (int i = 0; i < w.fresh; ++i) {
+          const int id = P.list[from + i];
+          t.pages[static_cast<int64_t>(b) * t.max_pages + H + i] = id;
+          t.refs[id] = 1;
+        }
+    }
+    long_from[tid] = is_long ? from : -1;
+    if (__syncthreads_or(is_long)) {
+      for (int s = wave; s < KV_PLAN_NT && b0 + s < t.n_seq; s += KV_PLAN_WAVES) {
+        const int f = long_from[s];
+        if (f < 0) continue;
+        const int H = t.held[b0 + s], n = P.want[b0 + s].fresh;
+        for (int i = lane; i < n; i += KV_WAVE) {
+          const int id = P.list[f + i];
+          t.pages[static_cast<int64_t>(b0 + s) * t.max_pages + H + i] = id;
+          t.refs[id] = 1;
+        }
+      }
+      __syncthreads();
+    }
+    if (w.fresh > 0) t.held[b] += w.fresh;
+    base += static_cast<int>(sum & 0xffffffff);
+    n_moves += static_cast<int>(sum >> 32);
+  }
+  if (tid == 0) *P.n_moves = n_moves;
+}
+
+// Copies pages: a unit is the slots of one head of one page of one layer, of the
+// keys or the values; workgroups take units in turn.
+struct KvCopyParams {
+  KvPool p;
+  const KvMove* moves;
+  const int32_t* n_moves;
+  int row_chunks;  // 16-byte pieces of a token's row
+};
+
+constexpr int KV_COPY_NT = 256;
+
+__device__ __forceinline__ void kv_copy_units(const KvCopyParams& P, int64_t unit, int64_t step) {
+  const int64_t n = static_cast<int64_t>(*P.n_moves) * P.p.n_layers * 2 * P.p.n_heads;
+  for (; unit < n; unit += step) {
+    int64_t u = unit;
+    const int h = static_cast<int>(u % P.p.n_heads);
+    u /= P.p.n_heads;
+    char* base = (u & 1) ? P.p.v : P.p.k;
+    u >>= 1;
+    const int64_t layer = u % P.p.n_layers;
+    const KvMove mv = P.moves[u / P.p.n_layers];
+    base += layer * P.p.layer_stride + h * P.p.head_stride;
+    const char* src = base + mv.src * P.p.page_stride;
+    char* dst = base + mv.dst * P.p.page_stride;
+    const int pieces = mv.tokens * P.row_chunks;
+    for (int i = threadIdx.x; i < pieces; i += KV_COPY_NT) {
+      const int tok = i / P.row_chunks, c = i - tok * P.row_chunks;
+      const int64_t off = tok * P.p.token_stride + c * 16;
+      *reinterpret_cast<uint4*>(dst + off) = *reinterpret_cast<const uint4*>(src + off);
+    }
+  }
+}
+
+__global__ __launch_bounds__(KV_COPY_NT) void kv_copy_kernel(KvCopyParams P) {
+  kv_copy_units(P, blockIdx.x, gridDim.x);
+}
+
+// One wave per sequence: the new length, and the pages behind it given back.
+struct KvCommitParams {
+  KvTable t;
+  const int32_t* delta;
+  const uint8_t* done;
+  uint8_t* status;
+};
+
+__global__ __launch_bounds__(256) void kv_commit_kernel(KvCommitParams P) {
+  const KvTable& t = P.t;
+  const int b = blockIdx.x * (256 / KV_WAVE) + threadIdx.x / KV_WAVE, lane = threadIdx.x & (KV_WAVE - 1);
+  if (b >= t.n_seq) return;
+  const int L = t.length[b], H = t.held[b];
+  const bool over = P.done && P.done[b] != 0;
+  const int64_t to = over ? 0 : static_cast<int64_t>(L) + (P.delta ? P.delta[b] : 0);
+  const bool fine = H >= 0 && H <= t.max_pages && L >= 0 && to >= 0 && to <= (static_cast<int64_t>(H) << t.shift);
+  if (fine) {
+    const int keep = static_cast<int>((to + (1 << t.shift) - 1) >> t.shift);
+    int32_t* row = t.pages + static_cast<int64_t>(b) * t.max_pages;
+    for (int i = keep + lane; i < H; i += KV_WAVE) {
+      const int p = row[i];
+      row[i] = -1;
+      if (p >= 0 && p < t.n_pages) atomicSub(&t.refs[p], 1);
+    }
+    if (lane == 0) {
+      t.length[b] = static_cast<int>(to);
+      if (keep != H) t.held[b] = keep;
+    }
+  }
+  if (P.status && lane == 0) P.status[b] = fine ? SAKI_KV_OK : SAKI_KV_BAD;
+}
+
+// One wave per pair.  Whether a pair is allowed is decided from the lists and
+// from entries that no allowed pair changes: dst of an allowed pair is changed
+// by its own wave alone, and no allowed pair's src is any pair's dst.
+struct KvForkParams {
+  KvTable t;
+  const int32_t* src;
+  const int32_t* dst;
+  uint8_t* status;
+  int n;
+};
+
+__global__ __launch_bounds__(256) void kv_fork_kernel(KvForkParams P) {
+  const KvTable& t = P.t;
+  const int i = blockIdx.x * (256 / KV_WAVE) + threadIdx.x / KV_WAVE, lane = threadIdx.x & (KV_WAVE - 1);
+  if (i >= P.n) return;
+  const int s = P.src[i], d = P.dst[i];
+  bool fine = s >= 0 && s < t.n_seq && d >= 0 && d < t.n_seq;
+  bool clash = false;
+  for (int j = lane; j < P.n; j += KV_WAVE) {
+    const int o = P.dst[j];
+    clash |= (o == d && j < i) || P.src[j] == d;
+  }
+  fine = fine && !__any(clash);
+  int L = 0, H = 0;
+  if (fine) {
+    L = t.length[s];
+    H = t.held[s];
+    fine = t.length[d] == 0 && t.held[d] == 0 && L >= 0 && H >= 0 && H <= t.max_pages &&
+           static_cast<int64_t>(L) <= (static_cast<int64_t>(H) << t.shift);
+  }
+  if (fine) {
+    const int n = (L + (1 << t.shift) - 1) >> t.shift;
+    const int32_t* from = t.pages + static_cast<int64_t>(s) * t.max_pages;
+    int32_t* to = t.pages + static_cast<int64_t>(d) * t.max_pages;
+    for (int j = lane; j < n; j += KV_WAVE) {
+      const int p = from[j];
+      to[j] = p;
+      if (p >= 0 && p < t.n_pages) atomicAdd(&t.refs[p], 1);
+    }
+    if (lane == 0) {
+      t.length[d] = L;
+      t.held[d] = n;
+    }
+  }
+  if (P.status && lane == 0) P.status[i] = fine ? SAKI_KV_OK : SAKI_KV_BAD;
+}
+
+// Compaction's plan: the holes below n_live and the live pages from there on, both
+// ascending, are paired; counts move with the pages.
+struct KvCompactParams {
+  KvTable t;
+  int32_t* n_live;  // in the workspace
+  int32_t* n_live_out;
+  int32_t* to;  // [n_pages] where a live page >= n_live goes; -1: a free one
+  int32_t* holes;
+  int32_t* live;
+  KvMove* moves;
+  int32_t* n_moves;
+};
+
+__global__ __launch_bounds__(KV_PLAN_NT) void kv_compact_kernel(KvCompactParams P) {
+  const KvTable& t = P.t;
+  const int tid = threadIdx.x, wave = tid / KV_WAVE, lane = tid & (KV_WAVE - 1);
+  __shared__ int free_of[KV_PLAN_WAVES], holes_of[KV_PLAN_WAVES];
+  const bool vec = (reinterpret_cast<uintptr_t>(t.refs) & 15u) == 0;
+  const int counted = kv_count_free(t.refs, t.n_pages, vec);
+  if (lane == 0) free_of[wave] = counted;
+  __syncthreads();
+  int free_before = 0, n_free = 0;
+  for (int w = 0; w < KV_PLAN_WAVES; ++w) {
+    if (w < wave) free_before += free_of[w];
+    n_free += free_of[w];
+  }
+  const int n_live = t.n_pages - n_free;
+  const int per = kv_pages_per_wave(t.n_pages);
+  const int first = wave * per;
+  // ranks among all free and all live pages; of those, the holes are the free
+  // pages below n_live, which are the first ones, and the moving pages the last
+  int holes = 0;
+  int rank = free_before;
+  for (int g = 0; g < per; g += 256) {
+    const int m = kv_free_mask(t.refs, t.n_pages, first + g, vec);
+    const int c = __popc(m);
+    const int in = kv_wave_scan(c);
+    int f = rank + in - c;  // free pages before this lane's first
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int p = first + g + 4 * lane + e;
+      if (p >= t.n_pages) break;
+      const bool is_free = (m >> e) & 1;
+      if (is_free) {
+        if (p < n_live) {
+          P.holes[f] = p;
+          ++holes;
+        } else {
+          P.to[p] = -1;
+        }
+        ++f;
+      } else if (p >= n_live) {
+        // live pages before p: p - f; counted from the end, since how many live
+        // pages lie below n_live is not known yet
+        P.live[n_live - 1 - (p - f)] = p;
+      }
+    }
+    rank += __shfl(in, KV_WAVE - 1);
+  }
+  holes = kv_wave_sum(holes);
+  if (lane == 0) holes_of[wave] = holes;
+  __syncthreads();
+  int n = 0;
+  for (int w = 0; w < KV_PLAN_WAVES; ++w) n += holes_of[w];
+  // as many live pages lie from n_live on as holes below it
+  for (int i = tid; i < n; i += KV_PLAN_NT) {
+    const int src = P.live[n - 1 - i], dst = P.holes[i];
+    P.to[src] = dst;
+    P.moves[i] = KvMove{src, dst, 1 << t.shift};
+    t.refs[dst] = t.refs[src];
+    t.refs[src] = 0;
+  }
+  if (tid == 0) {
+    *P.n_moves = n;
+    *P.n_live = n_live;
+    if (P.n_live_out) *P.n_live_out = n_live;
+  }
+}
+
+// The moves, and the table's entries after them: the first workgroups take a
+// sequence a wave, the others copy.
+struct KvMoveParams {
+  KvCopyParams c;
+  KvTable t;
+  const int32_t* n_live;
+  const int32_t* to;
+  int table_groups;
+};
+
+__global__ __launch_bounds__(KV_COPY_NT) void kv_move_kernel(KvMoveParams P) {
+  if (static_cast<int>(blockIdx.x) >= P.table_groups) {
+    kv_copy_units(P.c, blockIdx.x - P.table_groups, gridDim.x - P.table_groups);
+    return;
+  }
+  if (*P.c.n_moves == 0) return;
+  const int wave = threadIdx.x / KV_WAVE, lane = threadIdx.x & (KV_WAVE - 1);
+  const int n_live = *P.n_live;
+  for (int b = blockIdx.x * (KV_COPY_NT / KV_WAVE) + wave; b < P.t.n_seq; b += P.table_groups * (KV_COPY_NT / KV_WAVE)) {
+    const int H = kv_held(P.t, b);
+    int32_t* row = P.t.pages + static_cast<int64_t>(b) * P.t.max_pages;
+    for (int i = lane; i < H; i += KV_WAVE) {
+      const int p = row[i];
+      if (p >= n_live && p < P.t.n_pages) {
+        const int to = P.to[p];
+        if (to >= 0) row[i] = to;
+      }
+    }
+  }
+}
+
+}  // namespace saki

@@ -15,6 +15,7 @@
 #include <string>
 
 #include "../../include/saki.h"
+#include "abi.hpp"
 #include "couple.hpp"
 #include "verify.hpp"
 
@@ -295,10 +296,23 @@ saki_status launch_route(const saki::RouteParams& P, int grid, hipStream_t st) {
 
 }  // namespace
 
+namespace saki {
+
+saki_status abi_fail(saki_status st, const char* msg) { return fail(st, msg); }
+
+saki_status abi_ok() { return ok(); }
+
+saki_status abi_launched(hipError_t e, const char* kernel) {
+  return e == hipSuccess ? SAKI_OK : fail(SAKI_E_LAUNCH, std::string(kernel) + ": " + hipGetErrorString(e));
+}
+
+saki_status abi_cus(int* cus) { return device_cus(cus); }
+
+}  // namespace saki
+
 extern "C" {
 
 size_t saki_workspace_bytes(int op, int64_t n_rows, int64_t vocab) {
-  (void)vocab;
   if (n_rows <= 0) return 0;
   switch (op) {
     case SAKI_OP_COUPLE:
@@ -311,6 +325,10 @@ size_t saki_workspace_bytes(int op, int64_t n_rows, int64_t vocab) {
       return 256;  // the work counter
     case SAKI_OP_SELECT:
       return loss_ws_bytes(n_rows);
+    case SAKI_OP_KV_RESERVE:
+    case SAKI_OP_KV_COMPACT:
+    case SAKI_OP_KV_ATTENTION:
+      return saki::kv_workspace_bytes(op, n_rows, vocab);
     default:
       return 0;
   }
