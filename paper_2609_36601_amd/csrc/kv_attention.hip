@@ -13,7 +13,11 @@ hipError_t launch(const KvAttnParams& P, int64_t units, bool join, hipStream_t s
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !join) return e;
   const unsigned split_units = static_cast<unsigned>(units < P.items ? units : P.items);
-  hipLaunchKernelGGL((kv_join_kernel<T, DP, R>), dim3(split_units), dim3(KV_ATT_NT), 0, st, P);
+  // one row a workgroup where that fills the card but little more, else four
+  if (split_units * 16 * R <= 4096)
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, R, 1>), dim3(split_units * 16 * R), dim3(KV_ATT_NT), 0, st, P);
+  else
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, R, 4>), dim3(split_units * 4 * R), dim3(KV_ATT_NT), 0, st, P);
   return hipGetLastError();
 }
 

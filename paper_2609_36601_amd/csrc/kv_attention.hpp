@@ -47,6 +47,7 @@ struct KvAttnParams {
   float* part;   // [slots][rows][DP] partial sums, then
   float* part_ml;  // [slots][rows][2] their maximum and sum
   int slots;
+  unsigned* split_units;  // how many units are split, for kv_join_kernel
 };
 
 // Blocks of BLK tokens that the rows of tokens [j0, j1) (positions p0 .. p1 - 1) see:
@@ -134,16 +135,22 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, int64_t item
   long long len = (all * Hk + P.items - 1) / P.items;
   if (len < 2 * KV_ATT_WAVES) len = 2 * KV_ATT_WAVES;
   auto splits_of = [&](const KvLoad& s) { return static_cast<int>((s.blocks + len - 1) / len); };
-  long long items = 0, slots = 0;
+  long long items = 0, slots = 0, split_units = 0;
   for (int b = b0; b < b1; ++b) {
     const KvLoad s = per == 1 ? keep : kv_load_of<ROWS, BLK>(P, b);
     const int n = splits_of(s);
+    if (n > 1) split_units += static_cast<long long>(s.tiles) * Hk;
     items += static_cast<long long>(s.tiles) * Hk * (JOIN ? n > 1 : n);
     if (n > 1) slots += static_cast<long long>(s.tiles) * Hk * n;
   }
   // (both sums in one scan: at most 2^31 items, as the grid is)
   long long sums = 0;
   const long long before = kv_block_scan<KV_ATT_NT, long long>((slots << 32) | items, part, &sums);
+  if (!JOIN && blockIdx.x == 0) {
+    long long n = 0;
+    kv_block_scan<KV_ATT_NT, long long>(split_units, part, &n);
+    if (tid == 0) *P.split_units = n < P.items ? static_cast<unsigned>(n) : static_cast<unsigned>(P.items);
+  }
   long long at = before & 0xffffffffll, slot = before >> 32;
   if (item >= at && item < at + items) {
     for (int b = b0; b < b1; ++b) {
@@ -175,8 +182,18 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, int64_t item
     }
   }
   __syncthreads();
-  *out = found;
-  return is_found != 0;
+  // (the same for the whole workgroup: in scalar registers)
+  const int* f = reinterpret_cast<const int*>(&found);
+  int* o = reinterpret_cast<int*>(out);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(KvItem) / 4); ++i) o[i] = __builtin_amdgcn_readfirstlane(f[i]);
+  return __builtin_amdgcn_readfirstlane(is_found) != 0;
+}
+
+// Workgroups that the registers of a CU hold (one wave of each on every SIMD).
+template <typename T>
+constexpr int kv_groups_per_cu(int dp, int r) {
+  return dp * r <= 64 ? 4 : dp * r <= 128 ? 3 : dp * r <= 256 ? 2 : 1;
 }
 
 template <typename T>
@@ -184,9 +201,24 @@ struct KvBlk {
   static constexpr int N = sizeof(T) == 2 ? 32 : 16;  // tokens of a wave's step
 };
 
+// Parts of a value (a pair of them in bf16): SIGN 0, the value if it is finite, else 0;
+// SIGN 1 (-1), one where it is +infinity (-infinity) or NaN, else 0.
+template <typename T, int SIGN>
+__device__ __forceinline__ uint32_t kv_select(uint32_t v) {
+  constexpr uint32_t EXP = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u, MAG = EXP | (EXP - 1);
+  constexpr uint32_t ONE = sizeof(T) == 2 ? 0x3f80u : 0x3f800000u, SIGN_BIT = MAG + 1;
+  auto one = [](uint32_t x) -> uint32_t {
+    const bool finite = (x & EXP) != EXP, nan = (x & MAG) > EXP, minus = (x & SIGN_BIT) != 0;
+    if (SIGN == 0) return finite ? x : 0u;
+    return !finite && (nan || minus == (SIGN < 0)) ? ONE : 0u;
+  };
+  if constexpr (sizeof(T) == 4) return one(v);
+  return one(v & 0xffffu) | one(v >> 16) << 16;
+}
+
 // One item: ROWS = 16 R rows, the blocks of its split dealt to the four waves.
 template <typename T, int DP, int R>
-__global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P) {
+__global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_attention_kernel(KvAttnParams P) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int BLK = KvBlk<T>::N;
   constexpr int ROWS = 16 * R;
@@ -201,7 +233,7 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
 
   KvItem it;
   if (!kv_find_item<ROWS, BLK, false>(P, blockIdx.x, &it)) return;
-  const int tid = threadIdx.x, wave = tid / KV_WAVE, lane = tid & (KV_WAVE - 1);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;
   const int row0 = it.tile * ROWS, rows = it.count * G;
@@ -246,43 +278,68 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
     const int mask = (1 << P.t.shift) - 1;
     const char* kb = P.p.k + it.head * P.p.head_stride;
     const char* vb = P.p.v + it.head * P.p.head_stride;
-    // the page of token `tok`, whose id is checked here
-    auto page_of = [&](int tok) {
-      const int id = row_pages[tok >> P.t.shift];
+    const int last = p1 - 1;  // no lane reads behind the tile's last token
+    // first token of block i
+    auto token_of = [&](int i) { return i < span.sinks ? i * BLK : span.lo + (i - span.sinks) * BLK; };
+    // The runs of 8 tokens that hold this lane's keys and values in the block at t0 (runs behind the
+    // last token: that token's); a run lies in one page, whose id is looked up once.
+    auto run_of = [&](int tok) { return tok <= last ? tok & ~7 : last & ~7; };
+    const int k_in = BF ? (c >> 2) * 8 : c, v_in = g * TOK;
+    int k_id = 0, v_id = 0;
+    auto load_ids = [&](int t0) {
+      k_id = row_pages[run_of(t0 + k_in) >> P.t.shift];
+      v_id = row_pages[run_of(t0 + v_in) >> P.t.shift];
+    };
+    auto page_at = [&](int id) {
       const bool in = id >= 0 && id < P.t.n_pages;
       bad |= !in;
       return static_cast<int64_t>(in ? id : 0) * P.p.page_stride;
     };
-    for (int i = from + wave; i < to; i += KV_ATT_WAVES) {
-      const int t0 = i < span.sinks ? i * BLK : span.lo + (i - span.sinks) * BLK;
-      const int last = p1 - 1;  // no lane reads behind the tile's last token
-      // keys: this lane's are tokens kt (and kt + 4)
-      uint4 kf[BF ? 2 : 1][QC];
+    uint4 kf[BF ? 2 : 1][QC];
+    uint32_t vr[TOK][VW];
+    const int token_stride = static_cast<int>(P.p.token_stride);
+    auto load_keys = [&](int t0) {
+      const int run = run_of(t0 + k_in);
+      const char* src = kb + page_at(k_id) + (g * 16);
 #pragma unroll
       for (int s = 0; s < (BF ? 2 : 1); ++s) {
-        int tok = BF ? t0 + (c >> 2) * 8 + (c & 3) + 4 * s : t0 + c;
+        int tok = BF ? run + (c & 3) + 4 * s : run + (c & 7);
         tok = tok < last ? tok : last;
-        const char* src = kb + page_of(tok) + (tok & mask) * P.p.token_stride;
+        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
 #pragma unroll
-        for (int e = 0; e < QC; ++e) {
-          const int d = e * (BF ? 32 : 16) + g * (BF ? 8 : 4);
-          kf[s][e] = d < D ? *reinterpret_cast<const uint4*>(src + d * sizeof(T)) : uint4{0, 0, 0, 0};
-        }
+        for (int e = 0; e < QC; ++e)
+          kf[s][e] = e * 64 + g * 16 < D * static_cast<int>(sizeof(T)) ? *reinterpret_cast<const uint4*>(at + e * 64)
+                                                                       : uint4{0, 0, 0, 0};
       }
-      // values: tokens vt0 .. vt0 + TOK - 1 (one page: pages hold whole runs of 8)
-      uint32_t vr[TOK][VW];
-      const int vt0 = t0 + g * TOK;
+    };
+    auto load_values = [&](int t0) {
+      const int run = run_of(t0 + v_in);
+      const char* src = vb + page_at(v_id) + c * NT * static_cast<int>(sizeof(T));
 #pragma unroll
       for (int e = 0; e < TOK; ++e) {
-        int tok = vt0 + e;
+        int tok = run + (BF ? 0 : v_in & 7) + e;
         tok = tok < last ? tok : last;
-        const char* src = vb + page_of(tok) + (tok & mask) * P.p.token_stride + c * NT * sizeof(T);
+        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
 #pragma unroll
         for (int w = 0; w < VC; ++w) {
-          const VPiece x = c * NT + w * VE < D ? reinterpret_cast<const VPiece*>(src)[w] : VPiece{};
+          const VPiece x = c * NT + w * VE < D ? reinterpret_cast<const VPiece*>(at)[w] : VPiece{};
           __builtin_memcpy(&vr[e][w * sizeof(VPiece) / 4], &x, sizeof(x));
         }
       }
+    };
+    // The next block's keys are loaded once this block's are multiplied, and its values
+    // once this block's are: both are under way while the rest of a block is computed.
+    int i = from + wave;
+    if (i < to) {
+      load_ids(token_of(i));
+      load_keys(token_of(i));
+      load_values(token_of(i));
+    }
+    while (i < to) {
+      const int t0 = token_of(i), vt0 = t0 + v_in;
+      const int next = i + KV_ATT_WAVES;
+      const int t_next = token_of(next);
+      if (next < to) load_ids(t_next);
       // scores
       f32x4 s[R][BF ? 2 : 1];
 #pragma unroll
@@ -303,6 +360,7 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
           }
           s[r][u] = x;
         }
+      if (next < to) load_keys(t_next);
       // whole block visible to every row of the tile?
       const bool whole = t0 + BLK - 1 <= p0 && (P.window <= 0 || t0 > p1 - 1 - P.window || t0 + BLK <= P.sinks);
 #pragma unroll
@@ -341,8 +399,8 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
             l[r] += x;
           }
       }
-      // a value that is not finite would reach rows that do not see its token
-      // (0 times infinity): such blocks take the rows one at a time
+      // a value that is not finite would reach rows that do not see its token (0 times
+      // infinity): such blocks are multiplied in three parts
       bool odd = false;
       if (!whole) {
         bool mine = false;
@@ -355,75 +413,66 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
           }
         odd = __any(mine);
       }
-      if (!odd) {
+      bf16x8 pf[R];
+      if constexpr (BF)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
+      // O += V^T P^T with tile t of the values, or with `f` of each of its elements
+      auto multiply = [&](int t, auto f, f32x4(&to_add)[R]) {
         if constexpr (BF) {
-          bf16x8 pf[R];
+          uint4 a;  // element t of the lane's eight value rows
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            w[e] = f(__builtin_amdgcn_perm(vr[2 * e + 1][t >> 1], vr[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u));
+          __builtin_memcpy(&a, w, 16);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            to_add[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], to_add[r], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float a = __uint_as_float(f(vr[e][t]));
+#pragma unroll
+            for (int r = 0; r < R; ++r) to_add[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[r][0][e], to_add[r], 0, 0, 0);
+          }
+        }
+      };
+      if (!odd) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          f32x4 x[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) x[r] = acc[r][t];
+          multiply(t, [](uint32_t v) { return v; }, x);
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[r][t] = x[r];
+        }
+      } else {
+        // the finite values as they are; then how much weight lies on values of
+        // +infinity or NaN, and of -infinity or NaN
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          f32x4 x[R], up[R], down[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            x[r] = acc[r][t];
+            up[r] = down[r] = f32x4{0, 0, 0, 0};
+          }
+          multiply(t, [](uint32_t v) { return kv_select<T, 0>(v); }, x);
+          multiply(t, [](uint32_t v) { return kv_select<T, 1>(v); }, up);
+          multiply(t, [](uint32_t v) { return kv_select<T, -1>(v); }, down);
 #pragma unroll
           for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            // element t of the lane's eight value rows
-            uint32_t a[4];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              a[w] = __builtin_amdgcn_perm(vr[2 * w + 1][t >> 1], vr[2 * w][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
-            }
-            const bf16x8 af = __builtin_bit_cast(bf16x8, uint4{a[0], a[1], a[2], a[3]});
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, pf[r], acc[r][t], 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float a = __uint_as_float(vr[e][t]);
-#pragma unroll
-              for (int r = 0; r < R; ++r) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[r][0][e], acc[r][t], 0, 0, 0);
-            }
-        }
-      } else {
-        for (int k = 0; k < 16; ++k) {
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const int at = __shfl(pos[r], k);
-            // the values with zeros at what row k does not see
-            uint32_t keep[TOK];
-#pragma unroll
-            for (int e = 0; e < TOK; ++e) {
-              const int tok = vt0 + e;
-              keep[e] = tok <= at && (P.window <= 0 || tok > at - P.window || tok < P.sinks) ? 0xffffffffu : 0u;
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              f32x4 x{0, 0, 0, 0};
-              if constexpr (BF) {
-                uint32_t a[4];
-                bf16x8 pf;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pf[e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  a[w] = __builtin_amdgcn_perm(vr[2 * w + 1][t >> 1] & keep[2 * w + 1], vr[2 * w][t >> 1] & keep[2 * w],
-                                               t & 1 ? 0x07060302u : 0x05040100u);
-                }
-                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, uint4{a[0], a[1], a[2], a[3]}), pf,
-                                                            x, 0, 0, 0);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float a = __uint_as_float(vr[e][t] & keep[e]);
-                  x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[r][0][e], x, 0, 0, 0);
-                }
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[r][t][e] += c == k ? x[e] : 0.0f;
-            }
-          }
+            for (int e = 0; e < 4; ++e)
+              acc[r][t][e] = x[r][e] + (up[r][e] > 0.0f ? INFINITY : 0.0f) - (down[r][e] > 0.0f ? INFINITY : 0.0f);
         }
       }
+      if (next < to) load_values(t_next);
+      i = next;
     }
   }
 
@@ -492,28 +541,33 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_attention_kernel(KvAttnParams P)
 }
 
 // Joins the partial sums of the split units, of which there are fewer than P.items
-// (each has more blocks than an item takes): one workgroup per unit.
-template <typename T, int DP, int R>
+// (each has more blocks than an item takes).  A workgroup takes JR rows of a unit; 16
+// threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.
+template <typename T, int DP, int R, int JR>
 __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
-  constexpr int ROWS = 16 * R, NT = DP / 16;
+  constexpr int ROWS = 16 * R, NT = DP / 16, PER = ROWS / JR, GROUPS = 16 / JR;
+  __shared__ float sum_o[KV_ATT_NT][NT + 1];
+  __shared__ float sum_m[16], sum_l[16];
+  if (blockIdx.x / PER >= *P.split_units) return;
   KvItem it;
-  if (!kv_find_item<ROWS, KvBlk<T>::N, true>(P, blockIdx.x, &it)) return;
-  if (it.slot < 0 || it.slot + it.splits > P.slots) return;
-  const int tid = threadIdx.x, jr = tid >> 4, jc = tid & 15;
+  if (!kv_find_item<ROWS, KvBlk<T>::N, true>(P, blockIdx.x / PER, &it)) return;
+  const int tid = threadIdx.x, jc = tid & 15, jr = (tid >> 4) % JR, grp = (tid >> 4) / JR;
   const int D = P.p.dim, G = P.group;
   const int row0 = it.tile * ROWS, rows = it.count * G;
-  for (int row = jr; row < ROWS && row0 + row < rows; row += KV_ATT_NT / 16) {
+  const int row = static_cast<int>(blockIdx.x % PER) * JR + jr;
+  const bool real = row0 + row < rows && it.slot >= 0 && it.slot + it.splits <= P.slots;
+  float m = -INFINITY, l = 0.0f, o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = 0.0f;
+  if (real) {
     const float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
     const float* po = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + jc * NT;
-    float top = -INFINITY;
-    for (int s = 0; s < it.splits; ++s) top = fmaxf(top, ml[static_cast<int64_t>(s) * ROWS * 2]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) o[t] = 0.0f;
-    for (int s = 0; s < it.splits; ++s) {
+    for (int s = grp; s < it.splits; s += GROUPS) m = fmaxf(m, ml[static_cast<int64_t>(s) * ROWS * 2]);
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
+    for (int s = grp; s < it.splits; s += GROUPS) {
       const float f = __builtin_amdgcn_exp2f(ml[static_cast<int64_t>(s) * ROWS * 2] - ref);
-      sum += f * ml[static_cast<int64_t>(s) * ROWS * 2 + 1];
+      l += f * ml[static_cast<int64_t>(s) * ROWS * 2 + 1];
       const float* x = po + static_cast<int64_t>(s) * ROWS * DP;
 #pragma unroll
       for (int t = 0; t < NT; t += 4) {
@@ -522,15 +576,37 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
         for (int e = 0; e < 4; ++e) o[t + e] += f * y[e];
       }
     }
-    const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-      if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
-    if (P.lse && jc == 0)
-      P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
   }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) sum_o[tid][t] = o[t];
+  if (jc == 0) {
+    sum_m[tid >> 4] = m;
+    sum_l[tid >> 4] = l;
+  }
+  __syncthreads();
+  if (grp != 0 || !real) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < GROUPS; ++w) top = fmaxf(top, sum_m[w * JR + jr]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < GROUPS; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sum_m[w * JR + jr] - ref);
+    sum += f * sum_l[w * JR + jr];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] += f * sum_o[(w * JR + jr) * 16 + jc][t];
+  }
+  const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
+  if (P.lse && jc == 0)
+    P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
 }
 
 // Most tiles of 16 rows that a workgroup takes: what the registers of its waves hold

@@ -202,7 +202,7 @@ size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
       return m > MAX_TOKENS ? 0 : static_cast<size_t>(compact_ws(m).bytes);
     case SAKI_OP_KV_ATTENTION: {
       const int64_t rows = n <= 16 ? 16 : n <= 32 ? 32 : KV_ATT_ROWS;
-      return static_cast<size_t>(SLOTS * rows * (pow2_dim(m) + 2) * 4);
+      return static_cast<size_t>(16 + SLOTS * rows * (pow2_dim(m) + 2) * 4);
     }
     default:
       return 0;
@@ -432,7 +432,8 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.sinks = sinks;
   P.items = KV_ATT_ITEMS;
   P.slots = static_cast<int>(SLOTS);
-  P.part = static_cast<float*>(ws);
+  P.split_units = static_cast<unsigned*>(ws);
+  P.part = static_cast<float*>(ws) + 4;
   P.part_ml = P.part + SLOTS * rows * dp;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   // without a second workgroup's worth of keys in any sequence nothing is split
