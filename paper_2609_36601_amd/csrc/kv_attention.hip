@@ -6,18 +6,18 @@ namespace saki {
 
 namespace {
 
-template <typename T, int DP, int R>
-hipError_t launch(const KvAttnParams& P, int64_t units, bool join, hipStream_t st) {
-  const unsigned grid = static_cast<unsigned>(units + P.items);
-  hipLaunchKernelGGL((kv_attention_kernel<T, DP, R>), dim3(grid), dim3(KV_ATT_NT), 0, st, P);
+template <typename T, int DP, int ROWS>
+hipError_t launch(void (*kernel)(KvAttnParams), const KvAttnParams& P, int64_t units, bool join, hipStream_t st) {
+  constexpr int64_t ITEMS = 1 << KV_ATT_ITEMS_LOG2<ROWS>;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(units + ITEMS)), dim3(KV_ATT_NT), 0, st, P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !join) return e;
-  const unsigned split_units = static_cast<unsigned>(units < P.items ? units : P.items);
+  const unsigned split_units = static_cast<unsigned>(units < ITEMS ? units : ITEMS);
   // one row a workgroup where that fills the card but little more, else four
-  if (split_units * 16 * R <= 4096)
-    hipLaunchKernelGGL((kv_join_kernel<T, DP, R, 1>), dim3(split_units * 16 * R), dim3(KV_ATT_NT), 0, st, P);
+  if (split_units * ROWS <= 4096)
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 1>), dim3(split_units * ROWS), dim3(KV_ATT_NT), 0, st, P);
   else
-    hipLaunchKernelGGL((kv_join_kernel<T, DP, R, 4>), dim3(split_units * 4 * R), dim3(KV_ATT_NT), 0, st, P);
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 4>), dim3(split_units * ROWS / 4), dim3(KV_ATT_NT), 0, st, P);
   return hipGetLastError();
 }
 
@@ -30,11 +30,13 @@ template <>
 hipError_t launch_kv_attention<PartT, PART_DP>(const KvAttnParams& P, int row_tiles, int64_t units, bool join,
                                                hipStream_t st) {
   constexpr int MOST = kv_row_tiles<PartT>(PART_DP);
+  if constexpr (sizeof(PartT) == 2 && PART_DP <= 128)
+    if (row_tiles == 8) return launch<PartT, PART_DP, KV_PROMPT_ROWS>(kv_prompt_kernel<PART_DP>, P, units, join, st);
   if constexpr (MOST >= 4)
-    if (row_tiles == 4) return launch<PartT, PART_DP, 4>(P, units, join, st);
+    if (row_tiles == 4) return launch<PartT, PART_DP, 64>(kv_attention_kernel<PartT, PART_DP, 4>, P, units, join, st);
   if constexpr (MOST >= 2)
-    if (row_tiles == 2) return launch<PartT, PART_DP, 2>(P, units, join, st);
-  return launch<PartT, PART_DP, 1>(P, units, join, st);
+    if (row_tiles == 2) return launch<PartT, PART_DP, 32>(kv_attention_kernel<PartT, PART_DP, 2>, P, units, join, st);
+  return launch<PartT, PART_DP, 16>(kv_attention_kernel<PartT, PART_DP, 1>, P, units, join, st);
 }
 
 }  // namespace saki

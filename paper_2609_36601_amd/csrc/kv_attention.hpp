@@ -29,10 +29,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KV_ATT_NT = 256;
 constexpr int KV_ATT_WAVES = KV_ATT_NT / KV_WAVE;
-constexpr int KV_ATT_ROWS = 64;    // most rows of a tile
-constexpr int KV_ATT_ITEMS = 1024; // items that a call is split into where it has fewer units
+constexpr int KV_ATT_ROWS = 64;  // most rows of a tile of kv_attention_kernel
+// Items that a call is split into where it has fewer units.
+template <int ROWS>
+constexpr int KV_ATT_ITEMS_LOG2 = ROWS <= KV_ATT_ROWS ? 10 : 9;
 constexpr float KV_LOG2E = 1.44269504088896340736f;
 constexpr float KV_LN2 = 0.693147180559945309417f;
+
+struct KvItem;
 
 struct KvAttnParams {
   KvTable t;
@@ -43,11 +47,11 @@ struct KvAttnParams {
   int n_q_heads, group;
   float scale2;  // scale * log2 e
   int window, sinks;
-  int items;     // target of the split
-  float* part;   // [slots][rows][DP] partial sums, then
+  float* part;     // [slots][rows][DP] partial sums, then
   float* part_ml;  // [slots][rows][2] their maximum and sum
   int slots;
-  unsigned* split_units;  // how many units are split, for kv_join_kernel
+  int* n_split;           // how many units are split, and which: for kv_join_kernel
+  KvItem* split;   // [items]
 };
 
 // Blocks of BLK tokens that the rows of tokens [j0, j1) (positions p0 .. p1 - 1) see:
@@ -108,13 +112,23 @@ struct KvItem {
   int fine;
 };
 
-// Finds item `item` of the call, or (JOIN) split unit `item`; every workgroup derives the
-// split from the lengths by itself, which spares a launch.  Items of a sequence are
-// ordered by tile (last first: with causal rows those are the longest), split, key
-// head, so that the workgroups of one key head, which read the same keys, tend to
-// one XCD.  False: there is no such item.
-template <int ROWS, int BLK, bool JOIN>
-__device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, int64_t item, KvItem* out) {
+// The same item for the whole workgroup, in scalar registers.
+__device__ __forceinline__ KvItem kv_uniform(const KvItem& x) {
+  KvItem r;
+  const int* f = reinterpret_cast<const int*>(&x);
+  int* o = reinterpret_cast<int*>(&r);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(KvItem) / 4); ++i) o[i] = __builtin_amdgcn_readfirstlane(f[i]);
+  return r;
+}
+
+// Finds the workgroup's item; every workgroup derives the split from the lengths by
+// itself, which spares a launch.  Items of a sequence are ordered by tile (last first: with
+// causal rows those are the longest), split, key head, so that the workgroups of one key
+// head, which read the same keys, tend to one XCD.  False: there is no such item.
+template <int ROWS, int BLK>
+__device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out) {
+  constexpr int ITEMS_LOG2 = KV_ATT_ITEMS_LOG2<ROWS>;
   __shared__ long long part[KV_ATT_WAVES];
   __shared__ KvItem found;
   __shared__ int is_found;
@@ -123,70 +137,70 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, int64_t item
   const int per = (P.t.n_seq + KV_ATT_NT - 1) / KV_ATT_NT;
   const int b0 = tid * per, b1 = b0 + per < P.t.n_seq ? b0 + per : P.t.n_seq;
   if (tid == 0) is_found = 0;
-  long long blocks = 0, all = 0;
+  long long blocks = 0;
   KvLoad keep;  // the thread's only sequence where it has one
   for (int b = b0; b < b1; ++b) {
     keep = kv_load_of<ROWS, BLK>(P, b);
     blocks += static_cast<long long>(keep.tiles) * keep.blocks;
   }
-  kv_block_scan<KV_ATT_NT, long long>(blocks, part, &all);
-  // blocks an item takes: what gives the call P.items of them, and at least one
-  // block for each wave twice
-  long long len = (all * Hk + P.items - 1) / P.items;
-  if (len < 2 * KV_ATT_WAVES) len = 2 * KV_ATT_WAVES;
-  auto splits_of = [&](const KvLoad& s) { return static_cast<int>((s.blocks + len - 1) / len); };
-  long long items = 0, slots = 0, split_units = 0;
+  // blocks an item takes: what gives the call its number of items, and at least 8
+  blocks = kv_wave_sum(blocks);
+  if ((tid & (KV_WAVE - 1)) == 0) part[tid / KV_WAVE] = blocks;
+  __syncthreads();
+  long long all = 0;
+#pragma unroll
+  for (int w = 0; w < KV_ATT_WAVES; ++w) all += part[w];
+  all = (all * Hk + (1 << ITEMS_LOG2) - 1) >> ITEMS_LOG2;
+  const unsigned len = all < 8 ? 8u : all < (1 << 30) ? static_cast<unsigned>(all) : 1u << 30;
+  // Sums over the sequences: items; slots of the split units' items, fewer than twice the
+  // items aimed at; split units, fewer than those (each has more blocks than an item).
+  auto sums_of = [&](const KvLoad& s, int* n) {
+    *n = static_cast<int>((static_cast<unsigned>(s.blocks) + len - 1) / len);
+    const long long units = static_cast<long long>(s.tiles) * Hk, items = units * *n;
+    return items + (*n > 1 ? (items << 32) + (units << 48) : 0);
+  };
+  int n = 0;
+  long long mine = 0, total = 0;
   for (int b = b0; b < b1; ++b) {
-    const KvLoad s = per == 1 ? keep : kv_load_of<ROWS, BLK>(P, b);
-    const int n = splits_of(s);
-    if (n > 1) split_units += static_cast<long long>(s.tiles) * Hk;
-    items += static_cast<long long>(s.tiles) * Hk * (JOIN ? n > 1 : n);
-    if (n > 1) slots += static_cast<long long>(s.tiles) * Hk * n;
+    if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
+    mine += sums_of(keep, &n);
   }
-  // (both sums in one scan: at most 2^31 items, as the grid is)
-  long long sums = 0;
-  const long long before = kv_block_scan<KV_ATT_NT, long long>((slots << 32) | items, part, &sums);
-  if (!JOIN && blockIdx.x == 0) {
-    long long n = 0;
-    kv_block_scan<KV_ATT_NT, long long>(split_units, part, &n);
-    if (tid == 0) *P.split_units = n < P.items ? static_cast<unsigned>(n) : static_cast<unsigned>(P.items);
-  }
-  long long at = before & 0xffffffffll, slot = before >> 32;
-  if (item >= at && item < at + items) {
+  long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part, &total);
+  const unsigned item = blockIdx.x;
+  if (item == 0 && tid == 0) *P.n_split = static_cast<int>(total >> 48);
+  if (item >= static_cast<unsigned>(at) && item - static_cast<unsigned>(at) < static_cast<unsigned>(mine)) {
     for (int b = b0; b < b1; ++b) {
-      const KvLoad s = per == 1 ? keep : kv_load_of<ROWS, BLK>(P, b);
-      const int n = splits_of(s);
-      const long long mine = static_cast<long long>(s.tiles) * Hk * (JOIN ? n > 1 : n);
-      if (item < at + mine) {
-        int i = static_cast<int>(item - at);
+      if (per > 1) {
+        keep = kv_load_of<ROWS, BLK>(P, b);
+        mine = sums_of(keep, &n);
+      }
+      unsigned i = item - static_cast<unsigned>(at);
+      if (i < static_cast<unsigned>(mine)) {
         KvItem f;
-        f.head = i % Hk;
-        i /= Hk;
-        f.split = JOIN ? 0 : i % n;
-        const int tile_back = JOIN ? i : i / n;
-        f.tile = s.tiles - 1 - tile_back;
-        f.b = b;
-        f.first = s.first;
-        f.count = s.count;
-        f.start = static_cast<int>(s.start);
-        f.fine = s.fine;
+        const unsigned q = i / static_cast<unsigned>(Hk);
+        f.head = static_cast<int>(i - q * Hk);
+        const int back = static_cast<int>(q / static_cast<unsigned>(n));
+        f.split = static_cast<int>(q) - back * n;
+        f.tile = keep.tiles - 1 - back;
+        f.first = keep.first;
+        f.count = keep.count;
+        f.start = static_cast<int>(keep.start);
+        f.fine = keep.fine;
         f.splits = n;
-        // slots of a unit are consecutive
-        f.slot = static_cast<int>(slot) + (tile_back * Hk + f.head) * n + f.split;
+        f.b = b;
+        // a unit's slots are consecutive
+        f.slot = static_cast<int>((at >> 32) & 0xffff) + (back * Hk + f.head) * n + f.split;
         found = f;
         is_found = 1;
+        const int unit = static_cast<int>((at >> 48) & 0xffff) + back * Hk + f.head;
+        if (n > 1 && f.split == 0 && unit >= 0 && unit < 1 << ITEMS_LOG2) P.split[unit] = f;
         break;
       }
       at += mine;
-      if (n > 1) slot += static_cast<long long>(s.tiles) * Hk * n;
     }
   }
   __syncthreads();
-  // (the same for the whole workgroup: in scalar registers)
-  const int* f = reinterpret_cast<const int*>(&found);
-  int* o = reinterpret_cast<int*>(out);
-#pragma unroll
-  for (int i = 0; i < static_cast<int>(sizeof(KvItem) / 4); ++i) o[i] = __builtin_amdgcn_readfirstlane(f[i]);
+  *out = kv_uniform(found);
   return __builtin_amdgcn_readfirstlane(is_found) != 0;
 }
 
@@ -216,6 +230,46 @@ __device__ __forceinline__ uint32_t kv_select(uint32_t v) {
   return one(v & 0xffffu) | one(v >> 16) << 16;
 }
 
+// Scores of a row (a lane's 4 U of a block; they belong to tokens tok ..) to weights relative to
+// the running maximum m, with l their sum; where the maximum moves, O and l are scaled.
+template <int U, int NT>
+__device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float* m, float* l, float scale2, bool whole,
+                                          int tok, int pos, int window, int sinks) {
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x = s[u][e] * scale2;
+      if (!whole) {
+        const int t = tok + 4 * u + e;
+        const bool seen = t <= pos && (window <= 0 || t > pos - window || t < sinks);
+        x = seen ? x : -INFINITY;
+      }
+      s[u][e] = x;
+      top = fmaxf(top, x);
+    }
+  if (__any(top > *m + 8.0f)) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float to = fmaxf(*m, top);
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(*m - to);
+    *m = to;
+    *l *= f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] *= f;
+  }
+  const float ref = *m == -INFINITY ? 0.0f : *m;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = __builtin_amdgcn_exp2f(s[u][e] - ref);
+      s[u][e] = x;
+      *l += x;
+    }
+}
+
 // One item: ROWS = 16 R rows, the blocks of its split dealt to the four waves.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_attention_kernel(KvAttnParams P) {
@@ -232,7 +286,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   __shared__ float join_m[KV_ATT_WAVES][ROWS], join_l[KV_ATT_WAVES][ROWS];
 
   KvItem it;
-  if (!kv_find_item<ROWS, BLK, false>(P, blockIdx.x, &it)) return;
+  if (!kv_find_item<ROWS, BLK>(P, &it)) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;
@@ -364,41 +418,8 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       // whole block visible to every row of the tile?
       const bool whole = t0 + BLK - 1 <= p0 && (P.window <= 0 || t0 > p1 - 1 - P.window || t0 + BLK <= P.sinks);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < (BF ? 2 : 1); ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = s[r][u][e] * P.scale2;
-            if (!whole) {
-              const int tok = vt0 + 4 * u + e;
-              const bool seen = tok <= pos[r] && (P.window <= 0 || tok > pos[r] - P.window || tok < P.sinks);
-              x = seen ? x : -INFINITY;
-            }
-            s[r][u][e] = x;
-            top = fmaxf(top, x);
-          }
-        if (__any(top > m[r] + 8.0f)) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float to_m = fmaxf(m[r], top);
-          const float f = to_m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[r] - to_m);
-          m[r] = to_m;
-          l[r] *= f;
-#pragma unroll
-          for (int t = 0; t < NT; ++t) acc[r][t] *= f;
-        }
-        const float ref = m[r] == -INFINITY ? 0.0f : m[r];
-#pragma unroll
-        for (int u = 0; u < (BF ? 2 : 1); ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = __builtin_amdgcn_exp2f(s[r][u][e] - ref);
-            s[r][u][e] = x;
-            l[r] += x;
-          }
-      }
+      for (int r = 0; r < R; ++r)
+        kv_soften<BF ? 2 : 1, NT>(s[r], acc[r], &m[r], &l[r], P.scale2, whole, vt0, pos[r], P.window, P.sinks);
       // a value that is not finite would reach rows that do not see its token (0 times
       // infinity): such blocks are multiplied in three parts
       bool odd = false;
@@ -540,17 +561,16 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   }
 }
 
-// Joins the partial sums of the split units, of which there are fewer than P.items
-// (each has more blocks than an item takes).  A workgroup takes JR rows of a unit; 16
+// Joins the partial sums of the split units, of which there are no more than
+// items aimed at (each has more blocks than an item takes).  A workgroup takes JR rows of a unit; 16
 // threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.
-template <typename T, int DP, int R, int JR>
+template <typename T, int DP, int ROWS, int JR>
 __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
-  constexpr int ROWS = 16 * R, NT = DP / 16, PER = ROWS / JR, GROUPS = 16 / JR;
+  constexpr int NT = DP / 16, PER = ROWS / JR, GROUPS = 16 / JR;
   __shared__ float sum_o[KV_ATT_NT][NT + 1];
   __shared__ float sum_m[16], sum_l[16];
-  if (blockIdx.x / PER >= *P.split_units) return;
-  KvItem it;
-  if (!kv_find_item<ROWS, KvBlk<T>::N, true>(P, blockIdx.x / PER, &it)) return;
+  if (static_cast<int>(blockIdx.x / PER) >= *P.n_split) return;
+  const KvItem it = kv_uniform(P.split[blockIdx.x / PER]);
   const int tid = threadIdx.x, jc = tid & 15, jr = (tid >> 4) % JR, grp = (tid >> 4) / JR;
   const int D = P.p.dim, G = P.group;
   const int row0 = it.tile * ROWS, rows = it.count * G;
@@ -609,6 +629,279 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
     P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
 }
 
+// Prompts: many rows a sequence.  Each of the four waves takes 32 rows of the item's 128, and
+// all of them the same keys and values, 64 tokens at a time, through LDS: the values
+// transposed on the way in (8 tokens by 4 elements a thread), so that the second product's
+// operand is 16 consecutive bytes there.  The next tokens are loaded while these are
+// multiplied; two LDS buffers, one barrier for each 64 tokens.
+template <int DP>
+struct KvPromptShared {
+  // a row of keys is an LDS row of DP elements and 16 bytes more, which spreads the rows that a
+  // wave reads at once over the banks; its 32 tokens are kept in the order of the product's rows
+  uint16_t k[2][64][DP + 8];
+  uint16_t v[2][DP][64 + 8];
+  int odd[2];
+};
+
+constexpr int KV_PROMPT_ROWS = 128;
+
+template <int DP>
+__global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P) {
+  constexpr int R = 2, BLK = 64, ROWS = KV_PROMPT_ROWS;
+  constexpr int NT = DP / 16, QC = DP / 32;
+  constexpr int KP = 64 * DP / 8 / KV_ATT_NT;  // 16-byte pieces of keys a thread stages
+  constexpr int VP = DP / 4 * 8 / KV_ATT_NT;   // 8 x 4 blocks of values a thread stages
+  static_assert(VP >= 1 || DP == 64, "");
+  constexpr int VB = VP > 0 ? VP : 1;
+  __shared__ KvPromptShared<DP> sh;
+  KvItem it;
+  if (!kv_find_item<ROWS, BLK>(P, &it)) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
+  const int c = lane & 15, g = lane >> 4;
+  const int D = P.p.dim, G = P.group;
+  const int row0 = it.tile * ROWS, rows = it.count * G;
+  const int n_rows = rows - row0 < ROWS ? rows - row0 : ROWS;
+  const int j0 = row0 / G, j1 = (row0 + n_rows - 1) / G + 1;
+  const int p0 = it.start + j0, p1 = it.start + j1;
+  // this wave's rows and the positions of their tokens
+  const int w0 = wave * 32 < n_rows ? wave * 32 : n_rows - 1, w1 = w0 + 31 < n_rows ? w0 + 31 : n_rows - 1;
+  const int wp0 = it.start + (row0 + w0) / G, wp1 = it.start + (row0 + w1) / G;
+  const bool idle = wave * 32 >= n_rows;
+  bool bad = !it.fine;
+
+  int pos[R];
+  uint4 qf[R][QC];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = wave * 32 + 16 * r + c;
+    const int rr = row0 + (row < n_rows ? row : n_rows - 1);
+    const int j = rr / G, head = it.head * G + rr - j * G;
+    pos[r] = it.start + j;
+    const char* src = P.q.data + (it.first + j) * P.q.token + head * P.q.head;
+#pragma unroll
+    for (int e = 0; e < QC; ++e)
+      qf[r][e] = e * 32 + g * 8 < D ? *reinterpret_cast<const uint4*>(src + e * 64 + g * 16) : uint4{0, 0, 0, 0};
+  }
+  f32x4 acc[R][NT];
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0, 0, 0, 0};
+  }
+
+  if (it.fine) {
+    const KvSpan span = kv_span<BLK>(p0, p1, P.window, P.sinks);
+    const int from = static_cast<int>(static_cast<int64_t>(span.blocks) * it.split / it.splits);
+    const int to = static_cast<int>(static_cast<int64_t>(span.blocks) * (it.split + 1) / it.splits);
+    const int32_t* row_pages = P.t.pages + static_cast<int64_t>(it.b) * P.t.max_pages;
+    const int mask = (1 << P.t.shift) - 1, last = p1 - 1;
+    const char* kb = P.p.k + it.head * P.p.head_stride;
+    const char* vb = P.p.v + it.head * P.p.head_stride;
+    const int token_stride = static_cast<int>(P.p.token_stride);
+    auto token_of = [&](int i) { return i < span.sinks ? i * BLK : span.lo + (i - span.sinks) * BLK; };
+    auto run_of = [&](int tok) { return tok <= last ? tok & ~7 : last & ~7; };
+    auto page_at = [&](int id) {
+      const bool in = id >= 0 && id < P.t.n_pages;
+      bad |= !in;
+      return static_cast<int64_t>(in ? id : 0) * P.p.page_stride;
+    };
+    // Staging.  Keys: thread takes piece tid % (DP / 8) of tokens tid / (DP / 8) + i * step.  Values: the
+    // 8 tokens of run tid % 8, elements 4 * (tid / 8) + 128 i on: eight lanes write 128 consecutive bytes
+    constexpr int PIECES = DP / 8, STEP = KV_ATT_NT / PIECES;
+    const int kc = tid % PIECES, kt = tid / PIECES;
+    const int vrun = tid & 7, vd = 4 * (tid >> 3);
+    const bool v_takes = VP > 0 || tid < DP / 4 * 8;
+    int k_id[KP], v_id = 0;
+    uint4 ks[KP];
+    uint2 vs[VB][8];
+    auto load_ids = [&](int t0) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) k_id[i] = row_pages[run_of(t0 + kt + i * STEP) >> P.t.shift];
+      v_id = row_pages[run_of(t0 + vrun * 8) >> P.t.shift];
+    };
+    auto load_tokens = [&](int t0) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        int tok = t0 + kt + i * STEP;
+        tok = tok < last ? tok : last;
+        const char* at = kb + page_at(k_id[i]) + static_cast<int64_t>(tok & mask) * token_stride + kc * 16;
+        ks[i] = kc * 8 < D ? *reinterpret_cast<const uint4*>(at) : uint4{0, 0, 0, 0};
+      }
+      const int run = run_of(t0 + vrun * 8);
+      const char* src = vb + page_at(v_id);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int tok = run + e < last ? run + e : last;
+        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
+#pragma unroll
+        for (int i = 0; i < VB; ++i) {
+          const int d = vd + 128 * i;
+          vs[i][e] = v_takes && d < D ? *reinterpret_cast<const uint2*>(at + d * 2) : uint2{0, 0};
+        }
+      }
+    };
+    auto whole_for = [&](int t0, int n, int first, int end) {
+      return t0 + n - 1 <= first && (P.window <= 0 || t0 > end - P.window || t0 + n <= P.sinks);
+    };
+    auto stage = [&](int buf, int t0) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        // token 8 g + 4 s + e of 32 is row 16 s + 4 g + e of the product
+        const int tok = kt + i * STEP;
+        const int row = (tok & 32) | (tok & 4) << 2 | (tok & 24) >> 1 | (tok & 3);
+        *reinterpret_cast<uint4*>(&sh.k[buf][row][kc * 8]) = ks[i];
+      }
+      if (v_takes) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < VB; ++i)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = __builtin_amdgcn_perm(d < 2 ? vs[i][2 * e + 1].x : vs[i][2 * e + 1].y,
+                                           d < 2 ? vs[i][2 * e].x : vs[i][2 * e].y, d & 1 ? 0x07060302u : 0x05040100u);
+            *reinterpret_cast<uint4*>(&sh.v[buf][vd + 128 * i + d][vrun * 8]) = uint4{w[0], w[1], w[2], w[3]};
+          }
+        if (!whole_for(t0, BLK, p0, p1 - 1)) {
+#pragma unroll
+          for (int i = 0; i < VB; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t x = vs[i][e].x, y = vs[i][e].y;
+              odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u ||
+                     (y & 0x7f800000u) == 0x7f800000u;
+            }
+        }
+        if (odd) sh.odd[buf] = 1;
+      }
+    };
+    if (tid < 2) sh.odd[tid] = 0;
+    int i = from, buf = 0;
+    if (i < to) {
+      load_ids(token_of(i));
+      load_tokens(token_of(i));
+    }
+    __syncthreads();  // the flags are clear
+    if (i < to) stage(0, token_of(i));
+    if (i + 1 < to) load_ids(token_of(i + 1));
+    __syncthreads();
+    for (; i < to; ++i, buf ^= 1) {
+      const int t0 = token_of(i);
+      if (i + 1 < to) load_tokens(token_of(i + 1));
+      if (i + 2 < to) load_ids(token_of(i + 2));
+      const bool tile_odd = sh.odd[buf] != 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int tb = t0 + 32 * h;
+        if (idle || tb > wp1) continue;
+        f32x4 s[R][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          uint4 kf[QC];
+#pragma unroll
+          for (int e = 0; e < QC; ++e) kf[e] = *reinterpret_cast<const uint4*>(&sh.k[buf][32 * h + 16 * u + c][e * 32 + g * 8]);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            s[r][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < QC; ++e)
+              s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[e]),
+                                                                __builtin_bit_cast(bf16x8, qf[r][e]), s[r][u], 0, 0, 0);
+          }
+        }
+        const bool whole = whole_for(tb, 32, wp0, wp1);
+        bf16x8 pf[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) kv_soften<2, NT>(s[r], acc[r], &m[r], &l[r], P.scale2, whole, tb + g * 8, pos[r], P.window, P.sinks);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
+        if (whole || !tile_odd) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const uint4 a = *reinterpret_cast<const uint4*>(&sh.v[buf][16 * t + c][32 * h + g * 8]);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], acc[r][t], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const uint4 a = *reinterpret_cast<const uint4*>(&sh.v[buf][16 * t + c][32 * h + g * 8]);
+            uint4 part[3];
+            part[0] = uint4{kv_select<uint16_t, 0>(a.x), kv_select<uint16_t, 0>(a.y), kv_select<uint16_t, 0>(a.z),
+                            kv_select<uint16_t, 0>(a.w)};
+            part[1] = uint4{kv_select<uint16_t, 1>(a.x), kv_select<uint16_t, 1>(a.y), kv_select<uint16_t, 1>(a.z),
+                            kv_select<uint16_t, 1>(a.w)};
+            part[2] = uint4{kv_select<uint16_t, -1>(a.x), kv_select<uint16_t, -1>(a.y), kv_select<uint16_t, -1>(a.z),
+                            kv_select<uint16_t, -1>(a.w)};
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const f32x4 zero{0, 0, 0, 0};
+              const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[0]), pf[r], acc[r][t], 0, 0, 0);
+              const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[1]), pf[r], zero, 0, 0, 0);
+              const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[2]), pf[r], zero, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[r][t][e] = x[e] + (up[e] > 0.0f ? INFINITY : 0.0f) - (down[e] > 0.0f ? INFINITY : 0.0f);
+            }
+          }
+        }
+      }
+      // the other buffer was read before the last barrier, and its flag too
+      if (i + 1 < to) {
+        if (tid == 0) sh.odd[buf ^ 1] = 0;
+        if (!whole_for(token_of(i + 1), BLK, p0, p1 - 1)) __syncthreads();
+        stage(buf ^ 1, token_of(i + 1));
+      }
+      __syncthreads();
+    }
+  }
+
+  const bool any_bad = __syncthreads_or(bad);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    if (any_bad) l[r] = __builtin_nanf("");
+    const int row = wave * 32 + 16 * r + c;
+    if (row >= n_rows) continue;
+    if (it.splits > 1) {
+      if (it.slot >= 0 && it.slot < P.slots) {
+        float* dst = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + g * 4;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(dst + 16 * t) = acc[r][t];
+        if (g == 0) {
+          float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
+          ml[0] = m[r];
+          ml[1] = l[r];
+        }
+      }
+    } else {
+      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+      uint16_t* dst = reinterpret_cast<uint16_t*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head) + g * 4;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (16 * t + g * 4 < D) {
+          uint16_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = kv_to_bf16(acc[r][t][e] * inv);
+          __builtin_memcpy(__builtin_assume_aligned(dst + 16 * t, 8), y, 8);
+        }
+      if (P.lse && g == 0)
+        P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] =
+            ((m[r] == -INFINITY ? 0.0f : m[r]) + log2f(l[r])) * KV_LN2;
+    }
+  }
+}
+
 // Most tiles of 16 rows that a workgroup takes: what the registers of its waves hold
 // (O and Q of each row tile beside a block's keys and values).
 template <typename T>
@@ -616,8 +909,8 @@ constexpr int kv_row_tiles(int dp) {
   return sizeof(T) == 2 ? (dp <= 64 ? 4 : dp <= 128 ? 2 : 1) : (dp <= 128 ? 2 : 1);
 }
 
-// Launches for heads of up to DP elements, `row_tiles` of 16 rows a workgroup; `units`
-// bounds the units of the call.
+// Launches for heads of up to DP elements, `row_tiles` of 16 rows a workgroup (8: the
+// kernel for prompts); `units` bounds the units of the call.
 template <typename T, int DP>
 hipError_t launch_kv_attention(const KvAttnParams& P, int row_tiles, int64_t units, bool join, hipStream_t st);
 

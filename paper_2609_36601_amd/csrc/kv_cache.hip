@@ -137,9 +137,22 @@ KvStrides device_heads(const saki_kv_heads* x, const saki_kv_pool* p) {
 
 int pow2_dim(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Slots for partial sums: items of units that are split, at most twice the items
-// aimed at (a unit of more than one item has at least half of each of them full).
-constexpr int64_t SLOTS = 2 * KV_ATT_ITEMS;
+// Workspace of an attention call of `rows` query rows: the split units, and slots for
+// the partial sums of their items, at most twice the items aimed at (a unit of more
+// than one item fills at least half of each).  Tiles have no more rows than the call.
+struct AttentionWs {
+  int64_t split, part, slots, part_ml, bytes;
+};
+AttentionWs attention_ws(int dp, int tile_rows) {
+  AttentionWs w{};
+  const int64_t items = int64_t{1} << (tile_rows > KV_ATT_ROWS ? KV_ATT_ITEMS_LOG2<KV_PROMPT_ROWS> : KV_ATT_ITEMS_LOG2<KV_ATT_ROWS>);
+  w.split = 16;  // after their number
+  w.part = w.split + up16(items * static_cast<int64_t>(sizeof(KvItem)));
+  w.slots = 2 * items;
+  w.part_ml = w.part + w.slots * tile_rows * dp * 4;
+  w.bytes = w.part_ml + w.slots * tile_rows * 8;
+  return w;
+}
 
 struct ReserveWs {
   int64_t want, moves, n_moves, writers, last, list, bytes;
@@ -201,8 +214,8 @@ size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
     case SAKI_OP_KV_COMPACT:
       return m > MAX_TOKENS ? 0 : static_cast<size_t>(compact_ws(m).bytes);
     case SAKI_OP_KV_ATTENTION: {
-      const int64_t rows = n <= 16 ? 16 : n <= 32 ? 32 : KV_ATT_ROWS;
-      return static_cast<size_t>(16 + SLOTS * rows * (pow2_dim(m) + 2) * 4);
+      // (prompts' tiles have twice the rows and half the slots)
+      return static_cast<size_t>(attention_ws(pow2_dim(m), n <= 16 ? 16 : n <= 32 ? 32 : KV_ATT_ROWS).bytes);
     }
     default:
       return 0;
@@ -412,12 +425,13 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   // rows of a tile: those of a sequence of mean length
   const int64_t mean = n * group / table->n_seq;
   const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
-  const int tiles = std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
-  const int64_t rows = 16 * tiles;
+  const int tiles = bf && dp <= 128 && mean > KV_ATT_ROWS ? KV_PROMPT_ROWS / 16
+                                                          : std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
+  const int rows = 16 * tiles;
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;
-  if (units > INT32_MAX - KV_ATT_ITEMS) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  if (units > INT32_MAX - 4096) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
   KvAttnParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);
@@ -430,15 +444,16 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.scale2 = scale * KV_LOG2E;
   P.window = window;
   P.sinks = sinks;
-  P.items = KV_ATT_ITEMS;
-  P.slots = static_cast<int>(SLOTS);
-  P.split_units = static_cast<unsigned*>(ws);
-  P.part = static_cast<float*>(ws) + 4;
-  P.part_ml = P.part + SLOTS * rows * dp;
+  const AttentionWs at = attention_ws(dp, rows);
+  char* w = static_cast<char*>(ws);
+  P.n_split = reinterpret_cast<int*>(w);
+  P.split = reinterpret_cast<KvItem*>(w + at.split);
+  P.part = reinterpret_cast<float*>(w + at.part);
+  P.part_ml = reinterpret_cast<float*>(w + at.part_ml);
+  P.slots = static_cast<int>(at.slots);
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  // without a second workgroup's worth of keys in any sequence nothing is split
-  const int64_t most_blocks = table->max_pages * table->page_size / (bf ? 32 : 16) + 1;
-  const bool join = most_blocks > 2 * KV_ATT_WAVES;
+  // without more than 8 blocks of keys in any sequence nothing is split
+  const bool join = table->max_pages * table->page_size > 8 * (bf ? 32 : 16);
   hipError_t e;
   if (bf)
     e = dp == 64    ? launch_kv_attention<uint16_t, 64>(P, tiles, units, join, hs)
