@@ -282,7 +282,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   constexpr int VW = NT * sizeof(T) / 4;   // 32-bit words of a lane's share of a value row
   using VPiece = typename std::conditional<(VW >= 4), uint4, uint2>::type;
   constexpr int VC = VW * 4 / sizeof(VPiece), VE = sizeof(VPiece) / sizeof(T);  // its loads, elements of a load
-  __shared__ float join_o[KV_ATT_WAVES][16][DP + 4];
+  __shared__ __align__(16) float join_o[KV_ATT_WAVES][16][DP + 4];
   __shared__ float join_m[KV_ATT_WAVES][ROWS], join_l[KV_ATT_WAVES][ROWS];
 
   KvItem it;
@@ -638,8 +638,8 @@ template <int DP>
 struct KvPromptShared {
   // a row of keys is an LDS row of DP elements and 16 bytes more, which spreads the rows that a
   // wave reads at once over the banks; its 32 tokens are kept in the order of the product's rows
-  uint16_t k[2][64][DP + 8];
-  uint16_t v[2][DP][64 + 8];
+  alignas(16) uint16_t k[2][64][DP + 8];
+  alignas(16) uint16_t v[2][DP][64 + 8];
   int odd[2];
 };
 
