@@ -45,7 +45,8 @@ struct KvAttnParams {
   KvStrides q, out;
   float* lse;
   int n_q_heads, group;
-  float scale2;  // scale * log2 e
+  float scale2;  // |scale| log2 e
+  uint32_t flip;  // sign bits of a pair of elements (one, in f32) where the scale is negative
   int window, sinks;
   float* part;     // [slots][rows][DP] partial sums, then
   float* part_ml;  // [slots][rows][2] their maximum and sum
@@ -115,11 +116,17 @@ struct KvItem {
 // The same item for the whole workgroup, in scalar registers.
 __device__ __forceinline__ KvItem kv_uniform(const KvItem& x) {
   KvItem r;
-  const int* f = reinterpret_cast<const int*>(&x);
-  int* o = reinterpret_cast<int*>(&r);
-#pragma unroll
-  for (int i = 0; i < static_cast<int>(sizeof(KvItem) / 4); ++i) o[i] = __builtin_amdgcn_readfirstlane(f[i]);
+#define KV_FIELD(f) r.f = __builtin_amdgcn_readfirstlane(x.f)
+  KV_FIELD(b), KV_FIELD(first), KV_FIELD(count), KV_FIELD(start), KV_FIELD(tile), KV_FIELD(head), KV_FIELD(split),
+      KV_FIELD(splits), KV_FIELD(slot), KV_FIELD(fine);
+#undef KV_FIELD
   return r;
+}
+
+// The blocks of a split: whole blocks, spread evenly.
+__device__ __forceinline__ int kv_split_at(int blocks, int splits, int split) {
+  const int q = blocks / splits, r = blocks - q * splits;
+  return q * split + (split < r ? split : r);
 }
 
 // Finds the workgroup's item; every workgroup derives the split from the lengths by
@@ -230,29 +237,36 @@ __device__ __forceinline__ uint32_t kv_select(uint32_t v) {
   return one(v & 0xffffu) | one(v >> 16) << 16;
 }
 
-// Scores of a row (a lane's 4 U of a block; they belong to tokens tok ..) to weights relative to
-// the running maximum m, with l their sum; where the maximum moves, O and l are scaled.
-template <int U, int NT>
-__device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float* m, float* l, float scale2, bool whole,
-                                          int tok, int pos, int window, int sinks) {
+__device__ __forceinline__ uint4 kv_flip(uint4 x, uint32_t f) { return uint4{x.x ^ f, x.y ^ f, x.z ^ f, x.w ^ f}; }
+
+// Scores of a row (a lane's 4 U of a block; those of u belong to tokens tok + 32 (u / 2) +
+// 4 (u % 2) ..) to weights relative to the running maximum m, with l their sum; where the
+// maximum moves, O and l are scaled.  scale2 >= 0.  MASKED: some row does not see some token.
+template <bool MASKED, int U, int NT>
+__device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float* m, float* l, float scale2, int tok,
+                                          int pos, int window, int sinks) {
   float top = -INFINITY;
+  uint32_t seen = 0xffffffffu;
+  if constexpr (MASKED) {
+    seen = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int t = tok + 32 * (u >> 1) + 4 * (u & 1) + e;
+        const bool yes = t <= pos && (window <= 0 || t > pos - window || t < sinks);
+        seen |= static_cast<uint32_t>(yes) << (4 * u + e);
+        s[u][e] = yes ? s[u][e] : -INFINITY;
+      }
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float x = s[u][e] * scale2;
-      if (!whole) {
-        const int t = tok + 4 * u + e;
-        const bool seen = t <= pos && (window <= 0 || t > pos - window || t < sinks);
-        x = seen ? x : -INFINITY;
-      }
-      s[u][e] = x;
-      top = fmaxf(top, x);
-    }
-  if (__any(top > *m + 8.0f)) {
+    for (int e = 0; e < 4; ++e) top = fmaxf(top, s[u][e]);
+  if (__any(top * scale2 > *m + 8.0f)) {
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float to = fmaxf(*m, top);
+    const float to = fmaxf(*m, top * scale2);
     const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(*m - to);
     *m = to;
     *l *= f;
@@ -264,7 +278,9 @@ __device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float x = __builtin_amdgcn_exp2f(s[u][e] - ref);
+      float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale2, -ref));
+      // (a hidden score is -infinity, which a scale of 0 would make a NaN)
+      if constexpr (MASKED) x = (seen >> (4 * u + e)) & 1 ? x : 0.0f;
       s[u][e] = x;
       *l += x;
     }
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
 #pragma unroll
     for (int i = 0; i < QC; ++i) {
       const int d = i * (BF ? 32 : 16) + g * (BF ? 8 : 4);
-      qf[r][i] = d < D ? *reinterpret_cast<const uint4*>(src + d * sizeof(T)) : uint4{0, 0, 0, 0};
+      qf[r][i] = kv_flip(d < D ? *reinterpret_cast<const uint4*>(src + d * sizeof(T)) : uint4{0, 0, 0, 0}, P.flip);
     }
   }
 
@@ -326,8 +342,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
 
   if (it.fine) {
     const KvSpan span = kv_span<BLK>(p0, p1, P.window, P.sinks);
-    const int from = static_cast<int>(static_cast<int64_t>(span.blocks) * it.split / it.splits);
-    const int to = static_cast<int>(static_cast<int64_t>(span.blocks) * (it.split + 1) / it.splits);
+    const int from = kv_split_at(span.blocks, it.splits, it.split), to = kv_split_at(span.blocks, it.splits, it.split + 1);
     const int32_t* row_pages = P.t.pages + static_cast<int64_t>(it.b) * P.t.max_pages;
     const int mask = (1 << P.t.shift) - 1;
     const char* kb = P.p.k + it.head * P.p.head_stride;
@@ -360,15 +375,20 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
         int tok = BF ? run + (c & 3) + 4 * s : run + (c & 7);
         tok = tok < last ? tok : last;
         const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
+        if (D == DP) {
 #pragma unroll
-        for (int e = 0; e < QC; ++e)
-          kf[s][e] = e * 64 + g * 16 < D * static_cast<int>(sizeof(T)) ? *reinterpret_cast<const uint4*>(at + e * 64)
-                                                                       : uint4{0, 0, 0, 0};
+          for (int e = 0; e < QC; ++e) kf[s][e] = *reinterpret_cast<const uint4*>(at + e * 64);
+        } else {
+#pragma unroll
+          for (int e = 0; e < QC; ++e)
+            kf[s][e] = e * 64 + g * 16 < D * static_cast<int>(sizeof(T)) ? *reinterpret_cast<const uint4*>(at + e * 64)
+                                                                         : uint4{0, 0, 0, 0};
+        }
       }
     };
     auto load_values = [&](int t0) {
       const int run = run_of(t0 + v_in);
-      const char* src = vb + page_at(v_id) + c * NT * static_cast<int>(sizeof(T));
+      const char* src = vb + page_at(v_id);
 #pragma unroll
       for (int e = 0; e < TOK; ++e) {
         int tok = run + (BF ? 0 : v_in & 7) + e;
@@ -376,7 +396,9 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
         const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
 #pragma unroll
         for (int w = 0; w < VC; ++w) {
-          const VPiece x = c * NT + w * VE < D ? reinterpret_cast<const VPiece*>(at)[w] : VPiece{};
+          // (elements from D on make rows of O that are not kept: any values will do)
+          const int d = c * NT + w * VE < D ? c * NT + w * VE : 0;
+          const VPiece x = *reinterpret_cast<const VPiece*>(at + d * sizeof(T));
           __builtin_memcpy(&vr[e][w * sizeof(VPiece) / 4], &x, sizeof(x));
         }
       }
@@ -419,7 +441,10 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       const bool whole = t0 + BLK - 1 <= p0 && (P.window <= 0 || t0 > p1 - 1 - P.window || t0 + BLK <= P.sinks);
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        kv_soften<BF ? 2 : 1, NT>(s[r], acc[r], &m[r], &l[r], P.scale2, whole, vt0, pos[r], P.window, P.sinks);
+        if (whole)
+          kv_soften<false>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
+        else
+          kv_soften<true>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
       // a value that is not finite would reach rows that do not see its token (0 times
       // infinity): such blocks are multiplied in three parts
       bool odd = false;
@@ -630,18 +655,37 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
 }
 
 // Prompts: many rows a sequence.  Each of the four waves takes 32 rows of the item's 128, and
-// all of them the same keys and values, 64 tokens at a time, through LDS: the values
-// transposed on the way in (8 tokens by 4 elements a thread), so that the second product's
-// operand is 16 consecutive bytes there.  The next tokens are loaded while these are
-// multiplied; two LDS buffers, one barrier for each 64 tokens.
+// all of them the same keys and values, 64 tokens at a time, through LDS, into which the
+// memory pipeline writes them without a detour through registers; the next 64 tokens are under
+// way while these are multiplied (two buffers, one barrier).  A token's row lies there as
+// in memory, but its 16-byte pieces are permuted: piece p of a row is at p ^ kv_swizzle(row), so
+// that the 16 rows which a read touches lie in 16 different banks.  The values are transposed
+// by the read (ds_read_b64_tr_b16: 16 lanes read 4 tokens of 16 elements, and each gets
+// one element's 4 tokens).
 template <int DP>
 struct KvPromptShared {
-  // a row of keys is an LDS row of DP elements and 16 bytes more, which spreads the rows that a
-  // wave reads at once over the banks; its 32 tokens are kept in the order of the product's rows
-  alignas(16) uint16_t k[2][64][DP + 8];
-  alignas(16) uint16_t v[2][DP][64 + 8];
-  int odd[2];
+  alignas(1024) uint16_t k[2][64 * DP];
+  alignas(1024) uint16_t v[2][64 * DP];
 };
+
+// Rows that differ here are read together: 8 a + 4 u + b for a, b in 0 .. 3 (keys), and
+// 8 a + b (values).
+template <int DP>
+__device__ __forceinline__ int kv_swizzle(int row) {
+  const int f = (row & 3) | (row >> 1 & 12);
+  return DP == 128 ? f : f >> 1;  // (two rows of 64 elements fill the banks)
+}
+
+// 16 bytes a lane from memory to LDS at `lds` + 16 lane.  Nothing waits for them but
+// kv_lds_wait (the compiler, which is not told, would have every LDS read wait); they
+// write no register.
+__device__ __forceinline__ void kv_to_lds(uint32_t lds, const char* from) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void kv_lds_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int KV_PROMPT_ROWS = 128;
 
@@ -649,10 +693,6 @@ template <int DP>
 __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P) {
   constexpr int R = 2, BLK = 64, ROWS = KV_PROMPT_ROWS;
   constexpr int NT = DP / 16, QC = DP / 32;
-  constexpr int KP = 64 * DP / 8 / KV_ATT_NT;  // 16-byte pieces of keys a thread stages
-  constexpr int VP = DP / 4 * 8 / KV_ATT_NT;   // 8 x 4 blocks of values a thread stages
-  static_assert(VP >= 1 || DP == 64, "");
-  constexpr int VB = VP > 0 ? VP : 1;
   __shared__ KvPromptShared<DP> sh;
   KvItem it;
   if (!kv_find_item<ROWS, BLK>(P, &it)) return;
@@ -680,7 +720,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     const char* src = P.q.data + (it.first + j) * P.q.token + head * P.q.head;
 #pragma unroll
     for (int e = 0; e < QC; ++e)
-      qf[r][e] = e * 32 + g * 8 < D ? *reinterpret_cast<const uint4*>(src + e * 64 + g * 16) : uint4{0, 0, 0, 0};
+      qf[r][e] = kv_flip(e * 32 + g * 8 < D ? *reinterpret_cast<const uint4*>(src + e * 64 + g * 16) : uint4{0, 0, 0, 0}, P.flip);
   }
   f32x4 acc[R][NT];
   float m[R], l[R];
@@ -694,172 +734,165 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 
   if (it.fine) {
     const KvSpan span = kv_span<BLK>(p0, p1, P.window, P.sinks);
-    const int from = static_cast<int>(static_cast<int64_t>(span.blocks) * it.split / it.splits);
-    const int to = static_cast<int>(static_cast<int64_t>(span.blocks) * (it.split + 1) / it.splits);
+    const int from = kv_split_at(span.blocks, it.splits, it.split), to = kv_split_at(span.blocks, it.splits, it.split + 1);
     const int32_t* row_pages = P.t.pages + static_cast<int64_t>(it.b) * P.t.max_pages;
     const int mask = (1 << P.t.shift) - 1, last = p1 - 1;
     const char* kb = P.p.k + it.head * P.p.head_stride;
     const char* vb = P.p.v + it.head * P.p.head_stride;
     const int token_stride = static_cast<int>(P.p.token_stride);
     auto token_of = [&](int i) { return i < span.sinks ? i * BLK : span.lo + (i - span.sinks) * BLK; };
-    auto run_of = [&](int tok) { return tok <= last ? tok & ~7 : last & ~7; };
     auto page_at = [&](int id) {
       const bool in = id >= 0 && id < P.t.n_pages;
       bad |= !in;
       return static_cast<int64_t>(in ? id : 0) * P.p.page_stride;
     };
-    // Staging.  Keys: thread takes piece tid % (DP / 8) of tokens tid / (DP / 8) + i * step.  Values: the
-    // 8 tokens of run tid % 8, elements 4 * (tid / 8) + 128 i on: eight lanes write 128 consecutive bytes
-    constexpr int PIECES = DP / 8, STEP = KV_ATT_NT / PIECES;
-    const int kc = tid % PIECES, kt = tid / PIECES;
-    const int vrun = tid & 7, vd = 4 * (tid >> 3);
-    const bool v_takes = VP > 0 || tid < DP / 4 * 8;
-    int k_id[KP], v_id = 0;
-    uint4 ks[KP];
-    uint2 vs[VB][8];
+    // A wave's share of 64 tokens: J times 64 pieces of keys and of values, whole rows
+    constexpr int PIECES = DP / 8, J = DP / 32, RPI = 64 / PIECES;
+    const uint32_t lds_k = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+                       (__attribute__((address_space(3))) uint16_t*)&sh.k[0][0])),
+                   lds_v = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+                       (__attribute__((address_space(3))) uint16_t*)&sh.v[0][0]));
+    int row_of[J], id_of[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) row_of[j] = (wave * J + j) * RPI + lane / PIECES;
     auto load_ids = [&](int t0) {
 #pragma unroll
-      for (int i = 0; i < KP; ++i) k_id[i] = row_pages[run_of(t0 + kt + i * STEP) >> P.t.shift];
-      v_id = row_pages[run_of(t0 + vrun * 8) >> P.t.shift];
-    };
-    auto load_tokens = [&](int t0) {
-#pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        int tok = t0 + kt + i * STEP;
-        tok = tok < last ? tok : last;
-        const char* at = kb + page_at(k_id[i]) + static_cast<int64_t>(tok & mask) * token_stride + kc * 16;
-        ks[i] = kc * 8 < D ? *reinterpret_cast<const uint4*>(at) : uint4{0, 0, 0, 0};
+      for (int j = 0; j < J; ++j) {
+        const int tok = t0 + row_of[j] < last ? t0 + row_of[j] : last;
+        id_of[j] = row_pages[tok >> P.t.shift];
       }
-      const int run = run_of(t0 + vrun * 8);
-      const char* src = vb + page_at(v_id);
+    };
+    auto load_tokens = [&](int buf, int t0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int tok = run + e < last ? run + e : last;
-        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
-#pragma unroll
-        for (int i = 0; i < VB; ++i) {
-          const int d = vd + 128 * i;
-          vs[i][e] = v_takes && d < D ? *reinterpret_cast<const uint2*>(at + d * 2) : uint2{0, 0};
+      for (int j = 0; j < J; ++j) {
+        const int tok = t0 + row_of[j] < last ? t0 + row_of[j] : last;
+        const int piece = lane % PIECES ^ kv_swizzle<DP>(row_of[j]);
+        const int64_t at = page_at(id_of[j]) + static_cast<int64_t>(tok & mask) * token_stride + piece * 16;
+        const uint32_t to = buf * 64 * DP * 2 + (wave * J + j) * 1024;
+        if (piece * 8 < D) {
+          kv_to_lds(lds_k + to, kb + at);
+          kv_to_lds(lds_v + to, vb + at);
         }
       }
     };
+    // whether every token at first .. end sees the n tokens from t0 on
     auto whole_for = [&](int t0, int n, int first, int end) {
       return t0 + n - 1 <= first && (P.window <= 0 || t0 > end - P.window || t0 + n <= P.sinks);
     };
-    auto stage = [&](int buf, int t0) {
+    // this lane's places in 32 tokens: of the keys' row 8 (c / 4) + c % 4 (+ 4 u) piece 4 e + g, and of the
+    // values' row 8 g + c / 4 (+ 4 q) elements 16 t + 4 (c % 4) on
+    const int k_row = (c >> 2) * 8 + (c & 3), v_row = g * 8 + (c >> 2);
+    int k_at[QC];
 #pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        // token 8 g + 4 s + e of 32 is row 16 s + 4 g + e of the product
-        const int tok = kt + i * STEP;
-        const int row = (tok & 32) | (tok & 4) << 2 | (tok & 24) >> 1 | (tok & 3);
-        *reinterpret_cast<uint4*>(&sh.k[buf][row][kc * 8]) = ks[i];
+    for (int e = 0; e < QC; ++e) k_at[e] = k_row * DP + ((4 * e + g) ^ kv_swizzle<DP>(k_row)) * 8;
+    const int v_at = v_row * DP + ((c >> 1 & 1) ^ kv_swizzle<DP>(v_row)) * 8 + (c & 1) * 4;
+    // element 16 t + c of tokens 8 g .. 8 g + 7
+    auto values = [&](const uint16_t* base, int t) {
+      const uint16_t* at = base + (v_at ^ (16 * t));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * DP));
+      uint4 r;
+      __builtin_memcpy(&r.x, &lo, 8);
+      __builtin_memcpy(&r.z, &hi, 8);
+      return r;
+    };
+    // the 32 tokens from t0 on, whose keys and values start at kt and vt
+    auto multiply = [&](auto masked, const uint16_t* kt, const uint16_t* vt, int t0) {
+      constexpr bool MASKED = decltype(masked)::value;
+      f32x4 s[R][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        uint4 kf[QC];
+#pragma unroll
+        for (int e = 0; e < QC; ++e) kf[e] = *reinterpret_cast<const uint4*>(kt + k_at[e] + u * 4 * DP);
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < QC; ++e)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[e]),
+                                                              __builtin_bit_cast(bf16x8, qf[r][e]), s[r][u], 0, 0, 0);
       }
-      if (v_takes) {
-        bool odd = false;
+      bf16x8 pf[R];
 #pragma unroll
-        for (int i = 0; i < VB; ++i)
+      for (int r = 0; r < R; ++r) {
+        kv_soften<MASKED>(s[r], acc[r], &m[r], &l[r], P.scale2, t0 + g * 8, pos[r], P.window, P.sinks);
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            uint32_t w[4];
+        for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
+      }
+      bool odd = false;
+      if constexpr (MASKED) {
+        bool mine = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 a = values(vt, t);
+          auto nonfinite = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
+          mine |= nonfinite(a.x) || nonfinite(a.y) || nonfinite(a.z) || nonfinite(a.w);
+        }
+        odd = __any(mine);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 a = values(vt, t);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], acc[r][t], 0, 0, 0);
+        }
+      } else {
+        // in three parts, as in kv_attention_kernel
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 a = values(vt, t);
+          auto part = [&](auto sign) {
+            constexpr int SIGN = decltype(sign)::value;
+            return __builtin_bit_cast(bf16x8, uint4{kv_select<uint16_t, SIGN>(a.x), kv_select<uint16_t, SIGN>(a.y),
+                                                    kv_select<uint16_t, SIGN>(a.z), kv_select<uint16_t, SIGN>(a.w)});
+          };
+          const bf16x8 fin = part(std::integral_constant<int, 0>{}), up = part(std::integral_constant<int, 1>{}),
+                       down = part(std::integral_constant<int, -1>{});
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const f32x4 zero{0, 0, 0, 0};
+            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fin, pf[r], acc[r][t], 0, 0, 0);
+            const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, pf[r], zero, 0, 0, 0);
+            const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, pf[r], zero, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              w[e] = __builtin_amdgcn_perm(d < 2 ? vs[i][2 * e + 1].x : vs[i][2 * e + 1].y,
-                                           d < 2 ? vs[i][2 * e].x : vs[i][2 * e].y, d & 1 ? 0x07060302u : 0x05040100u);
-            *reinterpret_cast<uint4*>(&sh.v[buf][vd + 128 * i + d][vrun * 8]) = uint4{w[0], w[1], w[2], w[3]};
+              acc[r][t][e] = x[e] + (y[e] > 0.0f ? INFINITY : 0.0f) - (z[e] > 0.0f ? INFINITY : 0.0f);
           }
-        if (!whole_for(t0, BLK, p0, p1 - 1)) {
-#pragma unroll
-          for (int i = 0; i < VB; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint32_t x = vs[i][e].x, y = vs[i][e].y;
-              odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u || (y & 0x7f80u) == 0x7f80u ||
-                     (y & 0x7f800000u) == 0x7f800000u;
-            }
         }
-        if (odd) sh.odd[buf] = 1;
       }
     };
-    if (tid < 2) sh.odd[tid] = 0;
+    if (D < DP) {  // elements from D on are zero in Q, and here, whatever the LDS held
+      for (int e = tid; e < 2 * 64 * DP / 8; e += KV_ATT_NT) reinterpret_cast<uint4*>(&sh.k[0][0])[e] = uint4{0, 0, 0, 0};
+      __syncthreads();
+    }
     int i = from, buf = 0;
     if (i < to) {
       load_ids(token_of(i));
-      load_tokens(token_of(i));
+      load_tokens(0, token_of(i));
+      if (i + 1 < to) load_ids(token_of(i + 1));
     }
-    __syncthreads();  // the flags are clear
-    if (i < to) stage(0, token_of(i));
-    if (i + 1 < to) load_ids(token_of(i + 1));
+    kv_lds_wait();
     __syncthreads();
     for (; i < to; ++i, buf ^= 1) {
       const int t0 = token_of(i);
-      if (i + 1 < to) load_tokens(token_of(i + 1));
+      // (the other buffer was read before the last barrier)
+      if (i + 1 < to) load_tokens(buf ^ 1, token_of(i + 1));
       if (i + 2 < to) load_ids(token_of(i + 2));
-      const bool tile_odd = sh.odd[buf] != 0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int tb = t0 + 32 * h;
-        if (idle || tb > wp1) continue;
-        f32x4 s[R][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          uint4 kf[QC];
-#pragma unroll
-          for (int e = 0; e < QC; ++e) kf[e] = *reinterpret_cast<const uint4*>(&sh.k[buf][32 * h + 16 * u + c][e * 32 + g * 8]);
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            s[r][u] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < QC; ++e)
-              s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[e]),
-                                                                __builtin_bit_cast(bf16x8, qf[r][e]), s[r][u], 0, 0, 0);
-          }
-        }
-        const bool whole = whole_for(tb, 32, wp0, wp1);
-        bf16x8 pf[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) kv_soften<2, NT>(s[r], acc[r], &m[r], &l[r], P.scale2, whole, tb + g * 8, pos[r], P.window, P.sinks);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
-        if (whole || !tile_odd) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const uint4 a = *reinterpret_cast<const uint4*>(&sh.v[buf][16 * t + c][32 * h + g * 8]);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-              acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], acc[r][t], 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const uint4 a = *reinterpret_cast<const uint4*>(&sh.v[buf][16 * t + c][32 * h + g * 8]);
-            uint4 part[3];
-            part[0] = uint4{kv_select<uint16_t, 0>(a.x), kv_select<uint16_t, 0>(a.y), kv_select<uint16_t, 0>(a.z),
-                            kv_select<uint16_t, 0>(a.w)};
-            part[1] = uint4{kv_select<uint16_t, 1>(a.x), kv_select<uint16_t, 1>(a.y), kv_select<uint16_t, 1>(a.z),
-                            kv_select<uint16_t, 1>(a.w)};
-            part[2] = uint4{kv_select<uint16_t, -1>(a.x), kv_select<uint16_t, -1>(a.y), kv_select<uint16_t, -1>(a.z),
-                            kv_select<uint16_t, -1>(a.w)};
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const f32x4 zero{0, 0, 0, 0};
-              const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[0]), pf[r], acc[r][t], 0, 0, 0);
-              const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[1]), pf[r], zero, 0, 0, 0);
-              const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[2]), pf[r], zero, 0, 0, 0);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                acc[r][t][e] = x[e] + (up[e] > 0.0f ? INFINITY : 0.0f) - (down[e] > 0.0f ? INFINITY : 0.0f);
-            }
-          }
+      if (!idle) {
+#pragma unroll 1
+        for (int h = 0; h < BLK && t0 + h <= wp1; h += 32) {
+          const uint16_t *kt = &sh.k[buf][h * DP], *vt = &sh.v[buf][h * DP];
+          if (whole_for(t0 + h, 32, wp0, wp1))
+            multiply(std::false_type{}, kt, vt, t0 + h);
+          else
+            multiply(std::true_type{}, kt, vt, t0 + h);
         }
       }
-      // the other buffer was read before the last barrier, and its flag too
-      if (i + 1 < to) {
-        if (tid == 0) sh.odd[buf ^ 1] = 0;
-        if (!whole_for(token_of(i + 1), BLK, p0, p1 - 1)) __syncthreads();
-        stage(buf ^ 1, token_of(i + 1));
-      }
+      kv_lds_wait();
       __syncthreads();
     }
   }

@@ -441,7 +441,8 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.lse = lse;
   P.n_q_heads = n_q_heads;
   P.group = group;
-  P.scale2 = scale * KV_LOG2E;
+  P.scale2 = fabsf(scale) * KV_LOG2E;
+  P.flip = scale < 0.0f ? (bf ? 0x80008000u : 0x80000000u) : 0u;
   P.window = window;
   P.sinks = sinks;
   const AttentionWs at = attention_ws(dp, rows);
