@@ -203,7 +203,7 @@ def _dtype_code(dt):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
+    s = torch.cuda.current_stream(torch.cuda.current_device()) if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
 
 
@@ -503,15 +503,22 @@ def kv_pool(k, v):
 
 
 def _heads(t):
+    """Reference to the descriptor of a token array, or None."""
     if t is None:
         return None
-    if t.dim() != 3 or t.stride(2) != 1:
+    stride = t.stride()
+    if len(stride) != 3 or stride[2] != 1:
         raise ValueError("token arrays must be [n_tokens, heads, head_dim] with consecutive elements of a head")
-    return SakiKVHeads(_ptr(t), t.stride(0), t.stride(1))
+    return ctypes.byref(SakiKVHeads(t.data_ptr(), stride[0], stride[1]))
 
 
 def _ref(s):
     return None if s is None else ctypes.byref(s)
+
+
+def _addr(t):
+    """A tensor's address for a void * argument (declared as such: a number will do), or None."""
+    return None if t is None else t.data_ptr()
 
 
 def _ws_bytes(ws):
@@ -520,44 +527,42 @@ def _ws_bytes(ws):
 
 def saki_kv_reserve(table, pool, n_new, status=None, workspace=None, stream=None):
     """Call saki_kv_reserve; n_new: an int32 tensor [n_seq], or one number for every sequence."""
-    load()
+    _lib or load()
     each = isinstance(n_new, torch.Tensor)
     if not each and not 0 <= n_new < 2**31:
         raise ValueError("n_new outside [0, 2^31)")
-    _check(_lib.saki_kv_reserve(_ref(table), _ref(pool), _ptr(n_new) if each else None, 0 if each else int(n_new),
-                                _ptr(status), _ptr(workspace), _ws_bytes(workspace), _stream(stream)))
+    _check(_lib.saki_kv_reserve(_ref(table), _ref(pool), _addr(n_new) if each else None, 0 if each else int(n_new),
+                                _addr(status), _addr(workspace), _ws_bytes(workspace), _stream(stream)))
 
 
 def saki_kv_commit(table, delta, done=None, status=None, stream=None):
-    load()
-    _check(_lib.saki_kv_commit(_ref(table), _ptr(delta), _ptr(done), _ptr(status), _stream(stream)))
+    _lib or load()
+    _check(_lib.saki_kv_commit(_ref(table), _addr(delta), _addr(done), _addr(status), _stream(stream)))
 
 
 def saki_kv_fork(table, src, dst, status=None, stream=None):
-    load()
-    _check(_lib.saki_kv_fork(_ref(table), src.numel(), _ptr(src), _ptr(dst), _ptr(status), _stream(stream)))
+    _lib or load()
+    _check(_lib.saki_kv_fork(_ref(table), src.numel(), _addr(src), _addr(dst), _addr(status), _stream(stream)))
 
 
 def saki_kv_compact(table, pool, n_live=None, workspace=None, stream=None):
-    load()
-    _check(_lib.saki_kv_compact(_ref(table), _ref(pool), _ptr(n_live), _ptr(workspace), _ws_bytes(workspace),
+    _lib or load()
+    _check(_lib.saki_kv_compact(_ref(table), _ref(pool), _addr(n_live), _addr(workspace), _ws_bytes(workspace),
                                 _stream(stream)))
 
 
 def saki_kv_append(table, pool, layer, tokens, k, v, q=None, q_out=None, rope=None, stream=None):
     """Call saki_kv_append; tokens: a SakiKVTokens, rope: a SakiKVRope or None."""
-    load()
+    _lib or load()
     _check(_lib.saki_kv_append(_ref(table), _ref(pool), int(layer), _ref(tokens), _ref(rope),
-                               0 if q is None else q.shape[1], _ref(_heads(q)), _ref(_heads(q_out)), _ref(_heads(k)),
-                               _ref(_heads(v)), _stream(stream)))
+                               0 if q is None else q.shape[1], _heads(q), _heads(q_out), _heads(k), _heads(v), _stream(stream)))
 
 
 def saki_kv_attention(table, pool, layer, tokens, q, out, lse=None, scale=1.0, window=0, sinks=0, workspace=None,
                       stream=None):
-    load()
+    _lib or load()
     for name, x in (("window", window), ("sinks", sinks)):
         if not 0 <= x < 2**31:
             raise ValueError(f"{name} outside [0, 2^31)")
-    _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _ref(_heads(q)),
-                                  _ref(_heads(out)), _ptr(lse), float(scale), int(window), int(sinks), _ptr(workspace),
+    _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _heads(q), _heads(out), _addr(lse), float(scale), int(window), int(sinks), _addr(workspace),
                                   _ws_bytes(workspace), _stream(stream)))

@@ -41,6 +41,9 @@ def rope(rotary_dim, base=10000.0, interleaved=False, scaling=None, factor=1.0, 
     return dict(freq=f.to(device), rotary_dim=rotary_dim, interleaved=interleaved, amplitude=amplitude)
 
 
+_HERE = contextlib.nullcontext()
+
+
 class PagedKV:
     """A cache: tensors k, v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (any order of the
     first four axes in memory), pages [n_seq, max_pages], length [n_seq], held [n_seq], refs [n_pages]
@@ -53,6 +56,7 @@ class PagedKV:
             raise ValueError("refs must have an entry for every page of the pool")
         self.k, self.v, self.pages, self.length, self.held, self.refs = k, v, pages, length, held, refs
         self.device, self.dtype = k.device, k.dtype
+        self._sizes = {}  # workspace bytes of the calls made so far
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.n_seq = pages.shape[0]
         self.pool = _b.kv_pool(k, v)
@@ -69,21 +73,27 @@ class PagedKV:
                    torch.zeros(n_seq, **ints), torch.zeros(n_pages, **ints))
 
     # -- helpers ---------------------------------------------------------------
-    @contextlib.contextmanager
     def _on(self, stream):
         """The cache's device and the call's stream current: outputs and workspaces are allocated for it."""
-        with torch.cuda.device(self.device):
-            if stream is None:
-                yield
-            else:
-                with torch.cuda.stream(stream):
-                    yield
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return _HERE
+        return self._elsewhere(stream)
+
+    @contextlib.contextmanager
+    def _elsewhere(self, stream):
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):  # (no change where stream is None)
+            yield
 
     def _new(self, dtype, *shape):
         return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _workspace(self, op, n, m):
-        return self._new(torch.uint8, max(_b.workspace_bytes(op, n, m), 16))
+        size = self._sizes.get((op, n))
+        if size is None:
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            size = self._sizes[op, n] = max(_b.workspace_bytes(op, n, m), 16)
+        return self._new(torch.uint8, size)
 
     def _ints(self, name, t, n=None):
         _b._want(name, t, torch.int32, (self.n_seq if n is None else n,), self.device)
@@ -99,11 +109,9 @@ class PagedKV:
             raise ValueError("shift outside [0, 2^30]")
         return _b.SakiKVTokens(_b._ptr(offsets), n_tokens, n_new or 0, shift)
 
-    def _rows(self, name, t, n_tokens, heads=None):
-        if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != self.head_dim or \
-                (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{name} must be [{n_tokens}, {'heads' if heads is None else heads}, {self.head_dim}]: got "
-                             f"{tuple(t.shape)}")
+    def _rows(self, name, t, n_tokens, heads):
+        if t.shape != (n_tokens, heads, self.head_dim):
+            raise ValueError(f"{name} must be [{n_tokens}, {heads}, {self.head_dim}]: got {tuple(t.shape)}")
         if t.dtype != self.dtype or t.device != self.device:
             raise ValueError(f"{name} must be {self.dtype} on {self.device}")
 
@@ -161,7 +169,7 @@ class PagedKV:
         self._rows("k", k, n, self.n_kv_heads)
         self._rows("v", v, n, self.n_kv_heads)
         if q is not None:
-            self._rows("q", q, n)
+            self._rows("q", q, n, q.shape[1])
         tokens = self._tokens(n, n_new, offsets, shift)
         turn = None
         if rope is not None:
@@ -181,7 +189,7 @@ class PagedKV:
         in append, which comes first): causal, with window > 0 over the last `window` positions and the first
         `sinks`.  scale: head_dim^-1/2 if None.  lse: float32 [n_tokens, heads] to fill, or None.  Returns out."""
         n, heads = q.shape[0], q.shape[1]
-        self._rows("q", q, n)
+        self._rows("q", q, n, heads)
         tokens = self._tokens(n, n_new, offsets, shift)
         if lse is not None:
             _b._want("lse", lse, torch.float32, (n, heads), self.device)
