@@ -40,53 +40,124 @@ struct KvReserveParams {
   int32_t* n_moves;
 };
 
-// Free pages among refs[first .. first + 256): bit e of the lane's mask stands for
-// page first + 4 lane + e.
-__device__ __forceinline__ int kv_free_mask(const int32_t* refs, int n_pages, int first, bool vec) {
-  const int p = first + 4 * (threadIdx.x & (KV_WAVE - 1));
-  int m = 0;
-  if (vec && p + 4 <= n_pages) {
-    const int4 r = *reinterpret_cast<const int4*>(refs + p);
-    m = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-  } else {
+// Which pages are free, as bits.  A wave reads 256 counts at a time, 4 consecutive ones a lane:
+// bit `lane` of word e of a group stands for its page 4 lane + e.  The words of a pool of up to
+// KV_BITS_PAGES pages stay in LDS between the count and the search (a search that read the
+// counts again took 18 dependent loads a wave for 73,000 pages: 23 us a call, now 12);
+// those of a larger one are formed again.
+constexpr int KV_BITS_PAGES = 1 << 19;
+
+struct KvFree {
+  const int32_t* refs;
+  int n_pages;
+  bool vec;                  // refs lies on 16 bytes
+  unsigned long long* bits;  // LDS
+
+  __device__ __forceinline__ KvFree(const KvTable& t, unsigned long long* lds)
+      : refs(t.refs), n_pages(t.n_pages), vec((reinterpret_cast<uintptr_t>(t.refs) & 15u) == 0), bits(lds) {}
+
+  // pages of each wave: whole groups of 256, in order
+  __device__ __forceinline__ int per_wave() const {
+    return ((n_pages + KV_PLAN_WAVES * 256 - 1) / (KV_PLAN_WAVES * 256)) * 256;
+  }
+
+  __device__ __forceinline__ int4 counts(int first) const {
+    const int p = first + 4 * (threadIdx.x & (KV_WAVE - 1));
+    if (vec && p + 4 <= n_pages) return *reinterpret_cast<const int4*>(refs + p);
+    int4 r{1, 1, 1, 1};
+    if (p < n_pages) r.x = refs[p];
+    if (p + 1 < n_pages) r.y = refs[p + 1];
+    if (p + 2 < n_pages) r.z = refs[p + 2];
+    if (p + 3 < n_pages) r.w = refs[p + 3];
+    return r;
+  }
+
+  static __device__ __forceinline__ void words_of(int4 r, unsigned long long (&w)[4]) {
+    w[0] = __ballot(r.x == 0);
+    w[1] = __ballot(r.y == 0);
+    w[2] = __ballot(r.z == 0);
+    w[3] = __ballot(r.w == 0);
+  }
+
+  // free pages of this wave's part of the pool
+  __device__ __forceinline__ int count() {
+    constexpr int DEPTH = 16;
+    const int lane = threadIdx.x & (KV_WAVE - 1);
+    const int per = per_wave(), first = __builtin_amdgcn_readfirstlane(threadIdx.x / KV_WAVE) * per;
+    int n = 0;
+    for (int g0 = 0; g0 < per; g0 += DEPTH * 256) {
+      int4 r[DEPTH];
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) r[d] = g0 + d * 256 < per ? counts(first + g0 + d * 256) : int4{1, 1, 1, 1};
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        if (g0 + d * 256 >= per) break;
+        unsigned long long w[4];
+        words_of(r[d], w);
+        n += __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]);
+        if (n_pages <= KV_BITS_PAGES && lane < 4)
+          bits[(first + g0 + d * 256) / 64 + lane] = lane < 2 ? (lane == 0 ? w[0] : w[1]) : (lane == 2 ? w[2] : w[3]);
+      }
+    }
+    return n;
+  }
+
+  // words of the group from page `first` on (the same wave's part)
+  __device__ __forceinline__ void words(int first, unsigned long long (&w)[4]) const {
+    if (n_pages <= KV_BITS_PAGES) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = bits[first / 64 + e];
+    } else {
+      words_of(counts(first), w);
+    }
+  }
+
+  // free pages of the group before this lane's first
+  static __device__ __forceinline__ int before(const unsigned long long (&w)[4]) {
+    int n = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (p + e < n_pages) m |= (refs[p + e] == 0) << e;
+      n = __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(w[e] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(w[e]), n));
+    return n;
   }
-  return m;
-}
+  static __device__ __forceinline__ int all(const unsigned long long (&w)[4]) {
+    return __popcll(w[0]) + __popcll(w[1]) + __popcll(w[2]) + __popcll(w[3]);
+  }
+};
 
-// Pages of each wave: whole groups of 256, in order.
-__device__ __forceinline__ int kv_pages_per_wave(int n_pages) {
-  return ((n_pages + KV_PLAN_WAVES * 256 - 1) / (KV_PLAN_WAVES * 256)) * 256;
-}
-
-// Free pages of this wave's part of the pool.
-__device__ __forceinline__ int kv_count_free(const int32_t* refs, int n_pages, bool vec) {
-  const int per = kv_pages_per_wave(n_pages);
-  const int first = (threadIdx.x / KV_WAVE) * per;
-  int mine = 0;
-#pragma unroll 8
-  for (int g = 0; g < per; g += 256) mine += __popc(kv_free_mask(refs, n_pages, first + g, vec));
-  return kv_wave_sum(mine);
-}
+// What bounds it: latency, of a chain of dependent loads and barriers in the one workgroup.  The
+// first 1,024 sequences' requests stay in their threads' registers and up to KV_LIST_LDS pages
+// in LDS (wave of 512 sequences over 73,000 pages: 18 -> 12 us).
+constexpr int KV_LIST_LDS = 4096;
 
 __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams P) {
   const KvTable& t = P.t;
-  const int tid = threadIdx.x, wave = tid / KV_WAVE, lane = tid & (KV_WAVE - 1);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int page_mask = (1 << t.shift) - 1;
-  __shared__ int free_of[KV_PLAN_WAVES];
-  __shared__ long long part64[KV_PLAN_WAVES];
-  const bool vec = (reinterpret_cast<uintptr_t>(t.refs) & 15u) == 0;
+  __shared__ int free_of[KV_PLAN_WAVES], list_lds[KV_LIST_LDS], long_from[KV_PLAN_NT];
+  __shared__ long long part[KV_PLAN_WAVES];
+  __shared__ unsigned long long bits[KV_BITS_PAGES / 64];
 
-  const int counted = kv_count_free(t.refs, t.n_pages, vec);
+  // 1. what every sequence asks for (the loads of the first ones are under way while the
+  // free pages are counted)
+  auto asked_of = [&](int b) { return P.n_new ? P.n_new[b] : P.uniform; };
+  int n0 = 0, L0 = 0, H0 = 0;
+  if (tid < t.n_seq) {
+    n0 = asked_of(tid);
+    L0 = t.length[tid];
+    H0 = t.held[tid];
+  }
+  KvFree pool(t, bits);
+  const int counted = pool.count();
   if (lane == 0) free_of[wave] = counted;
 
-  // 1. what every sequence asks for
   bool shares = false;
+  KvWant first_want{-1, -1, 0, 0};  // that of sequence tid
+  int first_status = SAKI_KV_OK;
+  auto want_of = [&](int b) { return b == tid ? first_want : P.want[b]; };
   for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
-    const int n = P.n_new ? P.n_new[b] : P.uniform;
-    const int L = t.length[b], H = t.held[b];
+    const bool first = b == tid;
+    const int n = first ? n0 : asked_of(b), L = first ? L0 : t.length[b], H = first ? H0 : t.held[b];
     KvWant w{-1, -1, 0, 0};
     int st = SAKI_KV_OK;
     if (n < 0 || L < 0 || H < 0 || H > t.max_pages || static_cast<int64_t>(L) > (static_cast<int64_t>(H) << t.shift)) {
@@ -114,121 +185,140 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
         }
       }
     }
-    P.want[b] = w;
-    if (P.status) P.status[b] = static_cast<uint8_t>(st);
+    if (first) {
+      first_want = w;
+      first_status = st;
+    } else {
+      P.want[b] = w;
+      if (P.status) P.status[b] = static_cast<uint8_t>(st);
+    }
   }
   // 2. of a shared page's writers, the last keeps it if all its holders write
-  const bool any_shares = __syncthreads_or(shares);
-  if (any_shares) {
+  if (__syncthreads_or(shares)) {
     for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
-      const KvWant w = P.want[b];
+      const KvWant w = want_of(b);
       if (w.slot < 0) continue;
       atomicAdd(&P.writers[w.page], 1);
       atomicMax(&P.last[w.page], b);
     }
     __syncthreads();
     for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
-      const KvWant w = P.want[b];
+      const KvWant w = want_of(b);
       // (atomic reads: the counts were changed in the L2)
       if (w.slot >= 0 && __hip_atomic_load(&P.writers[w.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == t.refs[w.page] &&
-          __hip_atomic_load(&P.last[w.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == b)
-        P.want[b].slot = -1;
+          __hip_atomic_load(&P.last[w.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == b) {
+        if (b == tid)
+          first_want.slot = -1;
+        else
+          P.want[b].slot = -1;
+      }
     }
-    __syncthreads();
   }
-  // 3. how much that is: the call takes all of it or nothing
-  long long asked = 0, total64 = 0;
-  for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) {
-    const KvWant w = P.want[b];
-    asked += w.fresh + (w.slot >= 0);
+  // 3. how much that is: the call takes all of it or nothing.  Pages in the lower half, copies
+  // in the upper half of a sum (at most 2^24 sequences; a request of more than 2^31
+  // pages in all is more than any pool holds, however its sum carries)
+  auto sum_of = [&](const KvWant& w) {
+    const long long copy = w.slot >= 0;
+    return (copy << 40) + w.fresh + copy;
+  };
+  constexpr long long PAGES = (1ll << 40) - 1;
+  const bool one = t.n_seq <= KV_PLAN_NT;  // each sequence has a thread
+  long long all = 0, at0 = 0;
+  if (one) {
+    at0 = kv_block_scan<KV_PLAN_NT, long long>(sum_of(first_want), part, &all);
+  } else {
+    long long mine = 0;
+    for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) mine += sum_of(want_of(b));
+    kv_block_scan<KV_PLAN_NT, long long>(mine, part, &all);
   }
-  kv_block_scan<KV_PLAN_NT, long long>(asked, part64, &total64);
   int before = 0, n_free = 0;
   for (int w = 0; w < KV_PLAN_WAVES; ++w) {
     if (w < wave) before += free_of[w];
     n_free += free_of[w];
   }
-  if (total64 > n_free) {
-    if (P.status)
-      for (int b = tid; b < t.n_seq; b += KV_PLAN_NT)
-        if ((P.n_new ? P.n_new[b] : P.uniform) > 0 && P.status[b] == SAKI_KV_OK) P.status[b] = SAKI_KV_NO_PAGES;
-    if (tid == 0) *P.n_moves = 0;
-    return;
+  const bool enough = (all & PAGES) <= n_free;
+  if (P.status) {
+    if (tid < t.n_seq)
+      P.status[tid] = static_cast<uint8_t>(!enough && n0 > 0 && first_status == SAKI_KV_OK ? SAKI_KV_NO_PAGES : first_status);
+    if (!enough)
+      for (int b = tid + KV_PLAN_NT; b < t.n_seq; b += KV_PLAN_NT)
+        if (asked_of(b) > 0 && P.status[b] == SAKI_KV_OK) P.status[b] = SAKI_KV_NO_PAGES;
   }
-  const int total = static_cast<int>(total64);
-  if (total == 0) {
-    if (tid == 0) *P.n_moves = 0;
-    return;
-  }
+  const int total = enough ? static_cast<int>(all & PAGES) : 0;
+  if (tid == 0) *P.n_moves = enough ? static_cast<int>(all >> 40) : 0;
+  if (total == 0) return;
   // 4. the lowest `total` free pages, ascending
+  const bool in_lds = total <= KV_LIST_LDS;
   {
-    const int per = kv_pages_per_wave(t.n_pages);
+    const int per = pool.per_wave();
     const int first = wave * per;
     int rank = before;
     for (int g = 0; g < per && rank < total; g += 256) {
-      const int m = kv_free_mask(t.refs, t.n_pages, first + g, vec);
-      const int c = __popc(m);
-      const int in = kv_wave_scan(c);
-      int at = rank + in - c;
+      unsigned long long w[4];
+      pool.words(first + g, w);
+      int at = rank + KvFree::before(w);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if ((m >> e) & 1) {
-          if (at < total) P.list[at] = first + g + 4 * lane + e;
+        if ((w[e] >> lane) & 1) {
+          if (at < total) {
+            if (in_lds)
+              list_lds[at] = first + g + 4 * lane + e;
+            else
+              P.list[at] = first + g + 4 * lane + e;
+          }
           ++at;
         }
-      rank += __shfl(in, KV_WAVE - 1);
+      rank += KvFree::all(w);
     }
   }
   __syncthreads();
+  auto taken = [&](int i) { return in_lds ? list_lds[i] : P.list[i]; };
   // 5. each sequence its share, in order; long shares by whole waves
-  int base = 0, n_moves = 0;
-  __shared__ int long_from[KV_PLAN_NT];
+  long long done = 0;
   for (int b0 = 0; b0 < t.n_seq; b0 += KV_PLAN_NT) {
     const int b = b0 + tid;
-    const KvWant w = b < t.n_seq ? P.want[b] : KvWant{-1, -1, 0, 0};
+    const KvWant w = b < t.n_seq ? want_of(b) : KvWant{-1, -1, 0, 0};
     const bool copy = w.slot >= 0;
-    // (both prefix sums in one: copies in the upper half)
     long long sum = 0;
-    const long long mine = (static_cast<long long>(copy) << 32) | static_cast<unsigned>(w.fresh + copy);
-    const long long at = kv_block_scan<KV_PLAN_NT, long long>(mine, part64, &sum);
-    int from = base + static_cast<int>(at & 0xffffffff);
+    const long long at = done + (one ? at0 : kv_block_scan<KV_PLAN_NT, long long>(sum_of(w), part, &sum));
+    done += sum;
+    int from = static_cast<int>(at & PAGES);
+    const int64_t row = static_cast<int64_t>(b) * t.max_pages;
     if (copy) {
-      const int to = P.list[from];
-      P.moves[n_moves + static_cast<int>(at >> 32)] = KvMove{w.page, to, w.fill};
-      t.pages[static_cast<int64_t>(b) * t.max_pages + w.slot] = to;
+      const int to = taken(from);
+      P.moves[at >> 40] = KvMove{w.page, to, w.fill};
+      t.pages[row + w.slot] = to;
       t.refs[to] = 1;
       atomicSub(&t.refs[w.page], 1);
       ++from;
     }
     const bool is_long = w.fresh > 8;
-    if (w.fresh > 0) {
-      const int H = t.held[b];
-      if (!is_long)
-        for (int i = 0; i < w.fresh; ++i) {
-          const int id = P.list[from + i];
-          t.pages[static_cast<int64_t>(b) * t.max_pages + H + i] = id;
-          t.refs[id] = 1;
-        }
-    }
-    long_from[tid] = is_long ? from : -1;
+    const int H = w.fresh > 0 ? (b == tid ? H0 : t.held[b]) : 0;
+    if (!is_long)
+      for (int i = 0; i < w.fresh; ++i) {
+        const int id = taken(from + i);
+        t.pages[row + H + i] = id;
+        t.refs[id] = 1;
+      }
+    if (w.fresh > 0) t.held[b] = H + w.fresh;
     if (__syncthreads_or(is_long)) {
+      __shared__ int long_held[KV_PLAN_NT], long_n[KV_PLAN_NT];
+      long_from[tid] = is_long ? from : -1;
+      long_held[tid] = H;
+      long_n[tid] = w.fresh;
+      __syncthreads();
       for (int s = wave; s < KV_PLAN_NT && b0 + s < t.n_seq; s += KV_PLAN_WAVES) {
         const int f = long_from[s];
         if (f < 0) continue;
-        const int H = t.held[b0 + s], n = P.want[b0 + s].fresh;
-        for (int i = lane; i < n; i += KV_WAVE) {
-          const int id = P.list[f + i];
-          t.pages[static_cast<int64_t>(b0 + s) * t.max_pages + H + i] = id;
+        for (int i = lane; i < long_n[s]; i += KV_WAVE) {
+          const int id = taken(f + i);
+          t.pages[static_cast<int64_t>(b0 + s) * t.max_pages + long_held[s] + i] = id;
           t.refs[id] = 1;
         }
       }
       __syncthreads();
     }
-    if (w.fresh > 0) t.held[b] += w.fresh;
-    base += static_cast<int>(sum & 0xffffffff);
-    n_moves += static_cast<int>(sum >> 32);
   }
-  if (tid == 0) *P.n_moves = n_moves;
 }
 
 // Copies pages: a unit is the slots of one head of one page of one layer, of the
@@ -364,8 +454,9 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_compact_kernel(KvCompactParams 
   const KvTable& t = P.t;
   const int tid = threadIdx.x, wave = tid / KV_WAVE, lane = tid & (KV_WAVE - 1);
   __shared__ int free_of[KV_PLAN_WAVES], holes_of[KV_PLAN_WAVES];
-  const bool vec = (reinterpret_cast<uintptr_t>(t.refs) & 15u) == 0;
-  const int counted = kv_count_free(t.refs, t.n_pages, vec);
+  __shared__ unsigned long long bits[KV_BITS_PAGES / 64];
+  KvFree pool(t, bits);
+  const int counted = pool.count();
   if (lane == 0) free_of[wave] = counted;
   __syncthreads();
   int free_before = 0, n_free = 0;
@@ -374,23 +465,21 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_compact_kernel(KvCompactParams 
     n_free += free_of[w];
   }
   const int n_live = t.n_pages - n_free;
-  const int per = kv_pages_per_wave(t.n_pages);
+  const int per = pool.per_wave();
   const int first = wave * per;
   // ranks among all free and all live pages; of those, the holes are the free
   // pages below n_live, which are the first ones, and the moving pages the last
   int holes = 0;
   int rank = free_before;
   for (int g = 0; g < per; g += 256) {
-    const int m = kv_free_mask(t.refs, t.n_pages, first + g, vec);
-    const int c = __popc(m);
-    const int in = kv_wave_scan(c);
-    int f = rank + in - c;  // free pages before this lane's first
+    unsigned long long w[4];
+    pool.words(first + g, w);
+    int f = rank + KvFree::before(w);  // free pages before this lane's first
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int p = first + g + 4 * lane + e;
       if (p >= t.n_pages) break;
-      const bool is_free = (m >> e) & 1;
-      if (is_free) {
+      if ((w[e] >> lane) & 1) {
         if (p < n_live) {
           P.holes[f] = p;
           ++holes;
@@ -404,7 +493,7 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_compact_kernel(KvCompactParams 
         P.live[n_live - 1 - (p - f)] = p;
       }
     }
-    rank += __shfl(in, KV_WAVE - 1);
+    rank += KvFree::all(w);
   }
   holes = kv_wave_sum(holes);
   if (lane == 0) holes_of[wave] = holes;

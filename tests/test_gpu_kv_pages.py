@@ -136,6 +136,26 @@ def test_long_sequences_and_many_pages(saki_lib):
     same_table(c, t)
 
 
+@pytest.mark.parametrize("n_pages", [524287, 524288, 600001])
+def test_pools_around_half_a_million_pages(saki_lib, n_pages):
+    """The free pages of larger pools are searched for in another way; refs need not lie on 16 bytes."""
+    rng = np.random.default_rng(n_pages)
+    t = ocache.Table(4, 60000, n_pages, 8)
+    t.refs[:] = rng.random(n_pages) < 0.8
+    k = torch.zeros(1, n_pages, 1, 8, 8, dtype=torch.bfloat16, device=DEV)
+    c = to_cache(saki_lib, t, k, k.clone())
+    refs = torch.zeros(n_pages + 1, dtype=torch.int32, device=DEV)[1:]
+    refs.copy_(c.refs)
+    c = saki_lib.PagedKV(c.k, c.v, c.pages, c.length, c.held, refs)
+    for want in ([3, 0, 100, 9], [5, 40000 * 8, 1, 1], [0, 0, 0, 10**5 * 8]):
+        status, _ = t.reserve(want)
+        assert c.reserve(i32(want)).cpu().tolist() == status
+        same_table(c, t)
+    n_live, moves = t.compact()
+    assert int(c.compact()) == n_live
+    same_table(c, t)
+
+
 def test_captured_wave_replays(saki_lib):
     """reserve and commit in a graph, replayed with eager work between: each replay as the oracle."""
     t = filled([5, 30, 17, 0], 8, 40, 12, np.random.default_rng(5))
