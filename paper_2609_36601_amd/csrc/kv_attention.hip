@@ -8,16 +8,17 @@ namespace {
 
 template <typename T, int DP, int ROWS>
 hipError_t launch(void (*kernel)(KvAttnParams), const KvAttnParams& P, int64_t units, bool join, hipStream_t st) {
-  constexpr int64_t ITEMS = 1 << KV_ATT_ITEMS_LOG2<ROWS>;
+  constexpr int64_t ITEMS = KV_MOST_ITEMS<T, DP, ROWS>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(units + ITEMS)), dim3(KV_ATT_NT), 0, st, P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !join) return e;
-  const unsigned split_units = static_cast<unsigned>(units < ITEMS ? units : ITEMS);
-  // one row a workgroup where that fills the card but little more, else four
-  if (split_units * ROWS <= 4096)
-    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 1>), dim3(split_units * ROWS), dim3(KV_ATT_NT), 0, st, P);
+  // one row a workgroup where few units can be split, else four; at most so many
+  // workgroups as the card takes at once
+  const int64_t rows = (units < ITEMS ? units : ITEMS) * ROWS;
+  if (rows <= 4096)
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 1>), dim3(static_cast<unsigned>(rows)), dim3(KV_ATT_NT), 0, st, P);
   else
-    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 4>), dim3(split_units * ROWS / 4), dim3(KV_ATT_NT), 0, st, P);
+    hipLaunchKernelGGL((kv_join_kernel<T, DP, ROWS, 4>), dim3(8 * KV_CUS), dim3(KV_ATT_NT), 0, st, P);
   return hipGetLastError();
 }
 

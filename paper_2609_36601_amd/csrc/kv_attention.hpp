@@ -30,11 +30,31 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int KV_ATT_NT = 256;
 constexpr int KV_ATT_WAVES = KV_ATT_NT / KV_WAVE;
 constexpr int KV_ATT_ROWS = 64;  // most rows of a tile of kv_attention_kernel
-// Items that a call is split into where it has fewer units.
-template <int ROWS>
-constexpr int KV_ATT_ITEMS_LOG2 = ROWS <= KV_ATT_ROWS ? 10 : 9;
 constexpr float KV_LOG2E = 1.44269504088896340736f;
 constexpr float KV_LN2 = 0.693147180559945309417f;
+
+constexpr int KV_PROMPT_ROWS = 128;
+
+// Workgroups of kv_attention_kernel that a CU takes (one wave of each on every SIMD), by the
+// registers of a wave: O and Q of its R row tiles, a block's keys and values.  More waves that
+// spill are slower: 512 drafts x 4,480 keys at three a CU with 68 bytes spilled 1,672 us,
+// at two without 1,527.
+template <typename T>
+constexpr int kv_groups_per_cu(int dp, int r) {
+  const int own = sizeof(T) == 2 ? dp / 4 + dp / 8 : dp / 4 + dp / 4, block = dp / 2;
+  const int regs = own * r + block;
+  return regs <= 64 ? 4 : regs <= 80 ? 3 : regs <= 160 ? 2 : 1;
+}
+
+// Items that a call with fewer units is split into: what the card takes at once, or four
+// times that where an item then still has KV_LONG_ITEM blocks, so that the last ones to
+// end are short (128 verifications of 1,800 to 7,200 keys: 505 -> 440 us).
+constexpr int KV_CUS = 256;
+constexpr int KV_LONG_ITEM = 128;
+template <typename T, int DP, int ROWS>
+constexpr int KV_ITEMS = KV_CUS * (ROWS == KV_PROMPT_ROWS ? 2 : kv_groups_per_cu<T>(DP, ROWS / 16));
+template <typename T, int DP, int ROWS>
+constexpr int KV_MOST_ITEMS = (ROWS == KV_PROMPT_ROWS ? 1 : 4) * KV_ITEMS<T, DP, ROWS>;
 
 struct KvItem;
 
@@ -51,6 +71,7 @@ struct KvAttnParams {
   float* part;     // [slots][rows][DP] partial sums, then
   float* part_ml;  // [slots][rows][2] their maximum and sum
   int slots;
+  int units;              // no more units than this
   int* n_split;           // how many units are split, and which: for kv_join_kernel
   KvItem* split;   // [items]
 };
@@ -133,10 +154,9 @@ __device__ __forceinline__ int kv_split_at(int blocks, int splits, int split) {
 // itself, which spares a launch.  Items of a sequence are ordered by tile (last first: with
 // causal rows those are the longest), split, key head, so that the workgroups of one key
 // head, which read the same keys, tend to one XCD.  False: there is no such item.
-template <int ROWS, int BLK>
+template <int ROWS, int BLK, int ITEMS, int MOST_ITEMS>
 __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out) {
-  constexpr int ITEMS_LOG2 = KV_ATT_ITEMS_LOG2<ROWS>;
-  __shared__ long long part[KV_ATT_WAVES];
+  __shared__ long long part[2][KV_ATT_WAVES];
   __shared__ KvItem found;
   __shared__ int is_found;
   const int tid = threadIdx.x;
@@ -151,13 +171,14 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
     blocks += static_cast<long long>(keep.tiles) * keep.blocks;
   }
   // blocks an item takes: what gives the call its number of items, and at least 8
-  blocks = kv_wave_sum(blocks);
-  if ((tid & (KV_WAVE - 1)) == 0) part[tid / KV_WAVE] = blocks;
-  __syncthreads();
   long long all = 0;
-#pragma unroll
-  for (int w = 0; w < KV_ATT_WAVES; ++w) all += part[w];
-  all = (all * Hk + (1 << ITEMS_LOG2) - 1) >> ITEMS_LOG2;
+  kv_block_scan<KV_ATT_NT, long long>(blocks, part[0], &all);
+  all *= Hk;
+  // (a unit's items are rounded up, by half of one on average)
+  const int aim = P.units < ITEMS ? ITEMS - P.units / 2 : ITEMS;
+  const bool many = MOST_ITEMS > ITEMS && all >= static_cast<long long>(KV_LONG_ITEM) * ITEMS;
+  all = many ? (all + MOST_ITEMS - 1) / MOST_ITEMS
+             : all < (1 << 30) ? (static_cast<int>(all) + aim - 1) / aim : (all + ITEMS - 1) / ITEMS;
   const unsigned len = all < 8 ? 8u : all < (1 << 30) ? static_cast<unsigned>(all) : 1u << 30;
   // Sums over the sequences: items; slots of the split units' items, fewer than twice the
   // items aimed at; split units, fewer than those (each has more blocks than an item).
@@ -172,9 +193,10 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
     if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
     mine += sums_of(keep, &n);
   }
-  long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part, &total);
+  long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part[1], &total);
   const unsigned item = blockIdx.x;
-  if (item == 0 && tid == 0) *P.n_split = static_cast<int>(total >> 48);
+  // (the bound only matters for token ranges that overlap, whose sums may pass their fields)
+  if (item == 0 && tid == 0) *P.n_split = min(static_cast<int>(total >> 48) & 0xffff, MOST_ITEMS);
   if (item >= static_cast<unsigned>(at) && item - static_cast<unsigned>(at) < static_cast<unsigned>(mine)) {
     for (int b = b0; b < b1; ++b) {
       if (per > 1) {
@@ -200,7 +222,7 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
         found = f;
         is_found = 1;
         const int unit = static_cast<int>((at >> 48) & 0xffff) + back * Hk + f.head;
-        if (n > 1 && f.split == 0 && unit >= 0 && unit < 1 << ITEMS_LOG2) P.split[unit] = f;
+        if (n > 1 && f.split == 0 && unit >= 0 && unit < MOST_ITEMS) P.split[unit] = f;
         break;
       }
       at += mine;
@@ -209,12 +231,6 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
   __syncthreads();
   *out = kv_uniform(found);
   return __builtin_amdgcn_readfirstlane(is_found) != 0;
-}
-
-// Workgroups that the registers of a CU hold (one wave of each on every SIMD).
-template <typename T>
-constexpr int kv_groups_per_cu(int dp, int r) {
-  return dp * r <= 64 ? 4 : dp * r <= 128 ? 3 : dp * r <= 256 ? 2 : 1;
 }
 
 template <typename T>
@@ -302,7 +318,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   __shared__ float join_m[KV_ATT_WAVES][ROWS], join_l[KV_ATT_WAVES][ROWS];
 
   KvItem it;
-  if (!kv_find_item<ROWS, BLK>(P, &it)) return;
+  if (!kv_find_item<ROWS, BLK, KV_ITEMS<T, DP, ROWS>, KV_MOST_ITEMS<T, DP, ROWS>>(P, &it)) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;
@@ -586,72 +602,90 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   }
 }
 
-// Joins the partial sums of the split units, of which there are no more than
-// items aimed at (each has more blocks than an item takes).  A workgroup takes JR rows of a unit; 16
-// threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.
+// Joins the partial sums of the split units, of which there are no more than items aimed at
+// (each has more blocks than an item takes).  A workgroup takes JR rows of a unit at a time;
+// 16 threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.
 template <typename T, int DP, int ROWS, int JR>
 __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
   constexpr int NT = DP / 16, PER = ROWS / JR, GROUPS = 16 / JR;
   __shared__ float sum_o[KV_ATT_NT][NT + 1];
   __shared__ float sum_m[16], sum_l[16];
-  if (static_cast<int>(blockIdx.x / PER) >= *P.n_split) return;
-  const KvItem it = kv_uniform(P.split[blockIdx.x / PER]);
   const int tid = threadIdx.x, jc = tid & 15, jr = (tid >> 4) % JR, grp = (tid >> 4) / JR;
   const int D = P.p.dim, G = P.group;
-  const int row0 = it.tile * ROWS, rows = it.count * G;
-  const int row = static_cast<int>(blockIdx.x % PER) * JR + jr;
-  const bool real = row0 + row < rows && it.slot >= 0 && it.slot + it.splits <= P.slots;
-  float m = -INFINITY, l = 0.0f, o[NT];
+  const int n = *P.n_split * PER;
+  for (int work = blockIdx.x; work < n; work += gridDim.x) {
+    const KvItem it = kv_uniform(P.split[work / PER]);
+    const int row0 = it.tile * ROWS, rows = it.count * G;
+    const int row = work % PER * JR + jr;
+    const bool real = row0 + row < rows && it.slot >= 0 && it.slot + it.splits <= P.slots;
+    float m = -INFINITY, l = 0.0f, o[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) o[t] = 0.0f;
-  if (real) {
-    const float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
-    const float* po = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + jc * NT;
-    for (int s = grp; s < it.splits; s += GROUPS) m = fmaxf(m, ml[static_cast<int64_t>(s) * ROWS * 2]);
-    const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll 4
-    for (int s = grp; s < it.splits; s += GROUPS) {
-      const float f = __builtin_amdgcn_exp2f(ml[static_cast<int64_t>(s) * ROWS * 2] - ref);
-      l += f * ml[static_cast<int64_t>(s) * ROWS * 2 + 1];
-      const float* x = po + static_cast<int64_t>(s) * ROWS * DP;
+    for (int t = 0; t < NT; ++t) o[t] = 0.0f;
+    if (real) {
+      const float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
+      const float* po = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + jc * NT;
+      // one pass, four splits' loads at a time
+      for (int s0 = grp; s0 < it.splits; s0 += 4 * GROUPS) {
+        float sm[4], sl[4];
+        f32x4 so[4][NT / 4];
 #pragma unroll
-      for (int t = 0; t < NT; t += 4) {
-        const f32x4 y = *reinterpret_cast<const f32x4*>(x + t);
+        for (int i = 0; i < 4; ++i) {
+          const int64_t s = s0 + i * GROUPS < it.splits ? s0 + i * GROUPS : s0;
+          sm[i] = s0 + i * GROUPS < it.splits ? ml[s * ROWS * 2] : -INFINITY;
+          sl[i] = ml[s * ROWS * 2 + 1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[t + e] += f * y[e];
+          for (int t = 0; t < NT / 4; ++t) so[i][t] = *reinterpret_cast<const f32x4*>(po + s * ROWS * DP + 4 * t);
+        }
+        const float to = fmaxf(fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), m);
+        const float ref = to == -INFINITY ? 0.0f : to;
+        const float old = __builtin_amdgcn_exp2f(m - ref);
+        m = to;
+        l *= old;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t] *= old;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (s0 + i * GROUPS >= it.splits) break;
+          const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
+          l += f * sl[i];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) o[t] += f * so[i][t / 4][t % 4];
+        }
       }
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum_o[tid][t] = o[t];
+    if (jc == 0) {
+      sum_m[tid >> 4] = m;
+      sum_l[tid >> 4] = l;
+    }
+    __syncthreads();
+    if (grp == 0 && real) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < GROUPS; ++w) top = fmaxf(top, sum_m[w * JR + jr]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < GROUPS; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sum_m[w * JR + jr] - ref);
+        sum += f * sum_l[w * JR + jr];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t] += f * sum_o[(w * JR + jr) * 16 + jc][t];
+      }
+      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
+      if (P.lse && jc == 0)
+        P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
+    }
+    __syncthreads();  // before the sums are written again
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) sum_o[tid][t] = o[t];
-  if (jc == 0) {
-    sum_m[tid >> 4] = m;
-    sum_l[tid >> 4] = l;
-  }
-  __syncthreads();
-  if (grp != 0 || !real) return;
-  float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < GROUPS; ++w) top = fmaxf(top, sum_m[w * JR + jr]);
-  const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) o[t] = 0.0f;
-#pragma unroll
-  for (int w = 0; w < GROUPS; ++w) {
-    const float f = __builtin_amdgcn_exp2f(sum_m[w * JR + jr] - ref);
-    sum += f * sum_l[w * JR + jr];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) o[t] += f * sum_o[(w * JR + jr) * 16 + jc][t];
-  }
-  const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-    if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
-  if (P.lse && jc == 0)
-    P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
 }
 
 // Prompts: many rows a sequence.  Each of the four waves takes 32 rows of the item's 128, and
@@ -687,15 +721,13 @@ __device__ __forceinline__ void kv_lds_wait() { asm volatile("s_waitcnt vmcnt(0)
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int KV_PROMPT_ROWS = 128;
-
 template <int DP>
 __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P) {
   constexpr int R = 2, BLK = 64, ROWS = KV_PROMPT_ROWS;
   constexpr int NT = DP / 16, QC = DP / 32;
   __shared__ KvPromptShared<DP> sh;
   KvItem it;
-  if (!kv_find_item<ROWS, BLK>(P, &it)) return;
+  if (!kv_find_item<ROWS, BLK, KV_ITEMS<uint16_t, DP, ROWS>, KV_MOST_ITEMS<uint16_t, DP, ROWS>>(P, &it)) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;

@@ -137,21 +137,44 @@ KvStrides device_heads(const saki_kv_heads* x, const saki_kv_pool* p) {
 
 int pow2_dim(int64_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Workspace of an attention call of `rows` query rows: the split units, and slots for
-// the partial sums of their items, at most twice the items aimed at (a unit of more
-// than one item fills at least half of each).  Tiles have no more rows than the call.
+// Workspace of an attention call with tiles of ROWS rows: the split units, and slots for the
+// partial sums of their items, at most twice the items aimed at (a unit of more than one
+// item fills at least half of each).
 struct AttentionWs {
   int64_t split, part, slots, part_ml, bytes;
 };
-AttentionWs attention_ws(int dp, int tile_rows) {
+template <typename T, int DP, int ROWS>
+AttentionWs attention_ws_of() {
   AttentionWs w{};
-  const int64_t items = int64_t{1} << (tile_rows > KV_ATT_ROWS ? KV_ATT_ITEMS_LOG2<KV_PROMPT_ROWS> : KV_ATT_ITEMS_LOG2<KV_ATT_ROWS>);
+  constexpr int64_t ITEMS = KV_MOST_ITEMS<T, DP, ROWS>;
   w.split = 16;  // after their number
-  w.part = w.split + up16(items * static_cast<int64_t>(sizeof(KvItem)));
-  w.slots = 2 * items;
-  w.part_ml = w.part + w.slots * tile_rows * dp * 4;
-  w.bytes = w.part_ml + w.slots * tile_rows * 8;
+  w.part = w.split + up16(ITEMS * static_cast<int64_t>(sizeof(KvItem)));
+  w.slots = 2 * ITEMS;
+  w.part_ml = w.part + w.slots * ROWS * DP * 4;
+  w.bytes = w.part_ml + w.slots * ROWS * 8;
   return w;
+}
+template <typename T, int DP>
+AttentionWs attention_ws_rows(int rows) {
+  if (rows == KV_PROMPT_ROWS) return attention_ws_of<T, DP, KV_PROMPT_ROWS>();
+  return rows == 64 ? attention_ws_of<T, DP, 64>() : rows == 32 ? attention_ws_of<T, DP, 32>() : attention_ws_of<T, DP, 16>();
+}
+AttentionWs attention_ws(bool bf, int dp, int rows) {
+  if (bf)
+    return dp == 64    ? attention_ws_rows<uint16_t, 64>(rows)
+           : dp == 128 ? attention_ws_rows<uint16_t, 128>(rows)
+                       : attention_ws_rows<uint16_t, 256>(rows);
+  return dp == 64    ? attention_ws_rows<float, 64>(rows)
+         : dp == 128 ? attention_ws_rows<float, 128>(rows)
+                     : attention_ws_rows<float, 256>(rows);
+}
+
+// Row tiles a workgroup takes in a call of `mean` rows a sequence and key head: those
+// of a sequence of mean length; past 64, the kernel for prompts.
+int attention_tiles(bool bf, int dp, int64_t mean) {
+  if (bf && dp <= 128 && mean > 64) return KV_PROMPT_ROWS / 16;
+  const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
+  return std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
 }
 
 struct ReserveWs {
@@ -214,8 +237,13 @@ size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
     case SAKI_OP_KV_COMPACT:
       return m > MAX_TOKENS ? 0 : static_cast<size_t>(compact_ws(m).bytes);
     case SAKI_OP_KV_ATTENTION: {
-      // (prompts' tiles have twice the rows and half the slots)
-      return static_cast<size_t>(attention_ws(pow2_dim(m), n <= 16 ? 16 : n <= 32 ? 32 : KV_ATT_ROWS).bytes);
+      // (a call's rows are at least those of a sequence of mean length, its tile's rows)
+      int64_t most = 0;
+      for (const int64_t rows : {1, 17, 33, 65})
+        if (rows <= n)
+          for (const bool bf : {false, true})
+            most = std::max(most, attention_ws(bf, pow2_dim(m), 16 * attention_tiles(bf, pow2_dim(m), rows)).bytes);
+      return static_cast<size_t>(most);
     }
     default:
       return 0;
@@ -422,16 +450,11 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   const bool bf = pool->dtype == SAKI_BF16;
   const int dp = pow2_dim(pool->head_dim);
   const int group = n_q_heads / pool->n_kv_heads;
-  // rows of a tile: those of a sequence of mean length
-  const int64_t mean = n * group / table->n_seq;
-  const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
-  const int tiles = bf && dp <= 128 && mean > KV_ATT_ROWS ? KV_PROMPT_ROWS / 16
-                                                          : std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
-  const int rows = 16 * tiles;
+  const int tiles = attention_tiles(bf, dp, n * group / table->n_seq), rows = 16 * tiles;
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;
-  if (units > INT32_MAX - 4096) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  if (units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
   KvAttnParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);
@@ -445,13 +468,14 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.flip = scale < 0.0f ? (bf ? 0x80008000u : 0x80000000u) : 0u;
   P.window = window;
   P.sinks = sinks;
-  const AttentionWs at = attention_ws(dp, rows);
+  const AttentionWs at = attention_ws(bf, dp, rows);
   char* w = static_cast<char*>(ws);
   P.n_split = reinterpret_cast<int*>(w);
   P.split = reinterpret_cast<KvItem*>(w + at.split);
   P.part = reinterpret_cast<float*>(w + at.part);
   P.part_ml = reinterpret_cast<float*>(w + at.part_ml);
   P.slots = static_cast<int>(at.slots);
+  P.units = static_cast<int>(units);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   // without more than 8 blocks of keys in any sequence nothing is split
   const bool join = table->max_pages * table->page_size > 8 * (bf ? 32 : 16);

@@ -53,34 +53,49 @@ __device__ __forceinline__ int kv_held(const KvTable& t, int b) {
   return h < 0 ? 0 : h > t.max_pages ? t.max_pages : h;
 }
 
-template <typename V>
-__device__ __forceinline__ V kv_wave_sum(V x) {
-#pragma unroll
-  for (int w = KV_WAVE / 2; w > 0; w >>= 1) x += __shfl_xor(x, w);
-  return x;
+// x of another lane by a data-parallel move, 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int kv_dpp(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, true);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ long long kv_dpp(long long x) {
+  const unsigned lo = static_cast<unsigned>(kv_dpp<CTRL, ROWS>(static_cast<int>(x)));
+  const unsigned hi = static_cast<unsigned>(kv_dpp<CTRL, ROWS>(static_cast<int>(x >> 32)));
+  return static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
 }
 
-// Inclusive prefix sum over the lanes of a wave.
+// Inclusive prefix sum over the lanes of a wave: within the rows of 16 by shifts, then each
+// row's last lane to the rows behind it.
 template <typename V>
 __device__ __forceinline__ V kv_wave_scan(V x) {
-  const int lane = threadIdx.x & (KV_WAVE - 1);
-#pragma unroll
-  for (int w = 1; w < KV_WAVE; w <<= 1) {
-    const V y = __shfl_up(x, w);
-    if (lane >= w) x += y;
-  }
+  x += kv_dpp<0x111, 0xF>(x);
+  x += kv_dpp<0x112, 0xF>(x);
+  x += kv_dpp<0x114, 0xF>(x);
+  x += kv_dpp<0x118, 0xF>(x);
+  x += kv_dpp<0x142, 0xA>(x);
+  x += kv_dpp<0x143, 0xC>(x);
   return x;
 }
 
-// Exclusive prefix sum over the workgroup's NT threads and the total; `part` is
-// NT / 64 values of LDS that the call may be the only one to use until the next
-// barrier.
+__device__ __forceinline__ int kv_last(int x) { return __builtin_amdgcn_readlane(x, KV_WAVE - 1); }
+__device__ __forceinline__ long long kv_last(long long x) {
+  const unsigned lo = static_cast<unsigned>(kv_last(static_cast<int>(x))), hi = static_cast<unsigned>(kv_last(static_cast<int>(x >> 32)));
+  return static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
+}
+
+template <typename V>
+__device__ __forceinline__ V kv_wave_sum(V x) {
+  return kv_last(kv_wave_scan(x));
+}
+
+// Exclusive prefix sum over the workgroup's NT threads and the total; `part` is NT / 64 values
+// of LDS, which must not be written to (again) before the workgroup's next barrier.
 template <int NT, typename V>
 __device__ __forceinline__ V kv_block_scan(V x, V* part, V* total) {
-  const int wave = threadIdx.x / KV_WAVE, lane = threadIdx.x & (KV_WAVE - 1);
+  const int wave = threadIdx.x / KV_WAVE;
   const V in = kv_wave_scan(x);
-  __syncthreads();
-  if (lane == KV_WAVE - 1) part[wave] = in;
+  if ((threadIdx.x & (KV_WAVE - 1)) == KV_WAVE - 1) part[wave] = in;
   __syncthreads();
   V before = 0, all = 0;
 #pragma unroll
