@@ -41,8 +41,8 @@ constexpr int KV_PROMPT_ROWS = 128;
 // at two without 1,527.
 template <typename T>
 constexpr int kv_groups_per_cu(int dp, int r) {
-  const int own = sizeof(T) == 2 ? dp / 4 + dp / 8 : dp / 4 + dp / 4, block = dp / 2;
-  const int regs = own * r + block;
+  const int q = r > 1 ? 0 : sizeof(T) == 2 ? dp / 8 : dp / 4;  // (in LDS for more than one row tile)
+  const int regs = dp / 4 * r + q + dp / 2 + (sizeof(T) == 2 ? 16 : 32) * (r - 1);
   return regs <= 64 ? 4 : regs <= 80 ? 3 : regs <= 160 ? 2 : 1;
 }
 
@@ -328,9 +328,12 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   const int p0 = it.start + j0, p1 = it.start + j1;  // positions of the tile's tokens
   bool bad = !it.fine;
 
-  // this lane's rows
+  // this lane's rows; their queries stay in registers for one row tile, else in LDS, where every wave
+  // reads them again for each block
+  constexpr bool Q_LDS = R > 1;
+  __shared__ uint4 q_lds[Q_LDS ? R * QC : 1][KV_WAVE];
   int pos[R];
-  uint4 qf[R][QC];
+  uint4 qf[Q_LDS ? 1 : R][QC];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = 16 * r + c;
@@ -342,9 +345,15 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
 #pragma unroll
     for (int i = 0; i < QC; ++i) {
       const int d = i * (BF ? 32 : 16) + g * (BF ? 8 : 4);
-      qf[r][i] = kv_flip(d < D ? *reinterpret_cast<const uint4*>(src + d * sizeof(T)) : uint4{0, 0, 0, 0}, P.flip);
+      const uint4 x = kv_flip(d < D ? *reinterpret_cast<const uint4*>(src + d * sizeof(T)) : uint4{0, 0, 0, 0}, P.flip);
+      if constexpr (Q_LDS) {
+        if ((r * QC + i) % KV_ATT_WAVES == wave) q_lds[r * QC + i][lane] = x;
+      } else {
+        qf[r][i] = x;
+      }
     }
   }
+  if constexpr (Q_LDS) __syncthreads();
 
   f32x4 acc[R][NT];
   float m[R], l[R];
@@ -370,10 +379,12 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
     // last token: that token's); a run lies in one page, whose id is looked up once.
     auto run_of = [&](int tok) { return tok <= last ? tok & ~7 : last & ~7; };
     const int k_in = BF ? (c >> 2) * 8 : c, v_in = g * TOK;
-    int k_id = 0, v_id = 0;
+    // (page ids are looked up two blocks ahead: loads return in order, and an id behind the values of
+    // the block before would have the keys wait for those)
+    int k_id = 0, v_id = 0, k_next = 0, v_next = 0;
     auto load_ids = [&](int t0) {
-      k_id = row_pages[run_of(t0 + k_in) >> P.t.shift];
-      v_id = row_pages[run_of(t0 + v_in) >> P.t.shift];
+      k_next = row_pages[run_of(t0 + k_in) >> P.t.shift];
+      v_next = row_pages[run_of(t0 + v_in) >> P.t.shift];
     };
     auto page_at = [&](int id) {
       const bool in = id >= 0 && id < P.t.n_pages;
@@ -424,14 +435,16 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
     int i = from + wave;
     if (i < to) {
       load_ids(token_of(i));
+      k_id = k_next;
+      v_id = v_next;
       load_keys(token_of(i));
+      if (i + KV_ATT_WAVES < to) load_ids(token_of(i + KV_ATT_WAVES));
       load_values(token_of(i));
     }
     while (i < to) {
       const int t0 = token_of(i), vt0 = t0 + v_in;
       const int next = i + KV_ATT_WAVES;
       const int t_next = token_of(next);
-      if (next < to) load_ids(t_next);
       // scores
       f32x4 s[R][BF ? 2 : 1];
 #pragma unroll
@@ -441,18 +454,24 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
           f32x4 x{0, 0, 0, 0};
 #pragma unroll
           for (int e = 0; e < QC; ++e) {
+            const uint4 q = Q_LDS ? q_lds[Q_LDS ? r * QC + e : 0][lane] : qf[Q_LDS ? 0 : r][e];
             if constexpr (BF) {
               x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u][e]),
-                                                          __builtin_bit_cast(bf16x8, qf[r][e]), x, 0, 0, 0);
+                                                          __builtin_bit_cast(bf16x8, q), x, 0, 0, 0);
             } else {
-              const f32x4 a = __builtin_bit_cast(f32x4, kf[u][e]), z = __builtin_bit_cast(f32x4, qf[r][e]);
+              const f32x4 a = __builtin_bit_cast(f32x4, kf[u][e]), z = __builtin_bit_cast(f32x4, q);
 #pragma unroll
               for (int w = 0; w < 4; ++w) x = __builtin_amdgcn_mfma_f32_16x16x4f32(a[w], z[w], x, 0, 0, 0);
             }
           }
           s[r][u] = x;
         }
-      if (next < to) load_keys(t_next);
+      if (next < to) {
+        k_id = k_next;
+        v_id = v_next;
+        load_keys(t_next);
+        if (next + KV_ATT_WAVES < to) load_ids(token_of(next + KV_ATT_WAVES));
+      }
       // whole block visible to every row of the tile?
       const bool whole = t0 + BLK - 1 <= p0 && (P.window <= 0 || t0 > p1 - 1 - P.window || t0 + BLK <= P.sinks);
 #pragma unroll
@@ -461,9 +480,12 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
           kv_soften<false>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
         else
           kv_soften<true>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
-      // a value that is not finite would reach rows that do not see its token (0 times
-      // infinity): such blocks are multiplied in three parts
+      // A value that is not finite would reach rows that do not see its token (0 times infinity):
+      // in blocks where that can be, such values are taken out, and how much weight lies on
+      // +infinity or NaN, and on -infinity or NaN, is multiplied by itself.
       bool odd = false;
+      constexpr int PER_WORD = 4 / sizeof(T), MARKS = (TOK * VW * PER_WORD + 31) / 32;
+      uint32_t up[MARKS], down[MARKS];
       if (!whole) {
         bool mine = false;
 #pragma unroll
@@ -474,6 +496,23 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
             if constexpr (BF) mine |= (vr[e][w] & 0x7f80u) == 0x7f80u;
           }
         odd = __any(mine);
+        if (odd) {
+#pragma unroll
+          for (int i = 0; i < MARKS; ++i) up[i] = down[i] = 0;
+#pragma unroll
+          for (int e = 0; e < TOK; ++e)
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              const int at = (e * VW + w) * PER_WORD;
+              const uint32_t u = kv_select<T, 1>(vr[e][w]), d = kv_select<T, -1>(vr[e][w]);
+#pragma unroll
+              for (int k = 0; k < PER_WORD; ++k) {
+                up[(at + k) / 32] |= (u >> (16 * k) & 0xffffu || (PER_WORD == 1 && u) ? 1u : 0u) << (at + k) % 32;
+                down[(at + k) / 32] |= (d >> (16 * k) & 0xffffu || (PER_WORD == 1 && d) ? 1u : 0u) << (at + k) % 32;
+              }
+              vr[e][w] = kv_select<T, 0>(vr[e][w]);
+            }
+        }
       }
       bf16x8 pf[R];
       if constexpr (BF)
@@ -481,56 +520,57 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
         for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
-      // O += V^T P^T with tile t of the values, or with `f` of each of its elements
-      auto multiply = [&](int t, auto f, f32x4(&to_add)[R]) {
+      // x += V^T P^T, tile t of the values
+      auto multiply = [&](int t, f32x4(&x)[R]) {
         if constexpr (BF) {
-          uint4 a;  // element t of the lane's eight value rows
-          uint32_t w[4];
+          uint32_t w[4];  // element t of the lane's eight value rows
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            w[e] = f(__builtin_amdgcn_perm(vr[2 * e + 1][t >> 1], vr[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u));
-          __builtin_memcpy(&a, w, 16);
+            w[e] = __builtin_amdgcn_perm(vr[2 * e + 1][t >> 1], vr[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+          const bf16x8 a = __builtin_bit_cast(bf16x8, uint4{w[0], w[1], w[2], w[3]});
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-            to_add[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], to_add[r], 0, 0, 0);
+          for (int r = 0; r < R; ++r) x[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[r], x[r], 0, 0, 0);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float a = __uint_as_float(f(vr[e][t]));
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int r = 0; r < R; ++r) to_add[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[r][0][e], to_add[r], 0, 0, 0);
-          }
+            for (int r = 0; r < R; ++r)
+              x[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][t]), s[r][0][e], x[r], 0, 0, 0);
         }
       };
-      if (!odd) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          f32x4 x[R];
+      for (int t = 0; t < NT; ++t) {
+        f32x4 x[R];
 #pragma unroll
-          for (int r = 0; r < R; ++r) x[r] = acc[r][t];
-          multiply(t, [](uint32_t v) { return v; }, x);
+        for (int r = 0; r < R; ++r) x[r] = acc[r][t];
+        multiply(t, x);
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r][t] = x[r];
-        }
-      } else {
-        // the finite values as they are; then how much weight lies on values of
-        // +infinity or NaN, and of -infinity or NaN
+        for (int r = 0; r < R; ++r) acc[r][t] = x[r];
+      }
+      if (odd) {
+        constexpr uint32_t ONE = BF ? 0x3f80u : 0x3f800000u;
+#pragma unroll 1
+        for (int sign = 0; sign < 2; ++sign) {
+          const float inf = sign ? -INFINITY : INFINITY;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          f32x4 x[R], up[R], down[R];
+          for (int e = 0; e < TOK; ++e)
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            x[r] = acc[r][t];
-            up[r] = down[r] = f32x4{0, 0, 0, 0};
+            for (int w = 0; w < VW; ++w) {
+              const int at = (e * VW + w) * PER_WORD;
+              const uint32_t bits = (sign ? down[at / 32] : up[at / 32]) >> at % 32;
+              vr[e][w] = (bits & 1 ? ONE : 0u) | (PER_WORD == 2 && bits & 2 ? ONE << 16 : 0u);
+            }
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            f32x4 x[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[r] = f32x4{0, 0, 0, 0};
+            multiply(t, x);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[r][t][e] += x[r][e] > 0.0f ? inf : 0.0f;
           }
-          multiply(t, [](uint32_t v) { return kv_select<T, 0>(v); }, x);
-          multiply(t, [](uint32_t v) { return kv_select<T, 1>(v); }, up);
-          multiply(t, [](uint32_t v) { return kv_select<T, -1>(v); }, down);
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[r][t][e] = x[r][e] + (up[r][e] > 0.0f ? INFINITY : 0.0f) - (down[r][e] > 0.0f ? INFINITY : 0.0f);
         }
       }
       if (next < to) load_values(t_next);
@@ -873,7 +913,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
             acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], acc[r][t], 0, 0, 0);
         }
       } else {
-        // in three parts, as in kv_attention_kernel
+        // the finite values, and the weight on those that are not, as in kv_attention_kernel
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint4 a = values(vt, t);
