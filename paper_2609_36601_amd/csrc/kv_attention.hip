@@ -8,7 +8,7 @@ namespace {
 
 template <typename T, int DP, int ROWS>
 hipError_t launch(void (*kernel)(KvAttnParams), const KvAttnParams& P, int64_t units, bool join, hipStream_t st) {
-  constexpr int64_t ITEMS = KV_MOST_ITEMS<T, DP, ROWS>;
+  constexpr int64_t ITEMS = KV_ITEMS<T, DP, ROWS>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(units + ITEMS)), dim3(KV_ATT_NT), 0, st, P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !join) return e;

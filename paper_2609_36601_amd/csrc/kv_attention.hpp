@@ -46,15 +46,12 @@ constexpr int kv_groups_per_cu(int dp, int r) {
   return regs <= 64 ? 4 : regs <= 80 ? 3 : regs <= 160 ? 2 : 1;
 }
 
-// Items that a call with fewer units is split into: what the card takes at once, or four
-// times that where an item then still has KV_LONG_ITEM blocks, so that the last ones to
-// end are short (128 verifications of 1,800 to 7,200 keys: 505 -> 440 us).
+// Items that a call with fewer units is split into: what the card takes at once.  More, so that
+// the last ones to end are short, gives the join more to do than it saves (128 verifications of
+// 1,800 to 7,200 keys 475 -> 487 us with four times as many, of 4,100 keys each 391 -> 431).
 constexpr int KV_CUS = 256;
-constexpr int KV_LONG_ITEM = 128;
 template <typename T, int DP, int ROWS>
 constexpr int KV_ITEMS = KV_CUS * (ROWS == KV_PROMPT_ROWS ? 2 : kv_groups_per_cu<T>(DP, ROWS / 16));
-template <typename T, int DP, int ROWS>
-constexpr int KV_MOST_ITEMS = (ROWS == KV_PROMPT_ROWS ? 1 : 4) * KV_ITEMS<T, DP, ROWS>;
 
 struct KvItem;
 
@@ -151,12 +148,15 @@ __device__ __forceinline__ int kv_split_at(int blocks, int splits, int split) {
 }
 
 // Finds the workgroup's item; every workgroup derives the split from the lengths by
-// itself, which spares a launch.  Items of a sequence are ordered by tile (last first: with
-// causal rows those are the longest), split, key head, so that the workgroups of one key
-// head, which read the same keys, tend to one XCD.  False: there is no such item.
-template <int ROWS, int BLK, int ITEMS, int MOST_ITEMS>
+// itself, which spares a launch.  The sequences whose tiles are longer than the mean come
+// first, so that the last workgroups to start are short.  Items of a sequence are ordered by
+// tile (last first: with causal rows those are the longest), split, key head, so that the
+// workgroups of one key head, which read the same keys, tend to one XCD.  False: there is
+// no such item.
+template <int ROWS, int BLK, int ITEMS>
 __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out) {
   __shared__ long long part[2][KV_ATT_WAVES];
+  __shared__ int part_split[KV_ATT_WAVES];
   __shared__ KvItem found;
   __shared__ int is_found;
   const int tid = threadIdx.x;
@@ -176,35 +176,48 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
   all *= Hk;
   // (a unit's items are rounded up, by half of one on average)
   const int aim = P.units < ITEMS ? ITEMS - P.units / 2 : ITEMS;
-  const bool many = MOST_ITEMS > ITEMS && all >= static_cast<long long>(KV_LONG_ITEM) * ITEMS;
-  all = many ? (all + MOST_ITEMS - 1) / MOST_ITEMS
-             : all < (1 << 30) ? (static_cast<int>(all) + aim - 1) / aim : (all + ITEMS - 1) / ITEMS;
-  const unsigned len = all < 8 ? 8u : all < (1 << 30) ? static_cast<unsigned>(all) : 1u << 30;
-  // Sums over the sequences: items; slots of the split units' items, fewer than twice the
-  // items aimed at; split units, fewer than those (each has more blocks than an item).
-  auto sums_of = [&](const KvLoad& s, int* n) {
-    *n = static_cast<int>((static_cast<unsigned>(s.blocks) + len - 1) / len);
-    const long long units = static_cast<long long>(s.tiles) * Hk, items = units * *n;
-    return items + (*n > 1 ? (items << 32) + (units << 48) : 0);
+  const bool small = all < (1 << 30);
+  const long long share = small ? (static_cast<int>(all) + aim - 1) / aim : (all + ITEMS - 1) / ITEMS;
+  const unsigned len = share < 8 ? 8u : share < (1 << 30) ? static_cast<unsigned>(share) : 1u << 30;
+  const long long mean = small ? static_cast<int>(all) / P.units : all / P.units;
+  // Sums over the sequences: items of long ones (lower half) and of the others; slots of the
+  // split units' items, fewer than twice the items aimed at, and (upper half) split units, fewer than
+  // those (each has more blocks than an item).
+  auto splits_of = [&](const KvLoad& s) { return static_cast<int>((static_cast<unsigned>(s.blocks) + len - 1) / len); };
+  auto items_of = [&](const KvLoad& s, int n) {
+    return static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(s.tiles * Hk * n))
+                                  << (s.blocks > mean ? 0 : 32));
   };
-  int n = 0;
+  auto split_of = [&](const KvLoad& s, int n) { return n > 1 ? s.tiles * Hk * (n + (1 << 16)) : 0; };
   long long mine = 0, total = 0;
+  int mine_split = 0, total_split = 0;
   for (int b = b0; b < b1; ++b) {
     if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
-    mine += sums_of(keep, &n);
+    const int n = splits_of(keep);
+    mine += items_of(keep, n);
+    mine_split += split_of(keep, n);
   }
-  long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part[1], &total);
+  int at_split = kv_wave_scan(mine_split);
+  const int wave = tid / KV_WAVE;
+  if ((tid & (KV_WAVE - 1)) == KV_WAVE - 1) part_split[wave] = at_split;
+  const long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part[1], &total);
+  at_split -= mine_split;
+#pragma unroll
+  for (int w = 0; w < KV_ATT_WAVES; ++w) {
+    if (w < wave) at_split += part_split[w];
+    total_split += part_split[w];
+  }
   const unsigned item = blockIdx.x;
   // (the bound only matters for token ranges that overlap, whose sums may pass their fields)
-  if (item == 0 && tid == 0) *P.n_split = min(static_cast<int>(total >> 48) & 0xffff, MOST_ITEMS);
-  if (item >= static_cast<unsigned>(at) && item - static_cast<unsigned>(at) < static_cast<unsigned>(mine)) {
+  if (item == 0 && tid == 0) *P.n_split = min(total_split >> 16 & 0xffff, ITEMS);
+  unsigned from[2] = {static_cast<unsigned>(at), static_cast<unsigned>(total) + static_cast<unsigned>(at >> 32)};
+  const unsigned own[2] = {static_cast<unsigned>(mine), static_cast<unsigned>(mine >> 32)};
+  if (item - from[0] < own[0] || item - from[1] < own[1]) {
     for (int b = b0; b < b1; ++b) {
-      if (per > 1) {
-        keep = kv_load_of<ROWS, BLK>(P, b);
-        mine = sums_of(keep, &n);
-      }
-      unsigned i = item - static_cast<unsigned>(at);
-      if (i < static_cast<unsigned>(mine)) {
+      if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
+      const int n = splits_of(keep), kind = keep.blocks > mean ? 0 : 1;
+      const unsigned count = static_cast<unsigned>(keep.tiles * Hk * n), i = item - from[kind];
+      if (i < count) {
         KvItem f;
         const unsigned q = i / static_cast<unsigned>(Hk);
         f.head = static_cast<int>(i - q * Hk);
@@ -218,14 +231,15 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
         f.splits = n;
         f.b = b;
         // a unit's slots are consecutive
-        f.slot = static_cast<int>((at >> 32) & 0xffff) + (back * Hk + f.head) * n + f.split;
+        f.slot = (at_split & 0xffff) + (back * Hk + f.head) * n + f.split;
         found = f;
         is_found = 1;
-        const int unit = static_cast<int>((at >> 48) & 0xffff) + back * Hk + f.head;
-        if (n > 1 && f.split == 0 && unit >= 0 && unit < MOST_ITEMS) P.split[unit] = f;
+        const int unit = (at_split >> 16 & 0xffff) + back * Hk + f.head;
+        if (n > 1 && f.split == 0 && unit < ITEMS) P.split[unit] = f;
         break;
       }
-      at += mine;
+      from[kind] += count;
+      at_split += split_of(keep, n);
     }
   }
   __syncthreads();
@@ -318,7 +332,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   __shared__ float join_m[KV_ATT_WAVES][ROWS], join_l[KV_ATT_WAVES][ROWS];
 
   KvItem it;
-  if (!kv_find_item<ROWS, BLK, KV_ITEMS<T, DP, ROWS>, KV_MOST_ITEMS<T, DP, ROWS>>(P, &it)) return;
+  if (!kv_find_item<ROWS, BLK, KV_ITEMS<T, DP, ROWS>>(P, &it)) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;
@@ -767,7 +781,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
   constexpr int NT = DP / 16, QC = DP / 32;
   __shared__ KvPromptShared<DP> sh;
   KvItem it;
-  if (!kv_find_item<ROWS, BLK, KV_ITEMS<uint16_t, DP, ROWS>, KV_MOST_ITEMS<uint16_t, DP, ROWS>>(P, &it)) return;
+  if (!kv_find_item<ROWS, BLK, KV_ITEMS<uint16_t, DP, ROWS>>(P, &it)) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int c = lane & 15, g = lane >> 4;
   const int D = P.p.dim, G = P.group;

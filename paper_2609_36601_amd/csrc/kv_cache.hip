@@ -146,7 +146,7 @@ struct AttentionWs {
 template <typename T, int DP, int ROWS>
 AttentionWs attention_ws_of() {
   AttentionWs w{};
-  constexpr int64_t ITEMS = KV_MOST_ITEMS<T, DP, ROWS>;
+  constexpr int64_t ITEMS = KV_ITEMS<T, DP, ROWS>;
   w.split = 16;  // after their number
   w.part = w.split + up16(ITEMS * static_cast<int64_t>(sizeof(KvItem)));
   w.slots = 2 * ITEMS;
