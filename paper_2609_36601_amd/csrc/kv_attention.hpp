@@ -468,6 +468,9 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
           f32x4 x{0, 0, 0, 0};
 #pragma unroll
           for (int e = 0; e < QC; ++e) {
+            // (four products of 32 cycles each; in bf16 one of 16.  The branches also keep the loads of Q from
+            // LDS apart, all of which at once would not fit the registers)
+            if (!BF && DP <= 128 && e * 16 >= D) break;
             const uint4 q = Q_LDS ? q_lds[Q_LDS ? r * QC + e : 0][lane] : qf[Q_LDS ? 0 : r][e];
             if constexpr (BF) {
               x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u][e]),
