@@ -20,7 +20,20 @@ the law of sequential exact-q sampling (App. F, Prop. spec_exact).
     advance(states, tokens) -> states after appending the tokens
     logits_into(states, s_out, t_out)   student / teacher logits of the
                                         prefixes, written into [n, V] views
-(workloads.SyntheticARTorch is a synthetic one).
+(workloads.SyntheticARTorch is a synthetic one).  Networks that keep key-value
+caches have instead of initial, advance and logits_into
+    caches                         the networks' cache.PagedKV, B sequences each
+    start(prompts) -> last token of each prompt, int64 [B]; each cache then
+                                   holds the prompts without their last tokens
+                                   (equal prompts may share pages: PagedKV.fork)
+    draft_into(tokens, j, s_out)   student logits after tokens [B], which are
+                                   appended at position length + j of its cache
+    verify_into(tokens, t_out)     teacher logits [B * k, V] after each of tokens
+                                   [B, k], appended from position length on
+The driver then reserves the pages of a wave before it and commits the caches
+with the trajectories: the tokens behind the first rejection are dropped and
+their pages given back, and a finished sequence gives back all of its pages
+(workloads.SyntheticAttentionPair is a synthetic one).
 
 Keying: draft j of sequence b in wave w and its verification share the
 global row g = w * B * k + b * k + j, so drafts equal the proposals the
@@ -61,6 +74,9 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
     if max_len <= 0:
         traj["done"].fill_(_b.SEQ_FINISHED)
         return traj, 0
+    caches = getattr(model, "caches", ())
+    if caches and stream is not None:
+        raise ValueError("a model with caches runs on the current stream")
     # logits of the B * k draft prefixes, block-major rows b * k + j
     S = _b.alloc_rows(B * k, V, dtype, dev)
     T = _b.alloc_rows(B * k, V, dtype, dev)
@@ -76,7 +92,10 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
     corr = torch.empty(B, dtype=torch.int32, device=dev)
     n_commit = torch.empty(B, dtype=torch.int32, device=dev)
     ws = torch.empty(max(_b.workspace_bytes(_b.SAKI_OP_VERIFY, B * k, V), 8), dtype=torch.uint8, device=dev)
-    state = model.initial(prompts)
+    # what the model continues from: its state, or with caches the last token
+    state = model.start(prompts) if caches else model.initial(prompts)
+    wanting = torch.full((B,), k, dtype=torch.int32, device=dev)  # tokens of the wave
+    lacking = torch.zeros((), dtype=torch.bool, device=dev)
 
     def timed(name, fn, *a, **kw):
         if timing is None:
@@ -84,22 +103,32 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
         st = torch.cuda.current_stream() if stream is None else stream
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         e0.record(st)
-        fn(*a, **kw)
+        out = fn(*a, **kw)
         e1.record(st)
         timing.setdefault(name, []).append((e0, e1))
+        return out
 
     limit = max_waves if max_waves is not None else max_len + 1
     wave = 0
     while wave < limit:
         g0 = wave * B * k
         H[:, 0] = state
+        for c in caches:
+            lacking |= (timed("cache", c.reserve, wanting) != _b.KV_OK).any()
         for j in range(k):
-            model.logits_into(H[:, j], S3[:, j], None)
+            if caches:
+                model.draft_into(H[:, j], j, S3[:, j])
+            else:
+                model.logits_into(H[:, j], S3[:, j], None)
             timed("sample", _b.saki_sample, S3[:, j], D[j], seed, row_offset=g0 + j, row_step=k,
                   stream=stream)
-            H[:, j + 1] = model.advance(H[:, j], D[j].clamp(min=0))
+            drafted = D[j].clamp(min=0)
+            H[:, j + 1] = drafted if caches else model.advance(H[:, j], drafted)
         drafts.copy_(D.t())
-        model.logits_into(H[:, :k].reshape(-1), None, T)
+        if caches:
+            model.verify_into(H[:, :k], T)
+        else:
+            model.logits_into(H[:, :k].reshape(-1), None, T)
         timed("verify", _b.saki_spec_verify, S, T, k, drafts.view(-1), eps, seed, row_offset=g0,
               eos_id=eos_id, accepted_len=acc, correction=corr, per_pos=pp, workspace=ws, stream=stream)
         if timing is not None:
@@ -107,12 +136,23 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
         timed("commit", _b.saki_commit, traj, max_len, k, eos_id, acc, corr, pp, n_commit,
               stream=stream)
         # the model continues from the committed prefix: the draft state after
-        # m - 1 drafts, advanced by the last committed token (rollback of the rest)
+        # m - 1 drafts, advanced by the last committed token (rollback of the rest);
+        # a cache holds the prefix without that token
         m = n_commit.long()
-        prev = H.gather(1, (m - 1).clamp(min=0)[:, None])[:, 0]
-        last = traj["tokens"].gather(1, (traj["length"].long() - 1).clamp(min=0)[:, None])[:, 0]
-        state = torch.where(m > 0, model.advance(prev, last.long()), state)
+        last = traj["tokens"].gather(1, (traj["length"].long() - 1).clamp(min=0)[:, None])[:, 0].long()
+        if caches:
+            for c in caches:
+                timed("cache", c.commit, n_commit, done=traj["done"])
+            wanting = torch.where(traj["done"] == _b.SEQ_RUNNING, k, 0).to(torch.int32)
+            state = torch.where(m > 0, last, state)
+        else:
+            prev = H.gather(1, (m - 1).clamp(min=0)[:, None])[:, 0]
+            state = torch.where(m > 0, model.advance(prev, last), state)
         wave += 1
-        if wave % check_every == 0 and not bool((traj["done"] == _b.SEQ_RUNNING).any()):
-            break
+        if wave % check_every == 0 or wave == limit:
+            running, short = torch.stack([(traj["done"] == _b.SEQ_RUNNING).any(), lacking]).tolist()
+            if short:
+                raise RuntimeError("a cache has too few pages for the rollout, or too few per sequence")
+            if not running:
+                break
     return traj, wave

@@ -251,3 +251,99 @@ class SyntheticARTorch:
         if t_out is not None:
             lo = a & 0xFFFFFFFF
             t_out.copy_(s / 2.0 + ((lo % 17) - 8).to(torch.float32) / 4.0)
+
+
+# ---------------------------------------------------------------------------
+# A synthetic pair of networks with key-value caches: a few layers of causal
+# attention with rotary positions (no feed-forward part) between an embedding
+# and logits, random weights.  Stands in for the rollout engine's student and teacher
+# where the caches matter.  Prompt p has 1 + mix(p) % most_prompt tokens, token i of it
+# mix(p ^ (i + 1) * K1) % V.
+# ---------------------------------------------------------------------------
+class SyntheticAttentionPair:
+    """`caches` holds the student's and the teacher's PagedKV (see speculative.rollout); sequences whose
+    prompts are equal share the first one's pages."""
+
+    def __init__(self, V, n_seq, max_pages, n_pages, page_size=16, layers=2, heads=4, kv_heads=2, head_dim=16,
+                 width=64, most_prompt=40, windows=(0, 0), sinks=0, dtype=torch.float32, seed=0, device="cuda"):
+        from .cache import PagedKV, rope
+        self.V, self.device, self.dtype, self.layers = int(V), device, dtype, layers
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.most_prompt, self.windows, self.sinks = most_prompt, windows, sinks
+        self.caches = tuple(PagedKV.alloc(n_seq, max_pages, n_pages, layers, kv_heads, page_size, head_dim, dtype, device)
+                            for _ in range(2))
+        self.rope = rope(head_dim, device=device)
+        g = torch.Generator().manual_seed(0xCA5E + seed)
+        rows = (heads + 2 * kv_heads) * head_dim
+
+        def weight(*shape):
+            return (torch.randn(*shape, generator=g) * shape[0] ** -0.5).to(device=device, dtype=dtype)
+
+        # the teacher is the student, moved
+        student = dict(embed=torch.randn(self.V, width, generator=g).to(device=device, dtype=dtype),
+                       qkv=[weight(width, rows) * 1.5 for _ in range(layers)],
+                       out=[weight(heads * head_dim, width) for _ in range(layers)], logits=weight(width, self.V) * 2.0)
+        moved = lambda w: w + 0.2 * (torch.randn(w.shape, generator=g) * w.shape[0] ** -0.5).to(device=device, dtype=dtype)  # noqa: E731
+        teacher = dict(embed=student["embed"], qkv=[moved(w) for w in student["qkv"]], out=[moved(w) for w in student["out"]],
+                       logits=moved(student["logits"]))
+        self.weights = (student, teacher)
+
+    def prompt(self, p):
+        """The token ids of prompt p."""
+        import numpy as np
+        n = 1 + int(_mix(p)) % self.most_prompt
+        with np.errstate(over="ignore"):
+            return (_mix(np.uint64(p) ^ (np.arange(1, n + 1, dtype=np.uint64) * np.uint64(_K1))) % np.uint64(self.V)).astype(np.int64)
+
+    def _hidden(self, net, tokens, attend):
+        """Hidden rows behind the last layer; attend(layer, q, k, v) -> the attention's output."""
+        w, D = self.weights[net], self.head_dim
+        h = w["embed"][tokens]
+        for i in range(self.layers):
+            x = (_unit(h) @ w["qkv"][i]).view(-1, self.heads + 2 * self.kv_heads, D)
+            q, k, v = x.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
+            h = h + attend(i, q, k, v).reshape(-1, self.heads * D) @ w["out"][i]
+        return _unit(h)
+
+    def _cached(self, net, tokens, **rows):
+        c = self.caches[net]
+
+        def attend(i, q, k, v):
+            return c.attention(i, c.append(i, k, v, q=q, rope=self.rope, **rows), window=self.windows[net],
+                               sinks=self.sinks, **rows)
+
+        return self._hidden(net, tokens, attend)
+
+    def start(self, prompts):
+        """Empties the caches and fills them with the prompts, but for their last tokens."""
+        ids = [int(p) for p in prompts]
+        text = [self.prompt(p) for p in ids]
+        firsts = {}
+        for b, p in enumerate(ids):
+            firsts.setdefault(p, b)
+        n = [len(text[b]) - 1 if firsts[ids[b]] == b else 0 for b in range(len(ids))]
+        i32 = dict(dtype=torch.int32, device=self.device)
+        new = torch.tensor(n, **i32)
+        offsets = torch.nn.functional.pad(new.cumsum(0), (1, 0)).to(torch.int32)
+        tokens = torch.tensor([t for b in range(len(ids)) for t in text[b][:n[b]]], dtype=torch.int64, device=self.device)
+        others = [b for b in range(len(ids)) if firsts[ids[b]] != b]
+        for net, c in enumerate(self.caches):
+            c.commit(done=torch.ones(c.n_seq, dtype=torch.uint8, device=self.device))
+            if bool((c.reserve(new) != 0).any()):
+                raise RuntimeError("a cache has too few pages for the prompts")
+            self._cached(net, tokens, offsets=offsets)
+            c.commit(new)
+            if others:
+                c.fork(torch.tensor([firsts[ids[b]] for b in others], **i32), torch.tensor(others, **i32))
+        return torch.tensor([int(t[-1]) for t in text], dtype=torch.int64, device=self.device)
+
+    def draft_into(self, tokens, j, s_out):
+        s_out.copy_(self._cached(0, tokens, n_new=1, shift=j) @ self.weights[0]["logits"])
+
+    def verify_into(self, tokens, t_out):
+        t_out.copy_(self._cached(1, tokens.reshape(-1), n_new=tokens.shape[1]) @ self.weights[1]["logits"])
+
+
+def _unit(h):
+    """Rows of root mean square 1."""
+    return h * torch.rsqrt(h.float().square().mean(-1, keepdim=True) + 1e-6).to(h.dtype)
