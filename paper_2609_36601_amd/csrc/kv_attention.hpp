@@ -267,28 +267,32 @@ __device__ __forceinline__ uint32_t kv_select(uint32_t v) {
   return one(v & 0xffffu) | one(v >> 16) << 16;
 }
 
+template <int SIGN>
+__device__ __forceinline__ uint4 kv_part(uint4 v) {
+  return uint4{kv_select<uint16_t, SIGN>(v.x), kv_select<uint16_t, SIGN>(v.y), kv_select<uint16_t, SIGN>(v.z),
+               kv_select<uint16_t, SIGN>(v.w)};
+}
+
 __device__ __forceinline__ uint4 kv_flip(uint4 x, uint32_t f) { return uint4{x.x ^ f, x.y ^ f, x.z ^ f, x.w ^ f}; }
 
-// Scores of a row (a lane's 4 U of a block; those of u belong to tokens tok + 32 (u / 2) +
-// 4 (u % 2) ..) to weights relative to the running maximum m, with l their sum; where the
-// maximum moves, O and l are scaled.  scale2 >= 0.  MASKED: some row does not see some token.
-template <bool MASKED, int U, int NT>
-__device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float* m, float* l, float scale2, int tok,
-                                          int pos, int window, int sinks) {
+// Hides the scores (a lane's 4 U of a block, of tokens tok + 4 u + e) that the row at `pos` does not see.
+template <int U>
+__device__ __forceinline__ void kv_mask(f32x4 (&s)[U], int tok, int pos, int window, int sinks) {
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = tok + 4 * u + e;
+      const bool seen = t <= pos && (window <= 0 || t > pos - window || t < sinks);
+      s[u][e] = seen ? s[u][e] : -INFINITY;
+    }
+}
+
+// Scores of a row to weights relative to the running maximum m, with l their sum; where the
+// maximum moves, O and l are scaled.  scale2 > 0.
+template <int U, int NT>
+__device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float* m, float* l, float scale2) {
   float top = -INFINITY;
-  uint32_t seen = 0xffffffffu;
-  if constexpr (MASKED) {
-    seen = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = tok + 32 * (u >> 1) + 4 * (u & 1) + e;
-        const bool yes = t <= pos && (window <= 0 || t > pos - window || t < sinks);
-        seen |= static_cast<uint32_t>(yes) << (4 * u + e);
-        s[u][e] = yes ? s[u][e] : -INFINITY;
-      }
-  }
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -308,9 +312,7 @@ __device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale2, -ref));
-      // (a hidden score is -infinity, which a scale of 0 would make a NaN)
-      if constexpr (MASKED) x = (seen >> (4 * u + e)) & 1 ? x : 0.0f;
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale2, -ref));
       s[u][e] = x;
       *l += x;
     }
@@ -491,12 +493,12 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       }
       // whole block visible to every row of the tile?
       const bool whole = t0 + BLK - 1 <= p0 && (P.window <= 0 || t0 > p1 - 1 - P.window || t0 + BLK <= P.sinks);
+      if (!whole)
+#pragma unroll
+        for (int r = 0; r < R; ++r) kv_mask(s[r], vt0, pos[r], P.window, P.sinks);
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        if (whole)
-          kv_soften<false>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
-        else
-          kv_soften<true>(s[r], acc[r], &m[r], &l[r], P.scale2, vt0, pos[r], P.window, P.sinks);
+        kv_soften(s[r], acc[r], &m[r], &l[r], P.scale2);
       // A value that is not finite would reach rows that do not see its token (0 times infinity):
       // in blocks where that can be, such values are taken out, and how much weight lies on
       // +infinity or NaN, and on -infinity or NaN, is multiplied by itself.
@@ -886,8 +888,8 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
       return r;
     };
     // the 32 tokens from t0 on, whose keys and values start at kt and vt
-    auto multiply = [&](auto masked, const uint16_t* kt, const uint16_t* vt, int t0) {
-      constexpr bool MASKED = decltype(masked)::value;
+    auto multiply = [&](const uint16_t* kt, const uint16_t* vt, int t0) {
+      const bool whole = whole_for(t0, 32, wp0, wp1);
       f32x4 s[R][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -903,53 +905,48 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
             s[r][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[e]),
                                                               __builtin_bit_cast(bf16x8, qf[r][e]), s[r][u], 0, 0, 0);
       }
-      bf16x8 pf[R];
+      // (the values' reads are under way while the weights are computed)
+      uint4 a[NT];
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        kv_soften<MASKED>(s[r], acc[r], &m[r], &l[r], P.scale2, t0 + g * 8, pos[r], P.window, P.sinks);
+      for (int t = 0; t < NT; ++t) a[t] = values(vt, t);
+      bool odd = false;  // as in kv_attention_kernel
+      if (!whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
-      }
-      bool odd = false;
-      if constexpr (MASKED) {
+        for (int r = 0; r < R; ++r) kv_mask(s[r], t0 + g * 8, pos[r], P.window, P.sinks);
         bool mine = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const uint4 a = values(vt, t);
           auto nonfinite = [](uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; };
-          mine |= nonfinite(a.x) || nonfinite(a.y) || nonfinite(a.z) || nonfinite(a.w);
+          mine |= nonfinite(a[t].x) || nonfinite(a[t].y) || nonfinite(a[t].z) || nonfinite(a[t].w);
         }
         odd = __any(mine);
+        if (odd)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) a[t] = kv_part<0>(a[t]);
       }
-      if (!odd) {
+      bf16x8 pf[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        kv_soften(s[r], acc[r], &m[r], &l[r], P.scale2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[t]), pf[r], acc[r][t], 0, 0, 0);
+      if (odd) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const uint4 a = values(vt, t);
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[r], acc[r][t], 0, 0, 0);
-        }
-      } else {
-        // the finite values, and the weight on those that are not, as in kv_attention_kernel
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const uint4 a = values(vt, t);
-          auto part = [&](auto sign) {
-            constexpr int SIGN = decltype(sign)::value;
-            return __builtin_bit_cast(bf16x8, uint4{kv_select<uint16_t, SIGN>(a.x), kv_select<uint16_t, SIGN>(a.y),
-                                                    kv_select<uint16_t, SIGN>(a.z), kv_select<uint16_t, SIGN>(a.w)});
-          };
-          const bf16x8 fin = part(std::integral_constant<int, 0>{}), up = part(std::integral_constant<int, 1>{}),
-                       down = part(std::integral_constant<int, -1>{});
+          const uint4 x = values(vt, t), up = kv_part<1>(x), down = kv_part<-1>(x);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const f32x4 zero{0, 0, 0, 0};
-            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fin, pf[r], acc[r][t], 0, 0, 0);
-            const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, pf[r], zero, 0, 0, 0);
-            const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, pf[r], zero, 0, 0, 0);
+            const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, up), pf[r], zero, 0, 0, 0);
+            const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, down), pf[r], zero, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[r][t][e] = x[e] + (y[e] > 0.0f ? INFINITY : 0.0f) - (z[e] > 0.0f ? INFINITY : 0.0f);
+            for (int e = 0; e < 4; ++e) acc[r][t][e] += (y[e] > 0.0f ? INFINITY : 0.0f) - (z[e] > 0.0f ? INFINITY : 0.0f);
           }
         }
       }
@@ -975,10 +972,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 #pragma unroll 1
         for (int h = 0; h < BLK && t0 + h <= wp1; h += 32) {
           const uint16_t *kt = &sh.k[buf][h * DP], *vt = &sh.v[buf][h * DP];
-          if (whole_for(t0 + h, 32, wp0, wp1))
-            multiply(std::false_type{}, kt, vt, t0 + h);
-          else
-            multiply(std::true_type{}, kt, vt, t0 + h);
+          multiply(kt, vt, t0 + h);
         }
       }
       kv_lds_wait();
