@@ -769,11 +769,17 @@ __device__ __forceinline__ int kv_swizzle(int row) {
   return DP == 128 ? f : f >> 1;  // (two rows of 64 elements fill the banks)
 }
 
-// 16 bytes a lane from memory to LDS at `lds` + 16 lane.  Nothing waits for them but
+// 16 bytes a lane from memory at `from` + lane_offset to LDS at `lds` + 16 lane.  Nothing waits for them but
 // kv_lds_wait (the compiler, which is not told, would have every LDS read wait); they
 // write no register.
-__device__ __forceinline__ void kv_to_lds(uint32_t lds, const char* from) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+// (m0, which holds the LDS address, is read by nothing else in these kernels.)
+__device__ __forceinline__ void kv_to_lds(uint32_t lds, const char* from, uint32_t lane_offset) {
+  // the base is the same for the wave, which the compiler does not always see
+  const uint64_t f = reinterpret_cast<uint64_t>(from);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f)),
+                 hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f >> 32));
+  const uint64_t base = static_cast<uint64_t>(hi) << 32 | lo;
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void kv_lds_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -837,32 +843,37 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
       bad |= !in;
       return static_cast<int64_t>(in ? id : 0) * P.p.page_stride;
     };
-    // A wave's share of 64 tokens: J times 64 pieces of keys and of values, whole rows
+    // A wave's share of 64 tokens: 16 of them, J times RPI whole rows of keys and of values.  RPI tokens lie
+    // in one page, so a transfer's base is the same for the wave, and a lane's offset from it the same for
+    // every block: a block costs a lookup (lane j: of transfer j) and scalar arithmetic
     constexpr int PIECES = DP / 8, J = DP / 32, RPI = 64 / PIECES;
     const uint32_t lds_k = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
                        (__attribute__((address_space(3))) uint16_t*)&sh.k[0][0])),
                    lds_v = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
                        (__attribute__((address_space(3))) uint16_t*)&sh.v[0][0]));
-    int row_of[J], id_of[J];
+    const int row_in = lane / PIECES;
+    int piece[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) row_of[j] = (wave * J + j) * RPI + lane / PIECES;
-    auto load_ids = [&](int t0) {
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const int tok = t0 + row_of[j] < last ? t0 + row_of[j] : last;
-        id_of[j] = row_pages[tok >> P.t.shift];
-      }
+    for (int j = 0; j < J; ++j) piece[j] = lane % PIECES ^ kv_swizzle<DP>(wave * 16 + j * RPI + row_in);
+    // first token of transfer j (behind the last token: the run of rows that holds that one)
+    auto run_of = [&](int t0, int j) {
+      const int tok = t0 + wave * 16 + j * RPI;
+      return tok <= last ? tok : last & ~(RPI - 1);
     };
-    auto load_tokens = [&](int buf, int t0) {
+    int ids = 0;
+    auto load_ids = [&](int t0) __attribute__((always_inline)) { ids = row_pages[run_of(t0, lane % J) >> P.t.shift]; };
+    auto load_tokens = [&](int buf, int t0) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const int tok = t0 + row_of[j] < last ? t0 + row_of[j] : last;
-        const int piece = lane % PIECES ^ kv_swizzle<DP>(row_of[j]);
-        const int64_t at = page_at(id_of[j]) + static_cast<int64_t>(tok & mask) * token_stride + piece * 16;
+        const int id = __builtin_amdgcn_readlane(ids, j), run = run_of(t0, j);
+        const int64_t at = page_at(id) + static_cast<int64_t>(run & mask) * token_stride;
         const uint32_t to = buf * 64 * DP * 2 + (wave * J + j) * 1024;
-        if (piece * 8 < D) {
-          kv_to_lds(lds_k + to, kb + at);
-          kv_to_lds(lds_v + to, vb + at);
+        // (no row behind the last token is read)
+        const int row = t0 + BLK - 1 <= last || row_in < last - run ? row_in : last - run;
+        const uint32_t off = static_cast<uint32_t>(row) * token_stride + piece[j] * 16;
+        if (D == DP || piece[j] * 8 < D) {
+          kv_to_lds(lds_k + to, kb + at, off);
+          kv_to_lds(lds_v + to, vb + at, off);
         }
       }
     };
@@ -873,13 +884,14 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     // this lane's places in 32 tokens: of the keys' row 8 (c / 4) + c % 4 (+ 4 u) piece 4 e + g, and of the
     // values' row 8 g + c / 4 (+ 4 q) elements 16 t + 4 (c % 4) on
     const int k_row = (c >> 2) * 8 + (c & 3), v_row = g * 8 + (c >> 2);
-    int k_at[QC];
+    int k_at[QC], v_at[NT];
 #pragma unroll
     for (int e = 0; e < QC; ++e) k_at[e] = k_row * DP + ((4 * e + g) ^ kv_swizzle<DP>(k_row)) * 8;
-    const int v_at = v_row * DP + ((c >> 1 & 1) ^ kv_swizzle<DP>(v_row)) * 8 + (c & 1) * 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) v_at[t] = v_row * DP + ((2 * t + (c >> 1 & 1)) ^ kv_swizzle<DP>(v_row)) * 8 + (c & 1) * 4;
     // element 16 t + c of tokens 8 g .. 8 g + 7
-    auto values = [&](const uint16_t* base, int t) {
-      const uint16_t* at = base + (v_at ^ (16 * t));
+    auto values = [&](const uint16_t* base, int t) __attribute__((always_inline)) {
+      const uint16_t* at = base + v_at[t];
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * DP));
       uint4 r;
@@ -888,7 +900,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
       return r;
     };
     // the 32 tokens from t0 on, whose keys and values start at kt and vt
-    auto multiply = [&](const uint16_t* kt, const uint16_t* vt, int t0) {
+    auto multiply = [&](const uint16_t* kt, const uint16_t* vt, int t0) __attribute__((always_inline)) {
       const bool whole = whole_for(t0, 32, wp0, wp1);
       f32x4 s[R][2];
 #pragma unroll
@@ -955,7 +967,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
       for (int e = tid; e < 2 * 64 * DP / 8; e += KV_ATT_NT) reinterpret_cast<uint4*>(&sh.k[0][0])[e] = uint4{0, 0, 0, 0};
       __syncthreads();
     }
-    int i = from, buf = 0;
+    int i = from;
     if (i < to) {
       load_ids(token_of(i));
       load_tokens(0, token_of(i));
@@ -963,20 +975,25 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     }
     kv_lds_wait();
     __syncthreads();
-    for (; i < to; ++i, buf ^= 1) {
+    // block i, in buffer BUF
+    auto step = [&](auto buf) __attribute__((always_inline)) {
+      constexpr int BUF = decltype(buf)::value;
       const int t0 = token_of(i);
       // (the other buffer was read before the last barrier)
-      if (i + 1 < to) load_tokens(buf ^ 1, token_of(i + 1));
+      if (i + 1 < to) load_tokens(BUF ^ 1, token_of(i + 1));
       if (i + 2 < to) load_ids(token_of(i + 2));
       if (!idle) {
-#pragma unroll 1
-        for (int h = 0; h < BLK && t0 + h <= wp1; h += 32) {
-          const uint16_t *kt = &sh.k[buf][h * DP], *vt = &sh.v[buf][h * DP];
-          multiply(kt, vt, t0 + h);
-        }
+        if (t0 <= wp1) multiply(&sh.k[BUF][0], &sh.v[BUF][0], t0);
+        if (t0 + 32 <= wp1) multiply(&sh.k[BUF][32 * DP], &sh.v[BUF][32 * DP], t0 + 32);
       }
       kv_lds_wait();
       __syncthreads();
+    };
+    while (i < to) {
+      step(std::integral_constant<int, 0>{});
+      if (++i >= to) break;
+      step(std::integral_constant<int, 1>{});
+      ++i;
     }
   }
 
