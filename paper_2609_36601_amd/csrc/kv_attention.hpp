@@ -68,7 +68,9 @@ struct KvAttnParams {
   float* part;     // [slots][rows][DP] partial sums, then
   float* part_ml;  // [slots][rows][2] their maximum and sum
   int slots;
-  int units;              // no more units than this
+  float share;     // blocks an item takes, of each block of the sequences' tiles
+  float per_tile;  // 1 / tiles of the sequences
+  int span;        // tokens that a tile's rows span at most
   int* n_split;           // how many units are split, and which: for kv_join_kernel
   KvItem* split;   // [items]
 };
@@ -96,7 +98,7 @@ __device__ __forceinline__ KvSpan kv_span(int64_t p0, int64_t p1, int window, in
 // A sequence's share of the call: its tiles, and the blocks of its largest tile.
 struct KvLoad {
   int first, count;  // token rows
-  int64_t start;     // position of the first
+  int start;         // position of the first
   int tiles;
   int blocks;
   bool fine;
@@ -105,19 +107,20 @@ template <int ROWS, int BLK>
 __device__ __forceinline__ KvLoad kv_load_of(const KvAttnParams& P, int b) {
   KvLoad s;
   kv_rows(P.n, b, &s.first, &s.count);
-  s.start = static_cast<int64_t>(P.t.length[b]) + P.n.shift;
-  s.tiles = static_cast<int>((static_cast<int64_t>(s.count) * P.group + ROWS - 1) / ROWS);
-  const int64_t end = s.start + s.count;
-  s.fine = P.t.length[b] >= 0 && end <= (static_cast<int64_t>(kv_held(P.t, b)) << P.t.shift);
+  const int L = P.t.length[b], held = kv_held(P.t, b);
+  // (the host has seen to it that all rows together are fewer than 2^31)
+  s.tiles = (s.count * P.group + ROWS - 1) / ROWS;
+  const int64_t end = static_cast<int64_t>(L) + P.n.shift + s.count;
+  s.fine = L >= 0 && end <= (static_cast<int64_t>(held) << P.t.shift);
+  s.start = L + P.n.shift;
   s.blocks = 1;
   if (s.fine && s.count > 0) {
     if (P.window > 0) {
-      // the widest tile: at most ROWS rows, which span so many tokens
-      const int span = s.count < (ROWS + P.group - 2) / P.group + 1 ? s.count : (ROWS + P.group - 2) / P.group + 1;
-      const KvSpan a = kv_span<BLK>(end - span, end, P.window, P.sinks);
-      s.blocks = a.blocks + (span < s.count ? 1 : 0);
+      // the widest tile: P.span tokens at most, which may begin anywhere in a block
+      const int span = s.count < P.span ? s.count : P.span;
+      s.blocks = kv_span<BLK>(end - span, end, P.window, P.sinks).blocks + (span < s.count ? 1 : 0);
     } else {
-      s.blocks = static_cast<int>((end + BLK - 1) / BLK);
+      s.blocks = (static_cast<int>(end) + BLK - 1) / BLK;
     }
   }
   return s;
@@ -152,94 +155,102 @@ __device__ __forceinline__ int kv_split_at(int blocks, int splits, int split) {
 // first, so that the last workgroups to start are short.  Items of a sequence are ordered by
 // tile (last first: with causal rows those are the longest), split, key head, so that the
 // workgroups of one key head, which read the same keys, tend to one XCD.  False: there is
-// no such item.
+// no such item.  Every workgroup pays for this before it begins: sums in 32 bits, no divisions but
+// in the one thread that holds the item (3 us of a workgroup's 10 with 64-bit sums and divisions).
 template <int ROWS, int BLK, int ITEMS>
 __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out) {
-  __shared__ long long part[2][KV_ATT_WAVES];
-  __shared__ int part_split[KV_ATT_WAVES];
+  __shared__ int part_blocks[KV_ATT_WAVES];
+  __shared__ int4 part[KV_ATT_WAVES];
   __shared__ KvItem found;
   __shared__ int is_found;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, wave = tid / KV_WAVE;
+  const bool last_lane = (tid & (KV_WAVE - 1)) == KV_WAVE - 1;
   const int Hk = P.p.n_heads;
   const int per = (P.t.n_seq + KV_ATT_NT - 1) / KV_ATT_NT;
   const int b0 = tid * per, b1 = b0 + per < P.t.n_seq ? b0 + per : P.t.n_seq;
   if (tid == 0) is_found = 0;
+  // all blocks; 2^22 a thread stands for more than can be counted (then nothing is split)
   long long blocks = 0;
   KvLoad keep;  // the thread's only sequence where it has one
   for (int b = b0; b < b1; ++b) {
     keep = kv_load_of<ROWS, BLK>(P, b);
     blocks += static_cast<long long>(keep.tiles) * keep.blocks;
   }
-  // blocks an item takes: what gives the call its number of items, and at least 8
-  long long all = 0;
-  kv_block_scan<KV_ATT_NT, long long>(blocks, part[0], &all);
-  all *= Hk;
-  // (a unit's items are rounded up, by half of one on average)
-  const int aim = P.units < ITEMS ? ITEMS - P.units / 2 : ITEMS;
-  const bool small = all < (1 << 30);
-  const long long share = small ? (static_cast<int>(all) + aim - 1) / aim : (all + ITEMS - 1) / ITEMS;
-  const unsigned len = share < 8 ? 8u : share < (1 << 30) ? static_cast<unsigned>(share) : 1u << 30;
-  const long long mean = small ? static_cast<int>(all) / P.units : all / P.units;
-  // Sums over the sequences: items of long ones (lower half) and of the others; slots of the
-  // split units' items, fewer than twice the items aimed at, and (upper half) split units, fewer than
-  // those (each has more blocks than an item).
-  auto splits_of = [&](const KvLoad& s) { return static_cast<int>((static_cast<unsigned>(s.blocks) + len - 1) / len); };
-  auto items_of = [&](const KvLoad& s, int n) {
-    return static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(s.tiles * Hk * n))
-                                  << (s.blocks > mean ? 0 : 32));
-  };
-  auto split_of = [&](const KvLoad& s, int n) { return n > 1 ? s.tiles * Hk * (n + (1 << 16)) : 0; };
-  long long mine = 0, total = 0;
-  int mine_split = 0, total_split = 0;
-  for (int b = b0; b < b1; ++b) {
-    if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
-    const int n = splits_of(keep);
-    mine += items_of(keep, n);
-    mine_split += split_of(keep, n);
-  }
-  int at_split = kv_wave_scan(mine_split);
-  const int wave = tid / KV_WAVE;
-  if ((tid & (KV_WAVE - 1)) == KV_WAVE - 1) part_split[wave] = at_split;
-  const long long at = kv_block_scan<KV_ATT_NT, long long>(mine, part[1], &total);
-  at_split -= mine_split;
+  const int sum = kv_wave_scan(static_cast<int>(blocks < (1 << 22) ? blocks : 1 << 22));
+  if (last_lane) part_blocks[wave] = sum;
+  __syncthreads();
+  int all = 0;
+  bool many = false;
 #pragma unroll
   for (int w = 0; w < KV_ATT_WAVES; ++w) {
-    if (w < wave) at_split += part_split[w];
-    total_split += part_split[w];
+    all += part_blocks[w];
+    many |= part_blocks[w] >= 1 << 22;
   }
-  const unsigned item = blockIdx.x;
+  // blocks an item takes: its share (rounded up, and at least 8)
+  int len = static_cast<int>(static_cast<float>(all) * P.share) + 1;
+  len = many ? 1 << 30 : len < 8 ? 8 : len;
+  const int mean = static_cast<int>(static_cast<float>(all) * P.per_tile);
+  const float inv = 1.0f / static_cast<float>(len);
+  auto splits_of = [&](const KvLoad& s) {
+    int n = static_cast<int>(static_cast<float>(s.blocks) * inv);  // exact but for one
+    n = n < 1 ? 1 : n;
+    n += n * len < s.blocks;
+    return n - ((n - 1) * len >= s.blocks);
+  };
+  // Sums over the sequences: items of long ones and of the others; slots of the split units'
+  // items, fewer than twice the items aimed at, and (upper half) split units, fewer than
+  // those (each has more blocks than an item).
+  auto add = [&](const KvLoad& s, int4* x) {
+    const int n = splits_of(s), units = s.tiles * Hk;
+    (s.blocks > mean ? x->x : x->y) += units * n;
+    x->z += n > 1 ? units * (n + (1 << 16)) : 0;
+  };
+  int4 mine{0, 0, 0, 0};
+  for (int b = b0; b < b1; ++b) {
+    if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
+    add(keep, &mine);
+  }
+  int4 at{kv_wave_scan(mine.x), kv_wave_scan(mine.y), kv_wave_scan(mine.z), 0};
+  if (last_lane) part[wave] = at;
+  at.x -= mine.x, at.y -= mine.y, at.z -= mine.z;
+  __syncthreads();
+  int4 total{0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < KV_ATT_WAVES; ++w) {
+    const int4 p = part[w];
+    if (w < wave) at.x += p.x, at.y += p.y, at.z += p.z;
+    total.x += p.x, total.z += p.z;
+  }
+  at.y += total.x;
+  const int item = static_cast<int>(blockIdx.x);
   // (the bound only matters for token ranges that overlap, whose sums may pass their fields)
-  if (item == 0 && tid == 0) *P.n_split = min(total_split >> 16 & 0xffff, ITEMS);
-  unsigned from[2] = {static_cast<unsigned>(at), static_cast<unsigned>(total) + static_cast<unsigned>(at >> 32)};
-  const unsigned own[2] = {static_cast<unsigned>(mine), static_cast<unsigned>(mine >> 32)};
-  if (item - from[0] < own[0] || item - from[1] < own[1]) {
+  if (item == 0 && tid == 0) *P.n_split = min(total.z >> 16 & 0xffff, ITEMS);
+  if ((item >= at.x && item < at.x + mine.x) || (item >= at.y && item < at.y + mine.y)) {
     for (int b = b0; b < b1; ++b) {
       if (per > 1) keep = kv_load_of<ROWS, BLK>(P, b);
-      const int n = splits_of(keep), kind = keep.blocks > mean ? 0 : 1;
-      const unsigned count = static_cast<unsigned>(keep.tiles * Hk * n), i = item - from[kind];
-      if (i < count) {
+      const int n = splits_of(keep), i = item - (keep.blocks > mean ? at.x : at.y);
+      if (i >= 0 && i < keep.tiles * Hk * n) {
         KvItem f;
-        const unsigned q = i / static_cast<unsigned>(Hk);
-        f.head = static_cast<int>(i - q * Hk);
-        const int back = static_cast<int>(q / static_cast<unsigned>(n));
-        f.split = static_cast<int>(q) - back * n;
+        const int q = i / Hk;
+        f.head = i - q * Hk;
+        const int back = n == 1 ? q : q / n;
+        f.split = q - back * n;
         f.tile = keep.tiles - 1 - back;
         f.first = keep.first;
         f.count = keep.count;
-        f.start = static_cast<int>(keep.start);
+        f.start = keep.start;
         f.fine = keep.fine;
         f.splits = n;
         f.b = b;
         // a unit's slots are consecutive
-        f.slot = (at_split & 0xffff) + (back * Hk + f.head) * n + f.split;
+        f.slot = (at.z & 0xffff) + (back * Hk + f.head) * n + f.split;
         found = f;
         is_found = 1;
-        const int unit = (at_split >> 16 & 0xffff) + back * Hk + f.head;
+        const int unit = (at.z >> 16 & 0xffff) + back * Hk + f.head;
         if (n > 1 && f.split == 0 && unit < ITEMS) P.split[unit] = f;
         break;
       }
-      from[kind] += count;
-      at_split += split_of(keep, n);
+      add(keep, &at);
     }
   }
   __syncthreads();

@@ -454,7 +454,7 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;
-  if (units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  if (n * group > INT32_MAX || units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
   KvAttnParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);
@@ -477,7 +477,14 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.part = reinterpret_cast<float*>(w + at.part);
   P.part_ml = reinterpret_cast<float*>(w + at.part_ml);
   P.slots = static_cast<int>(at.slots);
-  P.units = static_cast<int>(units);
+  // An item's share of the blocks of all units; a unit's items are rounded up, by half of one on
+  // average, which calls of few units have to leave room for.  (A little more than that: the
+  // slots are counted on no item being smaller.)
+  const int items = static_cast<int>(at.slots / 2);
+  const double aim = units < items ? items - static_cast<double>(units) / 2 : items;
+  P.share = static_cast<float>(pool->n_kv_heads / aim * 1.00001);
+  P.per_tile = static_cast<float>(static_cast<double>(pool->n_kv_heads) / static_cast<double>(units));
+  P.span = (rows + group - 2) / group + 1;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   // without more than 8 blocks of keys in any sequence nothing is split
   const bool join = table->max_pages * table->page_size > 8 * (bf ? 32 : 16);
