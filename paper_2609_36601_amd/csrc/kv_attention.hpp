@@ -329,6 +329,19 @@ __device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float
     }
 }
 
+// N elements o[i] * f of a row, of which those below `left` are there (a multiple of 8).
+template <typename T, int N>
+__device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float f, int left) {
+#pragma unroll
+  for (int t = 0; t < N; t += 4)
+    if (t < left) {
+      T y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) kv_put(&y[e], o[t + e] * f);
+      __builtin_memcpy(__builtin_assume_aligned(dst + t, 4 * sizeof(T)), y, sizeof(y));
+    }
+}
+
 // One item: ROWS = 16 R rows, the blocks of its split dealt to the four waves.
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_attention_kernel(KvAttnParams P) {
@@ -663,9 +676,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
+      kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
       if (P.lse && jc == 0)
         P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
     }
@@ -748,9 +759,7 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
       const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (jc * NT + t < D) kv_put(dst + jc * NT + t, o[t] * inv);
+      kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
       if (P.lse && jc == 0)
         P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
     }
@@ -1014,35 +1023,53 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     l[r] += __shfl_xor(l[r], 16);
     l[r] += __shfl_xor(l[r], 32);
     if (any_bad) l[r] = __builtin_nanf("");
-    const int row = wave * 32 + 16 * r + c;
-    if (row >= n_rows) continue;
-    if (it.splits > 1) {
-      if (it.slot >= 0 && it.slot < P.slots) {
-        float* dst = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + g * 4;
+  }
+  if (it.splits > 1) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(dst + 16 * t) = acc[r][t];
-        if (g == 0) {
-          float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
-          ml[0] = m[r];
-          ml[1] = l[r];
-        }
+    for (int r = 0; r < R; ++r) {
+      const int row = wave * 32 + 16 * r + c;
+      if (row >= n_rows || it.slot < 0 || it.slot >= P.slots) continue;
+      float* dst = P.part + (static_cast<int64_t>(it.slot) * ROWS + row) * DP + g * 4;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(dst + 16 * t) = acc[r][t];
+      if (g == 0) {
+        float* ml = P.part_ml + (static_cast<int64_t>(it.slot) * ROWS + row) * 2;
+        ml[0] = m[r];
+        ml[1] = l[r];
       }
-    } else {
-      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
-      const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-      uint16_t* dst = reinterpret_cast<uint16_t*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head) + g * 4;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (16 * t + g * 4 < D) {
-          uint16_t y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = kv_to_bf16(acc[r][t][e] * inv);
-          __builtin_memcpy(__builtin_assume_aligned(dst + 16 * t, 8), y, 8);
-        }
-      if (P.lse && g == 0)
-        P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] =
-            ((m[r] == -INFINITY ? 0.0f : m[r]) + log2f(l[r])) * KV_LN2;
     }
+    return;
+  }
+  // The wave's rows through LDS (the workgroup is past its last read of the keys), so that DP / 8
+  // lanes write a row's consecutive bytes: a lane's own 8 bytes of 16 rows each took 4 us a workgroup.
+  uint16_t* own = &sh.k[0][0] + wave * 32 * DP;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+    // (pieces of 8 bytes, permuted as the keys' of 16)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      uint16_t y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = kv_to_bf16(acc[r][t][e] * inv);
+      __builtin_memcpy(__builtin_assume_aligned(own + (16 * r + c) * DP + ((4 * t + g) ^ (c & 7) << 1) * 4, 8), y, 8);
+    }
+    const int row = wave * 32 + 16 * r + c;
+    if (P.lse && g == 0 && row < n_rows) {
+      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] =
+          ((m[r] == -INFINITY ? 0.0f : m[r]) + log2f(l[r])) * KV_LN2;
+    }
+  }
+  constexpr int PIECES = DP / 8, PER = KV_WAVE / PIECES;
+  const int piece = lane % PIECES;
+#pragma unroll
+  for (int i = 0; i < 32; i += PER) {
+    const int in = i + lane / PIECES, row = wave * 32 + in;
+    if (row >= n_rows || piece * 8 >= D) continue;
+    const uint4 x = *reinterpret_cast<const uint4*>(own + in * DP + ((2 * piece) ^ (in & 7) << 1) * 4);
+    const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+    *reinterpret_cast<uint4*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head + piece * 16) = x;
   }
 }
 
