@@ -386,8 +386,9 @@ typedef struct {
 /* The pool: element d of token slot t, head h, page p, layer l is at
  * base[l * layer_stride + p * page_stride + h * head_stride + t * token_stride + d].
  * Keys and values have the same type, shape and strides (in elements).  Both
- * bases are 16-byte aligned and every stride is a multiple of 16 bytes; heads
- * and tokens may be in either order, and nothing may overlap. */
+ * bases are 16-byte aligned and every stride is a multiple of 16 bytes; the axes
+ * may be in any order, nothing may overlap, and page_size * token_stride is
+ * below 2^31 bytes. */
 typedef struct {
   void *k, *v;
   int32_t dtype;      /* saki_dtype                                                       */
@@ -505,7 +506,8 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  * lse = -infinity, one with a score of NaN or +infinity gets NaN.  Tokens of a sequence that lacks pages for them get NaN.
  * Products and softmax are accumulated in 32 bits; with bf16 the weights are
  * rounded to bf16 for their product with the values.
- *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536
+ *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads /
+ *              n_kv_heads below 2^31 - 256
  *   out        as q; may be q itself.  lse: float [n_tokens, n_q_heads] or NULL
  *   scale      finite;  window >= 0 (0: none);  sinks >= 0
  *   ws         saki_workspace_bytes(SAKI_OP_KV_ATTENTION, n_tokens * n_q_heads, head_dim)

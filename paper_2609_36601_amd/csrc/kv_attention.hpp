@@ -76,7 +76,7 @@ struct KvAttnParams {
 };
 
 // Blocks of BLK tokens that the rows of tokens [j0, j1) (positions p0 .. p1 - 1) see:
-// the first `sink` blocks, then those from token `lo` on.
+// the first `sinks` blocks, then those from token `lo` on.
 struct KvSpan {
   int lo;     // first token of the main part, a multiple of BLK
   int sinks;  // blocks of the sinks
@@ -115,12 +115,12 @@ __device__ __forceinline__ KvLoad kv_load_of(const KvAttnParams& P, int b) {
   s.start = L + P.n.shift;
   s.blocks = 1;
   if (s.fine && s.count > 0) {
+    s.blocks = (static_cast<int>(end) + BLK - 1) / BLK;
     if (P.window > 0) {
-      // the widest tile: P.span tokens at most, which may begin anywhere in a block
+      // the widest tile: P.span tokens at most, which may begin anywhere in a block (and no tile
+      // has more blocks than the sequence: where those are few, the host leaves out the join)
       const int span = s.count < P.span ? s.count : P.span;
-      s.blocks = kv_span<BLK>(end - span, end, P.window, P.sinks).blocks + (span < s.count ? 1 : 0);
-    } else {
-      s.blocks = (static_cast<int>(end) + BLK - 1) / BLK;
+      s.blocks = min(s.blocks, kv_span<BLK>(end - span, end, P.window, P.sinks).blocks + (span < s.count ? 1 : 0));
     }
   }
   return s;
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
     };
     uint4 kf[BF ? 2 : 1][QC];
     uint32_t vr[TOK][VW];
-    const int token_stride = static_cast<int>(P.p.token_stride);
+    const uint32_t token_stride = static_cast<uint32_t>(P.p.token_stride);  // (a page's tokens lie within 2^31 bytes)
     auto load_keys = [&](int t0) {
       const int run = run_of(t0 + k_in);
       const char* src = kb + page_at(k_id) + (g * 16);
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       for (int s = 0; s < (BF ? 2 : 1); ++s) {
         int tok = BF ? run + (c & 3) + 4 * s : run + (c & 7);
         tok = tok < last ? tok : last;
-        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
+        const char* at = src + static_cast<uint32_t>(tok & mask) * token_stride;
         if (D == DP) {
 #pragma unroll
           for (int e = 0; e < QC; ++e) kf[s][e] = *reinterpret_cast<const uint4*>(at + e * 64);
@@ -460,7 +460,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       for (int e = 0; e < TOK; ++e) {
         int tok = run + (BF ? 0 : v_in & 7) + e;
         tok = tok < last ? tok : last;
-        const char* at = src + static_cast<int64_t>(tok & mask) * token_stride;
+        const char* at = src + static_cast<uint32_t>(tok & mask) * token_stride;
 #pragma unroll
         for (int w = 0; w < VC; ++w) {
           // (elements from D on make rows of O that are not kept: any values will do)
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     const int mask = (1 << P.t.shift) - 1, last = p1 - 1;
     const char* kb = P.p.k + it.head * P.p.head_stride;
     const char* vb = P.p.v + it.head * P.p.head_stride;
-    const int token_stride = static_cast<int>(P.p.token_stride);
+    const uint32_t token_stride = static_cast<uint32_t>(P.p.token_stride);  // (a page's tokens lie within 2^31 bytes)
     auto token_of = [&](int i) { return i < span.sinks ? i * BLK : span.lo + (i - span.sinks) * BLK; };
     auto page_at = [&](int id) {
       const bool in = id >= 0 && id < P.t.n_pages;
@@ -886,7 +886,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int id = __builtin_amdgcn_readlane(ids, j), run = run_of(t0, j);
-        const int64_t at = page_at(id) + static_cast<int64_t>(run & mask) * token_stride;
+        const int64_t at = page_at(id) + static_cast<uint32_t>(run & mask) * token_stride;
         const uint32_t to = buf * 64 * DP * 2 + (wave * J + j) * 1024;
         // (no row behind the last token is read)
         const int row = t0 + BLK - 1 <= last || row_in < last - run ? row_in : last - run;

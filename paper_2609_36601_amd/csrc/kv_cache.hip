@@ -68,6 +68,8 @@ saki_status check_pool(const saki_kv_pool* p, const saki_kv_table* t) {
                   {t->page_size, p->token_stride}};
   if (const char* why = bad_layout(axes, 4, p->head_dim, elem_bytes(p->dtype)))
     return abi_fail(why[0] == 's' ? SAKI_E_ALIGN : SAKI_E_SHAPE, why);
+  if (p->token_stride * elem_bytes(p->dtype) > INT32_MAX / t->page_size)
+    return abi_fail(SAKI_E_SHAPE, "page_size * token_stride must be below 2^31 bytes");
   return SAKI_OK;
 }
 
@@ -454,7 +456,7 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;
-  if (n * group > INT32_MAX || units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  if (n * group > INT32_MAX - 256 || units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
   KvAttnParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);

@@ -126,6 +126,16 @@ def test_one_long_sequence_is_split(saki_lib, dtype, new):
     run(saki_lib, *make(saki_lib, dtype, [20011, 3, 900], [new] * 3, 4, 2, 128, 64, new), uniform=new, rows=3)
 
 
+@pytest.mark.parametrize("dtype,rows", [(BF, 256), (F32, 128)])
+def test_tables_too_short_for_a_split(saki_lib, dtype, rows):
+    """A table of 8 blocks a sequence: nothing is split and nothing joined, whatever the window."""
+    new = 10
+    t, c, q, off, dense = make(saki_lib, dtype, [rows - new], [new], 4, 2, 64, 16, 31)
+    c = saki_lib.PagedKV(c.k, c.v, c.pages[:, :rows // 16].contiguous(), c.length, c.held, c.refs)
+    for window in (0, rows - 56, rows // 2, 33):
+        run(saki_lib, t, c, q, off, dense, uniform=new, window=window, sinks=3)
+
+
 def test_shift_and_large_scores(saki_lib):
     """Tokens behind the committed ones (a draft position), and scores far from 0: the running maximum moves."""
     t, c, q, off, dense = make(saki_lib, BF, [60, 5, 300], [1, 1, 1], 2, 2, 64, 8, 3, shift=4)

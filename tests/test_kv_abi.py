@@ -49,6 +49,7 @@ BAD_POOLS = [(dict(dtype=2), 4), (dict(reserved=3), 3), (dict(n_kv_heads=0), 2),
              (dict(n_layers=65537), 2), (dict(k=0), 1), (dict(v=0), 1), (dict(v=72), 5), (dict(token_stride=60), 5),
              (dict(token_stride=56), 2), (dict(head_stride=64 * 15), 2), (dict(page_stride=64 * 16), 2),
              (dict(layer_stride=64), 2), (dict(layer_stride=-64), 5), (dict(page_stride=2**62), 5),
+             (dict(token_stride=2**26, head_stride=64, page_stride=128, layer_stride=2**31), 2),  # a page beyond 2^31 bytes
              # keys head-major and tokens inside, but pages closer than their tokens
              (dict(token_stride=128, head_stride=64, page_stride=1024), 2)]
 
@@ -144,6 +145,7 @@ def test_tokens_and_rows(lib):
     assert attend(hq=3) == 2 and attend(hq=0) == 2
     assert attend(scale=float("nan")) == 3 and attend(scale=float("inf")) == 3
     assert attend(window=-1) == 3 and attend(sinks=-1) == 3 and attend(lse=66) == 5
+    assert attend(n=tokens(n_tokens=2**31 - 4, n_new=2**29 - 1)) == 2
     assert attend(out=None) == 1 and attend(out=heads(head_stride=32)) == 2
     assert attend(ws=None) == 6 and attend(ws_bytes=100) == 6 and attend(ws=72) == 5
     assert attend(n=tokens(n_tokens=0, n_new=0), ws=None) == 0
