@@ -485,9 +485,9 @@ typedef struct {
 } saki_kv_rope;
 
 /* Rotates q into q_out and k, and writes k and v to the pages of their
- * positions in `layer`.  A token whose position is outside its
- * sequence's pages (saki_kv_reserve) is not written, and its q_out row is NaN.
- * No page written may be shared: call saki_kv_reserve first.
+ * positions in `layer`.  A token whose position is outside its sequence's pages,
+ * or on a page that other sequences hold too, is not written, and its q_out row is
+ * NaN: saki_kv_reserve first, again after a saki_kv_fork.
  *   rope   NULL: no rotation
  *   q      NULL (with q_out NULL, n_q_heads 0): keys and values only
  *   q_out  may be q itself; other overlaps between q_out and inputs are not allowed. */

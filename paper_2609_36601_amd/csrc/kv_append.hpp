@@ -91,7 +91,8 @@ __global__ __launch_bounds__(KV_APPEND_NT) void kv_append_kernel(KvAppendParams 
   const int64_t slot_page = pos >> P.t.shift;
   int page = -1;
   if (pos >= 0 && slot_page < kv_held(P.t, b)) page = P.t.pages[static_cast<int64_t>(b) * P.t.max_pages + slot_page];
-  const bool fine = page >= 0 && page < P.t.n_pages;
+  // (a page that other sequences hold too is not written: they would see the token)
+  const bool fine = page >= 0 && page < P.t.n_pages && P.t.refs[page] <= 1;
   const int R2 = P.pairs, D = P.p.dim;
   for (int i = tid; i < R2; i += KV_APPEND_NT) {
     const double turns = static_cast<double>(pos) * P.freq[i];

@@ -160,6 +160,25 @@ def test_tokens_without_pages_are_not_written(saki_lib):
         torch.cuda.synchronize()
 
 
+def test_shared_pages_are_not_written(saki_lib):
+    """After a fork both sequences hold the last page: neither may write to it before a reserve."""
+    t, c, x, off = make(saki_lib, torch.float32, [11, 0], [2, 0], 2, 1, 16, 8, 4)
+    pair = torch.tensor([0], dtype=torch.int32, device=DEV), torch.tensor([1], dtype=torch.int32, device=DEV)
+    c.commit(done=torch.tensor([0, 1], dtype=torch.uint8, device=DEV))
+    assert c.fork(*pair).tolist() == [0]
+    before = c.k.clone()
+    x = torch.cat([x, x + 1])
+    q = c.append(0, x[:, 2:3], x[:, 3:], q=x[:, :2], n_new=2)
+    assert torch.isnan(q).all() and torch.equal(c.k, before)
+    assert c.reserve(2).tolist() == [0, 0]
+    q = c.append(0, x[:, 2:3], x[:, 3:], q=x[:, :2], n_new=2)
+    assert torch.equal(q, x[:, :2])
+    for b in range(2):
+        page = int(c.pages[b, 1])
+        assert torch.equal(c.k[0, page, 0, 3:5], x[2 * b:2 * b + 2, 2])
+        assert torch.equal(c.k[:, page, :, :3], before[:, int(t.pages[0, 1]), :, :3])  # the 3 slots they share
+
+
 def test_many_sequences(saki_lib):
     """Ragged rows of 70,000 sequences (most without any): every row finds its own."""
     n = 70000
