@@ -77,6 +77,8 @@ class PagedKV:
         """The cache's device and the call's stream current: outputs and workspaces are allocated for it."""
         if stream is None and torch.cuda.current_device() == self.device.index:
             return _HERE
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device} for a cache on {self.device}")
         return self._elsewhere(stream)
 
     @contextlib.contextmanager

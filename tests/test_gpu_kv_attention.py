@@ -136,6 +136,17 @@ def test_tables_too_short_for_a_split(saki_lib, dtype, rows):
         run(saki_lib, t, c, q, off, dense, uniform=new, window=window, sinks=3)
 
 
+@pytest.mark.parametrize("dim,page,order,lengths,new", [
+    (64, 8, "heads", [3001], [100]), (128, 8, "heads", [2500, 0], [70, 200]), (128, 16, "tokens", [0, 5000], [65, 130]),
+    (40, 16, "heads", [700, 30, 0], [90, 0, 129]), (128, 256, "heads", [1, 257], [128, 255])])
+def test_prompts_behind_long_caches(saki_lib, dim, page, order, lengths, new):
+    """Many rows whose keys are split and joined, in pages shorter and longer than a tile."""
+    print(f"long prompts: dim {dim} page {page} {lengths} {new}", flush=True)
+    args = make(saki_lib, BF, lengths, new, 3, 2, dim, page, dim + page, order, spare=3)
+    run(saki_lib, *args, rows=9)
+    run(saki_lib, *args, rows=9, window=333, sinks=70)
+
+
 def test_shift_and_large_scores(saki_lib):
     """Tokens behind the committed ones (a draft position), and scores far from 0: the running maximum moves."""
     t, c, q, off, dense = make(saki_lib, BF, [60, 5, 300], [1, 1, 1], 2, 2, 64, 8, 3, shift=4)
@@ -174,6 +185,61 @@ def test_hidden_tokens_have_no_influence(saki_lib, dtype):
     out = c.attention(1, q, lse=lse, n_new=1)
     assert (out[0] == 0).all() and (lse[0] == -float("inf")).all()
     assert torch.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
+def test_hidden_tokens_in_prompts(saki_lib, dim, window, sinks):
+    """The same where one workgroup holds rows that see a token and rows that do not."""
+    t, c, q, off, dense = make(saki_lib, BF, [100, 0], [200, 150], 2, 2, dim, 32, dim + window)
+    for b, (kb, vb) in enumerate(dense):
+        kb[30], vb[30] = float("inf"), -float("inf")
+        vb[110] = NAN
+        kb[140] = NAN
+        vb[-1] = float("inf")
+        put(t, b, c.k, c.v, kb, vb)
+    out, lse = run(saki_lib, t, c, q, off, dense, window=window, sinks=sinks)
+    assert torch.isfinite(out[200:230]).all() and torch.isfinite(lse[200:230]).all()  # before token 30
+    t, c, q, off, dense = make(saki_lib, BF, [0, 0], [150, 130], 2, 1, dim, 8, 22)
+    q.abs_()
+    dense[0][0].fill_(-float("inf"))
+    put(t, 0, c.k, c.v, *dense[0])
+    lse = torch.empty(280, 2, device=DEV)
+    out = c.attention(1, q, lse=lse, offsets=torch.as_tensor([0, 150, 280], dtype=torch.int32, device=DEV))
+    assert (out[:150] == 0).all() and (lse[:150] == -float("inf")).all() and torch.isfinite(out[150:]).all()
+
+
+def test_prompts_without_pages_and_in_place(saki_lib):
+    t, c, q, off, dense = make(saki_lib, BF, [50, 70, 20, 1500], [100] * 4, 3, 2, 64, 8, 23)
+    want = c.attention(1, q, n_new=100)
+    wide = torch.zeros(400, 11, 64, dtype=BF, device=DEV)
+    wide[:, 2:8] = q
+    got = c.attention(1, wide[:, 2:8], out=wide[:, 2:8], n_new=100)
+    assert torch.equal(got, want) and (wide[:, :2] == 0).all() and (wide[:, 8:] == 0).all()
+    c.held[0] -= 1
+    c.pages[1, 3] = -1
+    c.pages[3, 100] = c.k.shape[1]
+    c.length[2] = -7
+    lse = torch.empty(q.shape[:2], device=DEV)
+    out = c.attention(1, q, lse=lse, n_new=100)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+def test_calls_at_once_on_two_streams(saki_lib):
+    """Calls on two streams with workspaces of their own do not disturb each other."""
+    a = make(saki_lib, BF, [9000, 5], [3, 3], 4, 2, 128, 16, 40)
+    b = make(saki_lib, BF, [300, 2000], [120, 120], 2, 2, 64, 32, 41)
+    want = [a[1].attention(1, a[2], n_new=3), b[1].attention(1, b[2], n_new=120)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (x, new) in enumerate(((a, 3), (b, 120))):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(x[1].attention(1, x[2], n_new=new))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
 
 
 def test_sequences_without_pages_get_nan(saki_lib):
