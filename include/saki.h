@@ -489,6 +489,7 @@ typedef struct {
  * or on a page that other sequences hold too, is not written, and its q_out row is
  * NaN: saki_kv_reserve first, again after a saki_kv_fork.
  *   rope   NULL: no rotation
+ *   tokens fewer than 2^24 rows
  *   q      NULL (with q_out NULL, n_q_heads 0): keys and values only
  *   q_out  may be q itself; other overlaps between q_out and inputs are not allowed. */
 saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool, int64_t layer,
@@ -503,11 +504,12 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  *   out = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j exp(scale q . k_j).
  * Keys and values at positions that a token does not see have no influence on
  * it, whatever they hold.  A token whose every score is -infinity gets out = 0,
- * lse = -infinity, one with a score of NaN or +infinity gets NaN.  Tokens of a sequence that lacks pages for them get NaN.
+ * lse = -infinity, one with a score of NaN or +infinity gets NaN.  Tokens of a
+ * sequence that lacks pages for them get NaN.
  * Products and softmax are accumulated in 32 bits; with bf16 the weights are
  * rounded to bf16 for their product with the values.
- *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads /
- *              n_kv_heads below 2^31 - 256
+ *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads / 16
+ *              + n_seq * n_kv_heads below 2^24 - 8192 (more may be SAKI_E_SHAPE)
  *   out        as q; may be q itself.  lse: float [n_tokens, n_q_heads] or NULL
  *   scale      finite;  window >= 0 (0: none);  sinks >= 0
  *   ws         saki_workspace_bytes(SAKI_OP_KV_ATTENTION, n_tokens * n_q_heads, head_dim)

@@ -529,6 +529,7 @@ def saki_kv_reserve(table, pool, n_new, status=None, workspace=None, stream=None
     """Call saki_kv_reserve; n_new: an int32 tensor [n_seq], or one number for every sequence."""
     _lib or load()
     each = isinstance(n_new, torch.Tensor)
+    _dense(n_new if each else None, status, workspace)
     if not each and not 0 <= n_new < 2**31:
         raise ValueError("n_new outside [0, 2^31)")
     _check(_lib.saki_kv_reserve(_ref(table), _ref(pool), _addr(n_new) if each else None, 0 if each else int(n_new),
@@ -537,16 +538,19 @@ def saki_kv_reserve(table, pool, n_new, status=None, workspace=None, stream=None
 
 def saki_kv_commit(table, delta, done=None, status=None, stream=None):
     _lib or load()
+    _dense(delta, done, status)
     _check(_lib.saki_kv_commit(_ref(table), _addr(delta), _addr(done), _addr(status), _stream(stream)))
 
 
 def saki_kv_fork(table, src, dst, status=None, stream=None):
     _lib or load()
+    _dense(src, dst, status)
     _check(_lib.saki_kv_fork(_ref(table), src.numel(), _addr(src), _addr(dst), _addr(status), _stream(stream)))
 
 
 def saki_kv_compact(table, pool, n_live=None, workspace=None, stream=None):
     _lib or load()
+    _dense(n_live, workspace)
     _check(_lib.saki_kv_compact(_ref(table), _ref(pool), _addr(n_live), _addr(workspace), _ws_bytes(workspace),
                                 _stream(stream)))
 
@@ -561,8 +565,10 @@ def saki_kv_append(table, pool, layer, tokens, k, v, q=None, q_out=None, rope=No
 def saki_kv_attention(table, pool, layer, tokens, q, out, lse=None, scale=1.0, window=0, sinks=0, workspace=None,
                       stream=None):
     _lib or load()
+    _dense(lse, workspace)
     for name, x in (("window", window), ("sinks", sinks)):
         if not 0 <= x < 2**31:
             raise ValueError(f"{name} outside [0, 2^31)")
-    _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _heads(q), _heads(out), _addr(lse), float(scale), int(window), int(sinks), _addr(workspace),
+    _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _heads(q), _heads(out),
+                                  _addr(lse), float(scale), int(window), int(sinks), _addr(workspace),
                                   _ws_bytes(workspace), _stream(stream)))

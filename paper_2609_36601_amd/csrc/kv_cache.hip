@@ -11,6 +11,7 @@ namespace {
 
 constexpr int64_t MAX_SEQ = int64_t{1} << 24;
 constexpr int64_t MAX_TOKENS = int64_t{1} << 30;  // of a sequence's pages, and of `shift`
+constexpr int64_t MAX_THREADS = int64_t{1} << 32;  // a launch has fewer
 
 int64_t up16(int64_t b) { return (b + 15) & ~int64_t{15}; }
 int elem_bytes(int32_t dtype) { return dtype == SAKI_BF16 ? 2 : 4; }
@@ -401,6 +402,7 @@ saki_status saki_kv_append(const saki_kv_table* table, const saki_kv_pool* pool,
   if (st != SAKI_OK) return st;
   st = check_heads(v, n, pool->n_kv_heads, pool, false, "v");
   if (st != SAKI_OK) return st;
+  if (n >= MAX_THREADS / KV_APPEND_NT) return abi_fail(SAKI_E_SHAPE, "too many tokens in one call");
   KvAppendParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);
@@ -456,7 +458,8 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;
-  if (n * group > INT32_MAX - 256 || units > INT32_MAX - 8192) return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
+  if (n * group > INT32_MAX - 256 || units >= MAX_THREADS / KV_ATT_NT - 8192)
+    return abi_fail(SAKI_E_SHAPE, "too many query rows in one call");
   KvAttnParams P{};
   P.t = device_table(table);
   P.p = device_pool(pool, layer);

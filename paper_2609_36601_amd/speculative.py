@@ -94,8 +94,9 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
     ws = torch.empty(max(_b.workspace_bytes(_b.SAKI_OP_VERIFY, B * k, V), 8), dtype=torch.uint8, device=dev)
     # what the model continues from: its state, or with caches the last token
     state = model.start(prompts) if caches else model.initial(prompts)
-    wanting = torch.full((B,), k, dtype=torch.int32, device=dev)  # tokens of the wave
-    lacking = torch.zeros((), dtype=torch.bool, device=dev)
+    if caches:
+        wanting = torch.full((B,), k, dtype=torch.int32, device=dev)  # tokens of the wave
+        lacking = torch.zeros((), dtype=torch.bool, device=dev)
 
     def timed(name, fn, *a, **kw):
         if timing is None:
@@ -149,10 +150,9 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
             prev = H.gather(1, (m - 1).clamp(min=0)[:, None])[:, 0]
             state = torch.where(m > 0, model.advance(prev, last), state)
         wave += 1
-        if wave % check_every == 0 or wave == limit:
-            running, short = torch.stack([(traj["done"] == _b.SEQ_RUNNING).any(), lacking]).tolist()
-            if short:
-                raise RuntimeError("a cache has too few pages for the rollout, or too few per sequence")
-            if not running:
-                break
+        check = wave % check_every == 0
+        if caches and (check or wave == limit) and bool(lacking):
+            raise RuntimeError("a cache has too few pages for the rollout, or too few per sequence")
+        if check and not bool((traj["done"] == _b.SEQ_RUNNING).any()):
+            break
     return traj, wave

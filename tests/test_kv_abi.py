@@ -200,3 +200,24 @@ def test_rope_scalings():
     assert between.any() and (ramp["freq"][between] < f["freq"][between]).all()
     assert (ramp["freq"][between] > f["freq"][between] / 8).all()
     assert saki.rope(0, device="cpu")["freq"].numel() == 0
+
+
+def test_more_rows_than_a_launch_takes(lib):
+    t, p, h = table(), pool(), heads()
+    for n in (2**22, 2**29 - 1):
+        rows = tokens(n_tokens=4 * n, n_new=n)
+        assert lib.saki_kv_append(t, p, 0, rows, None, 2, h, h, h, h, None) == 2
+    rows = tokens(n_tokens=2**30, n_new=2**28)
+    assert lib.saki_kv_attention(t, p, 0, rows, 2, h, h, None, 1.0, 0, 0, 64, 1 << 30, None) == 2
+
+
+def test_raw_calls_refuse_strided_arrays(lib):
+    import torch
+    every_other = torch.zeros(8, dtype=torch.int32)[::2]
+    t, p = b.SakiKVTable(4), b.SakiKVPool()
+    with pytest.raises(ValueError, match="contiguous"):
+        b.saki_kv_commit(t, every_other)
+    with pytest.raises(ValueError, match="contiguous"):
+        b.saki_kv_reserve(t, p, every_other)
+    with pytest.raises(ValueError, match="contiguous"):
+        b.saki_kv_fork(t, every_other, every_other)
