@@ -437,7 +437,7 @@ saki_status saki_kv_commit(const saki_kv_table *table, const int32_t *delta, con
 /* Sequence dst[i] becomes a copy of sequence src[i], i < n (device int32
  * arrays), by sharing its pages.  dst[i] must hold nothing, may be no pair's src
  * and no earlier pair's dst: such a pair, or one with an index outside [0, n_seq), is left out
- * with SAKI_KV_BAD.  n <= n_seq.
+ * with SAKI_KV_BAD.  n <= n_seq, at most 2^20.
  *   status  [n] SAKI_KV_*, or NULL */
 saki_status saki_kv_fork(const saki_kv_table *table, int64_t n, const int32_t *src, const int32_t *dst,
                          uint8_t *status, saki_stream_t stream);

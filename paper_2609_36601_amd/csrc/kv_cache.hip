@@ -11,6 +11,7 @@ namespace {
 
 constexpr int64_t MAX_SEQ = int64_t{1} << 24;
 constexpr int64_t MAX_TOKENS = int64_t{1} << 30;  // of a sequence's pages, and of `shift`
+constexpr int64_t MAX_FORKS = int64_t{1} << 20;   // pairs of a call: each is compared with all others
 constexpr int64_t MAX_THREADS = int64_t{1} << 32;  // a launch has fewer
 
 int64_t up16(int64_t b) { return (b + 15) & ~int64_t{15}; }
@@ -315,7 +316,7 @@ saki_status saki_kv_fork(const saki_kv_table* table, int64_t n, const int32_t* s
                          uint8_t* status, saki_stream_t stream) {
   saki_status st = check_table(table);
   if (st != SAKI_OK) return st;
-  if (n < 0 || n > table->n_seq) return abi_fail(SAKI_E_SHAPE, "n outside [0, n_seq]");
+  if (n < 0 || n > table->n_seq || n > MAX_FORKS) return abi_fail(SAKI_E_SHAPE, "n outside [0, n_seq], or more than 2^20");
   if (n == 0) return abi_ok();
   if (!src || !dst) return abi_fail(SAKI_E_NULLPTR, "src and dst are required");
   if (off(src, 4) || off(dst, 4)) return abi_fail(SAKI_E_ALIGN, "src and dst must be 4-byte aligned");

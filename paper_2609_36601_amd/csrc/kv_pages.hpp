@@ -215,8 +215,8 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
     }
   }
   // 3. how much that is: the call takes all of it or nothing.  Pages in the lower half, copies
-  // in the upper half of a sum (at most 2^24 sequences; a request of more than 2^31
-  // pages in all is more than any pool holds, however its sum carries)
+  // in the upper half of a sum (no more pages are asked for than the table has entries, and 2^40
+  // of those would be 4 TB)
   auto sum_of = [&](const KvWant& w) {
     const long long copy = w.slot >= 0;
     return (copy << 40) + w.fresh + copy;

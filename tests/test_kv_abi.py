@@ -207,6 +207,7 @@ def test_more_rows_than_a_launch_takes(lib):
     for n in (2**22, 2**29 - 1):
         rows = tokens(n_tokens=4 * n, n_new=n)
         assert lib.saki_kv_append(t, p, 0, rows, None, 2, h, h, h, h, None) == 2
+    assert lib.saki_kv_fork(table(n_seq=2**24), 2**20 + 1, 64, 64, None, None) == 2  # pairs are compared with each other
     rows = tokens(n_tokens=2**30, n_new=2**28)
     assert lib.saki_kv_attention(t, p, 0, rows, 2, h, h, None, 1.0, 0, 0, 64, 1 << 30, None) == 2
 
