@@ -1,6 +1,6 @@
 """Paged key-value caches in plain sequential Python / NumPy float64.
 
-Pages: one sequence after the other, one page at a time, from the rules of include/saki.h.
+Pages: one sequence after the other, one page at a time, from the rules of include/saki_kv.h.
 Rotary positions and attention: token by token from their definitions.
 """
 import numpy as np

@@ -1,4 +1,4 @@
-"""ctypes binding of libsaki.so (include/saki.h).
+"""ctypes binding of libsaki.so (include/saki.h, saki_kv.h).
 
 Argument marshalling only: every step of the path runs in the HIP library.
 Tensors are torch device tensors; the library sees their data pointers and the
@@ -29,8 +29,9 @@ STATUS = {0: "SAKI_OK", 1: "SAKI_E_NULLPTR", 2: "SAKI_E_SHAPE", 3: "SAKI_E_VALUE
 
 EXPORTED = ["saki_workspace_bytes", "saki_couple", "saki_couple_static", "saki_route_loss", "saki_spec_verify",
             "saki_select_positions", "saki_probe_metrics", "saki_sample", "saki_commit",
-            "saki_kv_reserve", "saki_kv_commit", "saki_kv_fork", "saki_kv_compact", "saki_kv_append", "saki_kv_attention",
             "saki_status_str", "saki_last_error"]
+EXPORTED_KV = ["saki_kv_reserve", "saki_kv_commit", "saki_kv_fork", "saki_kv_compact", "saki_kv_append",
+               "saki_kv_attention"]  # of include/saki_kv.h
 KV_OK, KV_NO_PAGES, KV_TOO_LONG, KV_BAD = 0, 1, 2, 3
 SEQ_RUNNING, SEQ_FINISHED, SEQ_STOPPED = 0, 1, 2
 SAKI_MAX_PROBE_K = 64

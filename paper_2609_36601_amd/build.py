@@ -1,4 +1,4 @@
-"""Builds libsaki.so (the gfx950 HIP library behind include/saki.h) in-tree."""
+"""Builds libsaki.so (the gfx950 HIP library behind include/saki.h and saki_kv.h) in-tree."""
 import os
 import subprocess
 import sys

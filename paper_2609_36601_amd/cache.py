@@ -1,4 +1,4 @@
-"""Paged key-value caches of a rollout's student and teacher (include/saki.h, saki_kv_*).
+"""Paged key-value caches of a rollout's student and teacher (include/saki_kv.h).
 
 PagedKV holds a pool of pages and a table of which pages each sequence holds; its
 methods are the library's calls with their outputs and workspaces allocated.  Every step runs

@@ -4,7 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
-#include "../../include/saki.h"
+#include "../../include/saki_kv.h"
 
 namespace saki {
 

@@ -156,7 +156,8 @@ __device__ __forceinline__ int kv_split_at(int blocks, int splits, int split) {
 // tile (last first: with causal rows those are the longest), split, key head, so that the
 // workgroups of one key head, which read the same keys, tend to one XCD.  False: there is
 // no such item.  Every workgroup pays for this before it begins: sums in 32 bits, no divisions but
-// in the one thread that holds the item (3 us of a workgroup's 10 with 64-bit sums and divisions).
+// in the one thread that holds the item (4.1 us with 64-bit sums and divisions in every thread, 2.9
+// without, 16 sequences).
 template <int ROWS, int BLK, int ITEMS>
 __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out) {
   __shared__ int part_blocks[KV_ATT_WAVES];
@@ -342,7 +343,16 @@ __device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float f,
     }
 }
 
-// One item: ROWS = 16 R rows, the blocks of its split dealt to the four waves.
+// One item: ROWS = 16 R rows, the blocks of its split dealt to the four waves, each of which has a
+// running maximum and sum of its own until the end: no barrier between blocks, and every wave's
+// loads, a block ahead, go from memory straight to the registers that the products read.
+// What bounds it: reading the keys and values (512 drafts over 4,480 keys, 8 + 8 heads of 128 bf16
+// elements: 1,555 us, 6.0 TB/s, what a large read reaches; 128 verifications of 8 tokens by 4 query
+// heads a key head, R = 2: 440 us, 5.4); for one long sequence that and the join's launch behind
+// it (131,072 keys: 44 and 7 us); for few short ones the way to the first product (16 drafts 16 us,
+// of which the keys' bytes take 14 only if all are under way at once); in f32 the matrix products, at
+// an eighth of bf16's rate, and the blocks at both ends of a row's window (ragged tokens behind a
+// window of 500: 82 us, 38 TFLOP/s over what the rows see).
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_attention_kernel(KvAttnParams P) {
   constexpr bool BF = sizeof(T) == 2;
@@ -685,7 +695,8 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
 
 // Joins the partial sums of the split units, of which there are no more than items aimed at
 // (each has more blocks than an item takes).  A workgroup takes JR rows of a unit at a time;
-// 16 threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.
+// 16 threads hold a row's elements, and the splits are dealt to the 16 / JR groups of them.  What
+// bounds it: latency.  A launch that finds nothing to join takes 4 us, 128 units of 16 drafts 8.
 template <typename T, int DP, int ROWS, int JR>
 __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
   constexpr int NT = DP / 16, PER = ROWS / JR, GROUPS = 16 / JR;
@@ -775,6 +786,10 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
 // that the 16 rows which a read touches lie in 16 different banks.  The values are transposed
 // by the read (ds_read_b64_tr_b16: 16 lanes read 4 tokens of 16 elements, and each gets
 // one element's 4 tokens).
+// What bounds it: vector instructions (7 for a matrix product: exponentials, their sums, the running
+// maximum) and the wait for the next tokens (one sequence of 16,384 tokens 750 TFLOP/s, on tiles that
+// are not exchanged 1,000); with ragged prompts the start of a workgroup, some 5 us, and the last ones
+// to end as well (16 of 2 to 2,500 tokens 285 us, 515 TFLOP/s).
 template <int DP>
 struct KvPromptShared {
   alignas(1024) uint16_t k[2][64 * DP];

@@ -6,7 +6,7 @@
 #include <math.h>
 #include <stdint.h>
 
-#include "../../include/saki.h"
+#include "../../include/saki_kv.h"
 
 namespace saki {
 

@@ -14,7 +14,6 @@
 #include <mutex>
 #include <string>
 
-#include "../../include/saki.h"
 #include "abi.hpp"
 #include "couple.hpp"
 #include "verify.hpp"

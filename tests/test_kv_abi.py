@@ -1,6 +1,7 @@
 """Refusals of the paged key-value cache, found on the host before a device is touched."""
 import ctypes
 import os
+import re
 
 import pytest
 import torch
@@ -15,6 +16,12 @@ def lib():
         from paper_2609_36601_amd import build
         build.build()
     return saki.load()
+
+
+def test_header_and_exports_agree(lib):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "saki_kv.h")).read()
+    names = set(re.findall(r"^saki_status\s+(saki_\w+)\s*\(", text, re.M))
+    assert names == set(b.EXPORTED_KV) and all(hasattr(lib, n) for n in names)
 
 
 def table(**kw):
