@@ -48,10 +48,10 @@ MEASURED_TRAFFIC = {
                dict(fetch_kib=13043150.1, write_kib=6189.4, fetch_scale=2.0, write_scale=1.0)},
     "stream": {"00d65faa91eaf0f80742922469398c4c9f569e617eee4fdf2719db3235af0969":
                dict(fetch_kib=2629986.2, write_kib=2850790.9, fetch_scale=2.0, write_scale=1.0)},
-    "route": {"af8737b4ad1a8ab44931f40886983b160244436e1bd2f6ce7088195b44814fc3":
-               dict(fetch_kib=17097049.1, write_kib=41663778.2, fetch_scale=2.0, write_scale=1.0)},
-    "probe": {"3a270d9228d1c9e89c5db6d7d1e7f5a0f929e3f9f2aca46c77c7c72a5e3c31df":
-               dict(fetch_kib=1285231.1, write_kib=976.0, fetch_scale=2.0, write_scale=1.0)},
+    "route": {"fab9ede9d7a033d180ba665aff4d8b0c1ea78aaffc46b38feb0678eb278d9b4b":
+               dict(fetch_kib=17097268.9, write_kib=41544960.3, fetch_scale=2.0, write_scale=1.0)},
+    "probe": {"add8c799ce94271dabdeeeb018e2a45c4d6bfd46dce7db7885aa58e1e8be0852":
+               dict(fetch_kib=1285626.8, write_kib=981.4, fetch_scale=2.0, write_scale=1.0)},
 }
 
 
