@@ -174,10 +174,21 @@ AttentionWs attention_ws(bool bf, int dp, int rows) {
 }
 
 // Row tiles a workgroup takes in a call of `mean` rows a sequence and key head: those
-// of a sequence of mean length; past 64, the kernel for prompts.
-int attention_tiles(bool bf, int dp, int64_t mean) {
-  if (bf && dp <= 128 && mean > 64) return KV_PROMPT_ROWS / 16;
+// of a sequence of mean length; past 64, and past what a tile takes where the sequences alone fill the
+// card (`full`), the kernel for prompts.  64 sequences, 2,000 keys, 8 key heads, us:
+//   rows                16   32   48   64   96  128    (heads of 128 elements)
+//   tiles of 16        101  118  159  201  285  370
+//   tiles of 32        105  107  129  132  180  228
+//   for prompts                  121  122  126  136
+//   rows                16   32   48   64   96  128    (64)
+//   tiles of 16         51   64   85  111  160  213
+//   tiles of 64                   56   58  101  103
+//   for prompts                   84   83   86   90
+// Where they do not fill it, a half-empty workgroup that is split costs more: 4 sequences, 8,000 keys,
+// 64 rows of 128 elements 45 us in tiles of 32, 56 in the kernel for prompts.
+int attention_tiles(bool bf, int dp, int64_t mean, bool full) {
   const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
+  if (bf && dp <= 128 && (mean > 64 || (full && mean > 16 * most))) return KV_PROMPT_ROWS / 16;
   return std::min(most, mean <= 16 ? 1 : mean <= 32 ? 2 : 4);
 }
 
@@ -246,7 +257,8 @@ size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
       for (const int64_t rows : {1, 17, 33, 65})
         if (rows <= n)
           for (const bool bf : {false, true})
-            most = std::max(most, attention_ws(bf, pow2_dim(m), 16 * attention_tiles(bf, pow2_dim(m), rows)).bytes);
+            for (const bool full : {false, true})
+              most = std::max(most, attention_ws(bf, pow2_dim(m), 16 * attention_tiles(bf, pow2_dim(m), rows, full)).bytes);
       return static_cast<size_t>(most);
     }
     default:
@@ -455,7 +467,8 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   const bool bf = pool->dtype == SAKI_BF16;
   const int dp = pow2_dim(pool->head_dim);
   const int group = n_q_heads / pool->n_kv_heads;
-  const int tiles = attention_tiles(bf, dp, n * group / table->n_seq), rows = 16 * tiles;
+  const bool full = table->n_seq * pool->n_kv_heads >= KV_ITEMS<uint16_t, 128, KV_PROMPT_ROWS>;
+  const int tiles = attention_tiles(bf, dp, n * group / table->n_seq, full), rows = 16 * tiles;
   int64_t units = tokens->offsets ? n * group / rows + std::min<int64_t>(table->n_seq, n)
                                   : table->n_seq * ((static_cast<int64_t>(tokens->n_new) * group + rows - 1) / rows);
   units *= pool->n_kv_heads;

@@ -330,3 +330,14 @@ def test_offsets_past_32_bits(saki_lib):
     t = ocache.Table(1, 4, 1, page)
     t.length[0] = 200
     check(out, None, q, [0, 1], [(kb, vb)], t, dim**-0.5, 0, 0)
+
+
+@pytest.mark.parametrize("dim,n", [(128, 64), (128, 63), (64, 64)])
+def test_many_sequences_of_half_a_tile(saki_lib, dim, n):
+    """36 to 64 rows a sequence and key head, where enough sequences change the kernel."""
+    rng = np.random.default_rng(n + dim)
+    args = make(saki_lib, BF, rng.integers(0, 90, n), [9] * n, 4, 8, dim, 16, dim + n)
+    run(saki_lib, *args, uniform=9, rows=2)
+    new = rng.integers(0, 33, n)
+    args = make(saki_lib, BF, rng.integers(0, 90, n), new + (new.sum() < 9 * n), 4, 8, dim, 8, dim + n)
+    run(saki_lib, *args, window=50, rows=2)
