@@ -32,7 +32,9 @@ hipError_t launch_kv_attention<PartT, PART_DP>(const KvAttnParams& P, int row_ti
                                                hipStream_t st) {
   constexpr int MOST = kv_row_tiles<PartT>(PART_DP);
   if constexpr (sizeof(PartT) == 2 && PART_DP <= 128)
-    if (row_tiles == 8) return launch<PartT, PART_DP, KV_PROMPT_ROWS>(kv_prompt_kernel<PART_DP>, P, units, join, st);
+    if (row_tiles == 8)
+      return launch<PartT, PART_DP, KV_PROMPT_ROWS>(
+          P.p.dim == PART_DP ? kv_prompt_kernel<PART_DP, true> : kv_prompt_kernel<PART_DP, false>, P, units, join, st);
   if constexpr (MOST >= 4)
     if (row_tiles == 4) return launch<PartT, PART_DP, 64>(kv_attention_kernel<PartT, PART_DP, 4>, P, units, join, st);
   if constexpr (MOST >= 2)
