@@ -259,6 +259,22 @@ __device__ __forceinline__ bool kv_find_item(const KvAttnParams& P, KvItem* out)
   return __builtin_amdgcn_readfirstlane(is_found) != 0;
 }
 
+// Token and query head of a tile's rows.  Row r of the tile is row rem + r of those from token j0 on; below
+// 2^21 the quotient by the group is exact as a product with its reciprocal (a half is added: the
+// quotient is then at least 1 / 2 group from a whole number).
+struct KvRowMap {
+  int j0, rem, group;
+  float inv;
+  __device__ __forceinline__ KvRowMap(int row0, int group) : group(group), inv(1.0f / static_cast<float>(group)) {
+    j0 = row0 / group;
+    rem = row0 - j0 * group;
+  }
+  __device__ __forceinline__ int token(int r) const {
+    return j0 + static_cast<int>((static_cast<float>(rem + r) + 0.5f) * inv);
+  }
+  __device__ __forceinline__ int member(int r, int j) const { return rem + r - (j - j0) * group; }
+};
+
 template <typename T>
 struct KvBlk {
   static constexpr int N = sizeof(T) == 2 ? 32 : 16;  // tokens of a wave's step
@@ -302,11 +318,15 @@ __device__ __forceinline__ void kv_mask(f32x4 (&s)[U], int tok, int pos, int win
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int t = tok + 4 * u + e;
-      const bool seen = t <= pos && (window <= 0 || t > pos - window || t < sinks);
-      s[u][e] = seen ? s[u][e] : -INFINITY;
-    }
+    for (int e = 0; e < 4; ++e) s[u][e] = tok + 4 * u + e <= pos ? s[u][e] : -INFINITY;
+  if (window > 0)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int t = tok + 4 * u + e;
+        s[u][e] = t > pos - window || t < sinks ? s[u][e] : -INFINITY;
+      }
 }
 
 // Scores of a row to weights relative to the running maximum m, with l their sum; where the
@@ -383,8 +403,8 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   const int D = P.p.dim, G = P.group;
   const int row0 = it.tile * ROWS, rows = it.count * G;
   const int n_rows = rows - row0 < ROWS ? rows - row0 : ROWS;
-  const int j0 = row0 / G, j1 = (row0 + n_rows - 1) / G + 1;
-  const int p0 = it.start + j0, p1 = it.start + j1;  // positions of the tile's tokens
+  const KvRowMap map(row0, G);
+  const int p0 = it.start + map.j0, p1 = it.start + map.token(n_rows - 1) + 1;  // positions of the tile's tokens
   bool bad = !it.fine;
 
   // this lane's rows; their queries stay in registers for one row tile, else in LDS, where every wave
@@ -397,8 +417,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   for (int r = 0; r < R; ++r) {
     const int row = 16 * r + c;
     const bool real = row < n_rows;
-    const int rr = row0 + (real ? row : n_rows - 1);
-    const int j = rr / G, head = it.head * G + rr - j * G;
+    const int in = real ? row : n_rows - 1, j = map.token(in), head = it.head * G + map.member(in, j);
     pos[r] = it.start + j;
     const char* src = P.q.data + (it.first + j) * P.q.token + head * P.q.head;
 #pragma unroll
@@ -695,7 +714,7 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
         }
       }
     } else {
-      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      const int j = map.token(row), head = it.head * G + map.member(row, j);
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
       kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
@@ -720,6 +739,7 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
   for (int work = blockIdx.x; work < n; work += gridDim.x) {
     const KvItem it = kv_uniform(P.split[work / PER]);
     const int row0 = it.tile * ROWS, rows = it.count * G;
+    const KvRowMap map(row0, G);
     const int row = work % PER * JR + jr;
     const bool real = row0 + row < rows && it.slot >= 0 && it.slot + it.splits <= P.slots;
     float m = -INFINITY, l = 0.0f, o[NT];
@@ -779,7 +799,7 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[t] += f * sum_o[(w * JR + jr) * 16 + jc][t];
       }
-      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      const int j = map.token(row), head = it.head * G + map.member(row, j);
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
       kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
@@ -848,11 +868,11 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
   const int D = WHOLE ? DP : P.p.dim, G = P.group;
   const int row0 = it.tile * ROWS, rows = it.count * G;
   const int n_rows = rows - row0 < ROWS ? rows - row0 : ROWS;
-  const int j0 = row0 / G, j1 = (row0 + n_rows - 1) / G + 1;
-  const int p0 = it.start + j0, p1 = it.start + j1;
+  const KvRowMap map(row0, G);
+  const int p0 = it.start + map.j0, p1 = it.start + map.token(n_rows - 1) + 1;
   // this wave's rows and the positions of their tokens
   const int w0 = wave * 32 < n_rows ? wave * 32 : n_rows - 1, w1 = w0 + 31 < n_rows ? w0 + 31 : n_rows - 1;
-  const int wp0 = it.start + (row0 + w0) / G, wp1 = it.start + (row0 + w1) / G;
+  const int wp0 = it.start + map.token(w0), wp1 = it.start + map.token(w1);
   const bool idle = wave * 32 >= n_rows;
   bool bad = !it.fine;
 
@@ -861,8 +881,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = wave * 32 + 16 * r + c;
-    const int rr = row0 + (row < n_rows ? row : n_rows - 1);
-    const int j = rr / G, head = it.head * G + rr - j * G;
+    const int in = row < n_rows ? row : n_rows - 1, j = map.token(in), head = it.head * G + map.member(in, j);
     pos[r] = it.start + j;
     const char* src = P.q.data + (it.first + j) * P.q.token + head * P.q.head;
 #pragma unroll
@@ -1097,7 +1116,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     }
     const int row = wave * 32 + 16 * r + c;
     if (P.lse && g == 0 && row < n_rows) {
-      const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+      const int j = map.token(row), head = it.head * G + map.member(row, j);
       P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] =
           ((m[r] == -INFINITY ? 0.0f : m[r]) + log2f(l[r])) * KV_LN2;
     }
@@ -1109,7 +1128,7 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
     const int in = i + lane / PIECES, row = wave * 32 + in;
     if (row >= n_rows || piece * 8 >= D) continue;
     const uint4 x = *reinterpret_cast<const uint4*>(own + in * DP + ((2 * piece) ^ (in & 7) << 1) * 4);
-    const int rr = row0 + row, j = rr / G, head = it.head * G + rr - j * G;
+    const int j = map.token(row), head = it.head * G + map.member(row, j);
     *reinterpret_cast<uint4*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head + piece * 16) = x;
   }
 }
