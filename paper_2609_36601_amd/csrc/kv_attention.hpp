@@ -380,7 +380,7 @@ __device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float f,
 // heads a key head, R = 2: 440 us, 5.4); for one long sequence that and the join's launch behind
 // it (131,072 keys: 44 and 7 us); for few short ones the way to the first product (16 drafts 16 us,
 // of which the keys' bytes take 14 only if all are under way at once); in f32 the matrix products, at
-// an eighth of bf16's rate, and the blocks at both ends of a row's window (ragged tokens behind a
+// a sixteenth of bf16's rate, and the blocks at both ends of a row's window (ragged tokens behind a
 // window of 500: 82 us, 38 TFLOP/s over what the rows see).
 template <typename T, int DP, int R>
 __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_attention_kernel(KvAttnParams P) {
@@ -818,10 +818,11 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
 // that the 16 rows which a read touches lie in 16 different banks.  The values are transposed
 // by the read (ds_read_b64_tr_b16: 16 lanes read 4 tokens of 16 elements, and each gets
 // one element's 4 tokens).
-// What bounds it: vector instructions (7 for a matrix product: exponentials, their sums, the running
-// maximum) and the wait for the next tokens (one sequence of 16,384 tokens 750 TFLOP/s, on tiles that
-// are not exchanged 1,000); with ragged prompts the start of a workgroup, some 5 us, and the last ones
-// to end as well (16 of 2 to 2,500 tokens 285 us, 515 TFLOP/s).
+// What bounds it: three pipes that a wave uses in turn and two waves a SIMD overlap in part: matrix products (a
+// third of the time), vector instructions (2.4 for a product: exponentials, their sums, the running
+// maximum) and LDS (16 KB for 32 products), and the wait for the next tokens.  One sequence of
+// 16,384 tokens, 8 key heads, 16 query heads: 1,270 us, 866 TFLOP/s; 16 ragged ones of 2 to 2,500 tokens
+// 195 us, 755, with the start of a workgroup, some 5 us, and the last ones to end.
 template <int DP>
 struct KvPromptShared {
   alignas(1024) uint16_t k[2][64 * DP];
