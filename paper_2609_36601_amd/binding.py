@@ -204,8 +204,9 @@ def _dtype_code(dt):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream(torch.cuda.current_device()) if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:  # (the handle without a Stream object around it: 1.4 us a call, 0.4 without)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 def _rows(student, teacher, row_offset):
