@@ -741,7 +741,12 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
     const int row0 = it.tile * ROWS, rows = it.count * G;
     const KvRowMap map(row0, G);
     const int row = work % PER * JR + jr;
-    const bool real = row0 + row < rows && it.slot >= 0 && it.slot + it.splits <= P.slots;
+    // (token ranges that overlap, which are not allowed, can make more items than were launched, and entries that
+    // none of them wrote: what does not fit is left out)
+    const bool fits = it.slot >= 0 && it.splits > 0 && it.splits <= P.slots - it.slot && it.first >= 0 && it.count > 0 &&
+                      it.count <= P.n.n_tokens - it.first && it.head >= 0 && it.head < P.p.n_heads && it.tile >= 0 &&
+                      it.tile <= it.count * G / ROWS;
+    const bool real = fits && row0 + row < rows;
     float m = -INFINITY, l = 0.0f, o[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t] = 0.0f;

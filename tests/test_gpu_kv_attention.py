@@ -242,6 +242,17 @@ def test_calls_at_once_on_two_streams(saki_lib):
         assert all(torch.equal(g, want[i]) for g in got[i])
 
 
+@pytest.mark.parametrize("new", [3, 70])
+def test_ranges_that_overlap_stay_in_bounds(saki_lib, new):
+    """Not allowed, and what the rows get is open; no row behind the tokens is written."""
+    t, c, q, off, dense = make(saki_lib, BF, [3000] * 40, [new] * 40, 4, 2, 64, 16, 42)
+    offsets = torch.as_tensor([0, new] * 20 + [0], dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 7.0)
+    c.attention(1, q[:new], out=out[:new], offsets=offsets)
+    torch.cuda.synchronize()
+    assert (out[new:] == 7.0).all()
+
+
 def test_sequences_without_pages_get_nan(saki_lib):
     t, c, q, off, dense = make(saki_lib, BF, [50, 70, 20], [2, 2, 2], 3, 2, 64, 8, 23)
     want = c.attention(1, q, n_new=2)

@@ -193,6 +193,13 @@ def test_handle_refuses_what_does_not_fit():
             saki.rope(**dict(dict(rotary_dim=8, device="cpu"), **kw))
 
 
+def test_streams_of_other_devices_are_refused():
+    from types import SimpleNamespace
+    c = saki.PagedKV.alloc(2, 4, 8, 1, 1, 8, 64, device="cpu")
+    with pytest.raises(ValueError, match="a stream of cuda:1"):
+        c.reserve(1, stream=SimpleNamespace(device=torch.device("cuda:1")))
+
+
 def test_rope_scalings():
     f = saki.rope(64, device="cpu")
     assert f["freq"].shape == (32,) and f["amplitude"] == 1.0
