@@ -177,15 +177,15 @@ AttentionWs attention_ws(bool bf, int dp, int rows) {
 // of a sequence of mean length; past 64, and past what a tile takes where the sequences alone fill the
 // card (`full`), the kernel for prompts.  64 sequences, 2,000 keys, 8 key heads, us:
 //   rows                16   32   48   64   96  128    (heads of 128 elements)
-//   tiles of 16        101  118  159  201  285  370
-//   tiles of 32        105  107  129  132  180  228
-//   for prompts                  121  122  126  136
+//   tiles of 16        100  129  170  212  296  384
+//   tiles of 32        116  120  142  142  192  239
+//   for prompts                  122  122  128  128
 //   rows                16   32   48   64   96  128    (64)
-//   tiles of 16         51   64   85  111  160  213
-//   tiles of 64                   56   58  101  103
-//   for prompts                   84   83   86   90
-// Where they do not fill it, a half-empty workgroup that is split costs more: 4 sequences, 8,000 keys,
-// 64 rows of 128 elements 45 us in tiles of 32, 56 in the kernel for prompts.
+//   tiles of 16         65   76   98  124  173  223
+//   tiles of 64         66   69   70   74  112  113
+//   for prompts                   76   76   82   81
+// Where they do not fill it, half-empty workgroups gain nothing (4 sequences, 8,000 keys, 64 rows of 128
+// elements: 45 to 60 us in tiles of 32, 56 to 61 in the kernel for prompts).
 int attention_tiles(bool bf, int dp, int64_t mean, bool full) {
   const int most = bf ? kv_row_tiles<uint16_t>(dp) : kv_row_tiles<float>(dp);
   if (bf && dp <= 128 && (mean > 64 || (full && mean > 16 * most))) return KV_PROMPT_ROWS / 16;
