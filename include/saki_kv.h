@@ -41,7 +41,7 @@ extern "C" {
 typedef struct {
   int64_t n_seq;     /* sequences, 0 .. 2^24                                              */
   int64_t max_pages; /* pages a sequence can hold (the width of `pages`), >= 1; max_pages *
-                        page_size <= 2^30                                                 */
+                        page_size <= 2^30, n_seq * max_pages < 2^38                       */
   int64_t n_pages;   /* pages of the pool, 1 .. 2^30                                      */
   int32_t page_size; /* tokens per page: a power of two, 8 .. 1024                        */
   int32_t reserved;  /* must be 0                                                         */

@@ -9,7 +9,6 @@ namespace saki {
 
 namespace {
 
-constexpr int64_t MAX_SEQ = int64_t{1} << 24;
 constexpr int64_t MAX_TOKENS = int64_t{1} << 30;  // of a sequence's pages, and of `shift`
 constexpr int64_t MAX_FORKS = int64_t{1} << 20;   // pairs of a call: each is compared with all others
 constexpr int64_t MAX_THREADS = int64_t{1} << 32;  // a launch has fewer
@@ -21,12 +20,14 @@ bool off(const void* p, unsigned align) { return (reinterpret_cast<uintptr_t>(p)
 saki_status check_table(const saki_kv_table* t) {
   if (!t) return abi_fail(SAKI_E_NULLPTR, "table descriptor is NULL");
   if (t->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_kv_table.reserved must be 0");
-  if (t->n_seq < 0 || t->n_seq > MAX_SEQ) return abi_fail(SAKI_E_SHAPE, "n_seq outside [0, 2^24]");
+  if (t->n_seq < 0 || t->n_seq > KV_MAX_SEQ) return abi_fail(SAKI_E_SHAPE, "n_seq outside [0, 2^24]");
   if (t->n_pages < 1 || t->n_pages > MAX_TOKENS) return abi_fail(SAKI_E_SHAPE, "n_pages outside [1, 2^30]");
   if (t->page_size < 8 || t->page_size > 1024 || (t->page_size & (t->page_size - 1)) != 0)
     return abi_fail(SAKI_E_SHAPE, "page_size must be a power of two, 8 .. 1024");
   if (t->max_pages < 1 || t->max_pages > MAX_TOKENS / t->page_size)
     return abi_fail(SAKI_E_SHAPE, "max_pages < 1, or max_pages * page_size > 2^30");
+  // (n_seq <= 2^24 and max_pages <= 2^27)
+  if (t->n_seq * t->max_pages >= KV_MAX_ENTRIES) return abi_fail(SAKI_E_SHAPE, "n_seq * max_pages must be below 2^38");
   if (t->n_seq == 0) return SAKI_OK;
   if (!t->pages || !t->length || !t->held || !t->refs)
     return abi_fail(SAKI_E_NULLPTR, "pages, length, held and refs are required");
@@ -248,7 +249,7 @@ size_t kv_workspace_bytes(int op, int64_t n, int64_t m) {
   if (n <= 0 || m <= 0) return 0;
   switch (op) {
     case SAKI_OP_KV_RESERVE:
-      return n > MAX_SEQ || m > MAX_TOKENS ? 0 : static_cast<size_t>(reserve_ws(n, m).bytes);
+      return n > KV_MAX_SEQ || m > MAX_TOKENS ? 0 : static_cast<size_t>(reserve_ws(n, m).bytes);
     case SAKI_OP_KV_COMPACT:
       return m > MAX_TOKENS ? 0 : static_cast<size_t>(compact_ws(m).bytes);
     case SAKI_OP_KV_ATTENTION: {

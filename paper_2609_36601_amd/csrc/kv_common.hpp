@@ -59,10 +59,10 @@ __device__ __forceinline__ int kv_dpp(int x) {
   return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, true);
 }
 template <int CTRL, int ROWS>
-__device__ __forceinline__ long long kv_dpp(long long x) {
+__device__ __forceinline__ int64_t kv_dpp(int64_t x) {
   const unsigned lo = static_cast<unsigned>(kv_dpp<CTRL, ROWS>(static_cast<int>(x)));
   const unsigned hi = static_cast<unsigned>(kv_dpp<CTRL, ROWS>(static_cast<int>(x >> 32)));
-  return static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
 // Inclusive prefix sum over the lanes of a wave: within the rows of 16 by shifts, then each
@@ -79,9 +79,9 @@ __device__ __forceinline__ V kv_wave_scan(V x) {
 }
 
 __device__ __forceinline__ int kv_last(int x) { return __builtin_amdgcn_readlane(x, KV_WAVE - 1); }
-__device__ __forceinline__ long long kv_last(long long x) {
+__device__ __forceinline__ int64_t kv_last(int64_t x) {
   const unsigned lo = static_cast<unsigned>(kv_last(static_cast<int>(x))), hi = static_cast<unsigned>(kv_last(static_cast<int>(x >> 32)));
-  return static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
 template <typename V>

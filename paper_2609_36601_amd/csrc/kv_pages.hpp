@@ -9,6 +9,7 @@
 #pragma once
 
 #include "kv_common.hpp"
+#include "kv_count.hpp"
 
 namespace saki {
 
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / KV_WAVE), lane = tid & (KV_WAVE - 1);
   const int page_mask = (1 << t.shift) - 1;
   __shared__ int free_of[KV_PLAN_WAVES], list_lds[KV_LIST_LDS], long_from[KV_PLAN_NT];
-  __shared__ long long part[KV_PLAN_WAVES];
+  __shared__ int64_t part[KV_PLAN_WAVES];
   __shared__ unsigned long long bits[KV_BITS_PAGES / 64];
 
   // 1. what every sequence asks for (the loads of the first ones are under way while the
@@ -216,29 +217,23 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
       }
     }
   }
-  // 3. how much that is: the call takes all of it or nothing.  Pages in the lower half, copies
-  // in the upper half of a sum (no more pages are asked for than the table has entries, and 2^40
-  // of those would be 4 TB)
-  auto sum_of = [&](const KvWant& w) {
-    const long long copy = w.slot >= 0;
-    return (copy << 40) + w.fresh + copy;
-  };
-  constexpr long long PAGES = (1ll << 40) - 1;
+  // 3. how much that is: the call takes all of it or nothing (pages and copies in one sum: kv_count)
+  auto sum_of = [&](const KvWant& w) { return kv_count(w.slot >= 0, w.fresh); };
   const bool one = t.n_seq <= KV_PLAN_NT;  // each sequence has a thread
-  long long all = 0, at0 = 0;
+  int64_t all = 0, at0 = 0;
   if (one) {
-    at0 = kv_block_scan<KV_PLAN_NT, long long>(sum_of(first_want), part, &all);
+    at0 = kv_block_scan<KV_PLAN_NT, int64_t>(sum_of(first_want), part, &all);
   } else {
-    long long mine = 0;
+    int64_t mine = 0;
     for (int b = tid; b < t.n_seq; b += KV_PLAN_NT) mine += sum_of(want_of(b));
-    kv_block_scan<KV_PLAN_NT, long long>(mine, part, &all);
+    kv_block_scan<KV_PLAN_NT, int64_t>(mine, part, &all);
   }
   int before = 0, n_free = 0;
   for (int w = 0; w < KV_PLAN_WAVES; ++w) {
     if (w < wave) before += free_of[w];
     n_free += free_of[w];
   }
-  const bool enough = (all & PAGES) <= n_free;
+  const bool enough = kv_count_pages(all) <= n_free;
   if (P.status) {
     if (tid < t.n_seq)
       P.status[tid] = static_cast<uint8_t>(!enough && n0 > 0 && first_status == SAKI_KV_OK ? SAKI_KV_NO_PAGES : first_status);
@@ -246,8 +241,8 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
       for (int b = tid + KV_PLAN_NT; b < t.n_seq; b += KV_PLAN_NT)
         if (asked_of(b) > 0 && P.status[b] == SAKI_KV_OK) P.status[b] = SAKI_KV_NO_PAGES;
   }
-  const int total = enough ? static_cast<int>(all & PAGES) : 0;
-  if (tid == 0) *P.n_moves = enough ? static_cast<int>(all >> 40) : 0;
+  const int total = enough ? static_cast<int>(kv_count_pages(all)) : 0;
+  if (tid == 0) *P.n_moves = enough ? static_cast<int>(kv_count_copies(all)) : 0;
   if (total == 0) return;
   // 4. the lowest `total` free pages, ascending
   const bool in_lds = total <= KV_LIST_LDS;
@@ -276,19 +271,19 @@ __global__ __launch_bounds__(KV_PLAN_NT) void kv_reserve_kernel(KvReserveParams 
   __syncthreads();
   auto taken = [&](int i) { return in_lds ? list_lds[i] : P.list[i]; };
   // 5. each sequence its share, in order; long shares by whole waves
-  long long done = 0;
+  int64_t done = 0;
   for (int b0 = 0; b0 < t.n_seq; b0 += KV_PLAN_NT) {
     const int b = b0 + tid;
     const KvWant w = b < t.n_seq ? want_of(b) : KvWant{-1, -1, 0, 0};
     const bool copy = w.slot >= 0;
-    long long sum = 0;
-    const long long at = done + (one ? at0 : kv_block_scan<KV_PLAN_NT, long long>(sum_of(w), part, &sum));
+    int64_t sum = 0;
+    const int64_t at = done + (one ? at0 : kv_block_scan<KV_PLAN_NT, int64_t>(sum_of(w), part, &sum));
     done += sum;
-    int from = static_cast<int>(at & PAGES);
+    int from = static_cast<int>(kv_count_pages(at));
     const int64_t row = static_cast<int64_t>(b) * t.max_pages;
     if (copy) {
       const int to = taken(from);
-      P.moves[at >> 40] = KvMove{w.page, to, w.fill};
+      P.moves[kv_count_copies(at)] = KvMove{w.page, to, w.fill};
       t.pages[row + w.slot] = to;
       t.refs[to] = 1;
       atomicSub(&t.refs[w.page], 1);
