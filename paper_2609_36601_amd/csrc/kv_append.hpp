@@ -57,19 +57,35 @@ __device__ __forceinline__ void kv_store8(T* p, const Kv8<T>& r) {
   for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) d[i] = u[i];
 }
 
-// The sequence whose rows hold `row`: the largest b with offsets[b] <= row, found
-// by the whole workgroup in steps of 256 candidates.
-__device__ __forceinline__ int kv_find_sequence(const KvTokens& T, int n_seq, int row) {
+// The sequence whose rows hold `row`, or -1, and its first row, found by the whole workgroup: the largest b with
+// offsets[b] <= row, in steps of 256 candidates.  That is the one if the offsets are in order; where its range
+// does not hold the row (a row of no sequence, or a range somewhere that is out of order and counts as
+// empty), every range is looked at.
+__device__ __forceinline__ int kv_find_sequence(const KvTokens& T, int n_seq, int row, int* first) {
   int lo = 0, n = n_seq;  // among lo .. lo + n - 1
   while (n > 1) {
     const int step = (n + KV_APPEND_NT - 1) / KV_APPEND_NT;
     const int at = static_cast<int>(threadIdx.x) * step;
     const int below = __syncthreads_count(at < n && T.offsets[lo + at] <= row);
-    if (below == 0) return lo;
+    if (below == 0) break;
     lo += (below - 1) * step;
     n = n - (below - 1) * step < step ? n - (below - 1) * step : step;
   }
-  return lo;
+  auto holds = [&](int b, int* first) {
+    int count;
+    kv_rows(T, b, first, &count);
+    return row >= *first && row - *first < count;
+  };
+  if (holds(lo, first)) return lo;
+  __shared__ int found;
+  if (threadIdx.x == 0) found = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < n_seq; b += KV_APPEND_NT)
+    if (holds(b, first)) atomicMax(&found, b);  // (one b, unless ranges overlap, which they may not)
+  __syncthreads();
+  const int b = found;
+  if (b >= 0) *first = T.offsets[b];
+  return b;
 }
 
 // One workgroup per token.  The angles of the token's pairs are formed once, in
@@ -131,10 +147,14 @@ __global__ __launch_bounds__(KV_APPEND_NT) void kv_append_kernel(KvAppendParams 
   for (int i = 0; i < KV_AHEAD; ++i)
     if (tid + i * KV_APPEND_NT < total) ahead[i] = load(tid + i * KV_APPEND_NT);
 
-  const int b = P.n.offsets ? kv_find_sequence(P.n, P.t.n_seq, row) : row / P.n.n_new;
-  int first, count;
-  kv_rows(P.n, b, &first, &count);
-  if (row < first || row >= first + count) return;  // the whole workgroup
+  int b, first;
+  if (P.n.offsets) {
+    b = kv_find_sequence(P.n, P.t.n_seq, row, &first);
+    if (b < 0) return;  // the whole workgroup
+  } else {
+    b = row / P.n.n_new;
+    first = b * P.n.n_new;
+  }
   const int64_t pos = static_cast<int64_t>(P.t.length[b]) + P.n.shift + (row - first);
   const int64_t slot_page = pos >> P.t.shift;
   int page = -1;
