@@ -172,8 +172,11 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  *   out = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j exp(scale q . k_j).
  * Keys and values at positions that a token does not see have no influence on
  * it, whatever they hold.  A token whose every score is -infinity gets out = 0,
- * lse = -infinity, one with a score of NaN or +infinity gets NaN.  Tokens of a
- * sequence that lacks pages for them get NaN.
+ * lse = -infinity, whatever the values hold; one with a score of NaN or +infinity gets NaN.
+ * Where a token gives a key that it sees the weight 0 (a score of -infinity beside finite
+ * ones, or some 100 below the largest), it is open whether a value there that is not
+ * finite makes the element NaN or has no influence.  Tokens of a sequence that lacks pages
+ * for them get NaN.
  * Products and softmax are accumulated in 32 bits; with bf16 the weights are
  * rounded to bf16 for their product with the values.
  *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads / 16

@@ -361,15 +361,18 @@ __device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float
     }
 }
 
-// N elements o[i] * f of a row, of which those below `left` are there (a multiple of 8).
+// N elements o[i] / sum of a row, of which those below `left` are there (a multiple of 8); 0 for a row without
+// any weight (o may still not be finite: 0 times a value that is not).
 template <typename T, int N>
-__device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float f, int left) {
+__device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float sum, int left) {
+  const bool none = sum == 0.0f;
+  const float f = 1.0f / sum;
 #pragma unroll
   for (int t = 0; t < N; t += 4)
     if (t < left) {
       T y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) kv_put(&y[e], o[t + e] * f);
+      for (int e = 0; e < 4; ++e) kv_put(&y[e], none ? 0.0f : o[t + e] * f);
       __builtin_memcpy(__builtin_assume_aligned(dst + t, 4 * sizeof(T)), y, sizeof(y));
     }
 }
@@ -717,9 +720,8 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
       }
     } else {
       const int j = map.token(row), head = it.head * G + map.member(row, j);
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-      kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
+      kv_put_row(dst + jc * NT, o, sum, D - jc * NT);
       if (P.lse && jc == 0)
         P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
     }
@@ -807,9 +809,8 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
         for (int t = 0; t < NT; ++t) o[t] += f * sum_o[(w * JR + jr) * 16 + jc][t];
       }
       const int j = map.token(row), head = it.head * G + map.member(row, j);
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       T* dst = reinterpret_cast<T*>(P.out.data + (it.first + j) * P.out.token + head * P.out.head);
-      kv_put_row(dst + jc * NT, o, inv, D - jc * NT);
+      kv_put_row(dst + jc * NT, o, sum, D - jc * NT);
       if (P.lse && jc == 0)
         P.lse[static_cast<int64_t>(it.first + j) * P.n_q_heads + head] = (ref + log2f(sum)) * KV_LN2;
     }
@@ -1125,13 +1126,14 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
   uint16_t* own = &sh.k[0][0] + wave * 32 * DP;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+    const bool none = l[r] == 0.0f;  // (as in kv_put_row)
+    const float inv = 1.0f / l[r];
     // (pieces of 8 bytes, permuted as the keys' of 16)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       uint16_t y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = kv_to_bf16(acc[r][t][e] * inv);
+      for (int e = 0; e < 4; ++e) y[e] = kv_to_bf16(none ? 0.0f : acc[r][t][e] * inv);
       __builtin_memcpy(__builtin_assume_aligned(own + (16 * r + c) * DP + ((4 * t + g) ^ (c & 7) << 1) * 4, 8), y, 8);
     }
     const int row = wave * 32 + 16 * r + c;
