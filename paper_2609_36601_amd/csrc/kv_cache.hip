@@ -484,9 +484,9 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   P.lse = lse;
   P.n_q_heads = n_q_heads;
   P.group = group;
-  // (not 0: a hidden score is -infinity, which 0 would make a NaN.  2^-126 leaves any score of finite
-  // bf16 products, and f32 ones below 2^100, without influence)
-  P.scale2 = std::max(fabsf(scale) * KV_LOG2E, 0x1p-126f);
+  // (not 0: a hidden score is -infinity, which 0 would make a NaN)
+  P.zero = scale == 0.0f;
+  P.scale2 = P.zero ? 1.0f : fabsf(scale) * KV_LOG2E;
   P.flip = scale < 0.0f ? (bf ? 0x80008000u : 0x80000000u) : 0u;
   P.window = window;
   P.sinks = sinks;

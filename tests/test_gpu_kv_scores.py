@@ -26,3 +26,33 @@ def test_no_score_above_minus_infinity_over_values_of_any_kind(saki_lib, dtype, 
     out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV)
     c.attention(1, q, out=out, lse=lse, n_new=new)
     assert bool((out == 0).all()) and bool((lse == -INF).all())
+
+
+@pytest.mark.parametrize("dtype,dim,lengths,new", [(BF, 128, [70, 5, 200], 2), (F32, 64, [70, 5, 200], 2),
+                                                   (BF, 64, [3, 100], 140), (BF, 128, [0, 65], 130), (BF, 256, [40, 9], 3),
+                                                   (F32, 256, [40, 9], 20)])
+@pytest.mark.parametrize("power", [0, 61, 64])
+def test_a_scale_of_zero_weighs_all_alike(saki_lib, dtype, dim, lengths, new, power):
+    """Whatever the size of the products (2^power for each factor: past 2^127 together), in 64 bits or not."""
+    t, c, q, off, dense = make(saki_lib, dtype, lengths, [new] * len(lengths), 2, 2, dim, 16, dim + new, scale_q=2.0**power)
+    for b, (kb, vb) in enumerate(dense):
+        kb.mul_(2.0**power)
+        put(t, b, c.k, c.v, kb, vb)
+    print(f"scale 0: {dtype} dim {dim} power {power}", flush=True)
+    run(saki_lib, t, c, q, off, dense, scale=0.0, uniform=new, rows=5)
+    run(saki_lib, t, c, q, off, dense, scale=-0.0, uniform=new, window=21, sinks=2, rows=5)
+    q[1, 0, 3], q[2, 1, 0] = INF, NAN  # 0 times these is not 0
+    dense[0][0][2, 0, 5] = INF
+    put(t, 0, c.k, c.v, *dense[0])
+    run(saki_lib, t, c, q, off, dense, scale=0.0, uniform=new, rows=5)
+
+
+@pytest.mark.parametrize("dtype,new", [(BF, 2), (F32, 2), (BF, 140)])
+@pytest.mark.parametrize("scale", [2.0**-128, -(2.0**-131), 2.0**-126])
+def test_scales_of_the_lowest_size(saki_lib, dtype, new, scale):
+    """Scales below 2^-126 on products near 2^126."""
+    t, c, q, off, dense = make(saki_lib, dtype, [70, 5], [new] * 2, 2, 2, 64, 16, 5, scale_q=2.0**61)
+    for b, (kb, vb) in enumerate(dense):
+        kb.mul_(2.0**61)
+        put(t, b, c.k, c.v, kb, vb)
+    run(saki_lib, t, c, q, off, dense, scale=scale, uniform=new, rows=9)
