@@ -182,7 +182,7 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads / 16
  *              + n_seq * n_kv_heads below 2^24 - 8192 (more may be SAKI_E_SHAPE)
  *   out        as q; may be q itself.  lse: float [n_tokens, n_q_heads] or NULL
- *   scale      finite;  window >= 0 (0: none);  sinks >= 0
+ *   scale      -2^127 .. 2^127;  window >= 0 (0: none);  sinks >= 0
  *   ws         saki_workspace_bytes(SAKI_OP_KV_ATTENTION, n_tokens * n_q_heads, head_dim)
  *              bytes, 16-byte aligned; calls that may run at the same time need
  *              separate workspaces */

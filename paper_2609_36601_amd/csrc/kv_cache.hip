@@ -453,7 +453,8 @@ saki_status saki_kv_attention(const saki_kv_table* table, const saki_kv_pool* po
   if (st != SAKI_OK) return st;
   if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % pool->n_kv_heads != 0)
     return abi_fail(SAKI_E_SHAPE, "n_q_heads must be a multiple of n_kv_heads, at most 65536");
-  if (!isfinite(scale)) return abi_fail(SAKI_E_VALUE, "scale is not finite");
+  // (a larger one times log2 e would be infinite in 32 bits)
+  if (!(fabsf(scale) <= 0x1p127f)) return abi_fail(SAKI_E_VALUE, "scale must be within -2^127 .. 2^127");
   if (window < 0 || sinks < 0) return abi_fail(SAKI_E_VALUE, "window < 0 or sinks < 0");
   if (off(lse, 4)) return abi_fail(SAKI_E_ALIGN, "lse must be 4-byte aligned");
   if (table->n_seq == 0 || tokens->n_tokens == 0) return abi_ok();

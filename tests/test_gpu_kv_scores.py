@@ -56,3 +56,16 @@ def test_scales_of_the_lowest_size(saki_lib, dtype, new, scale):
         kb.mul_(2.0**61)
         put(t, b, c.k, c.v, kb, vb)
     run(saki_lib, t, c, q, off, dense, scale=scale, uniform=new, rows=9)
+
+
+@pytest.mark.parametrize("dtype,new", [(BF, 2), (F32, 2), (BF, 140)])
+def test_the_largest_scale(saki_lib, dtype, new):
+    """2^127 on products of -2^-124 .. 2^-124 (none below 2^-126), some of them 0."""
+    t, c, q, off, dense = make(saki_lib, dtype, [70, 5], [new] * 2, 2, 2, 64, 16, 6)
+    q.copy_(torch.where(q > 0, 2.0**-64, -(2.0**-64)) * torch.where(q.abs() > 0.7, 1.0, 0.5))
+    for b, (kb, vb) in enumerate(dense):
+        one = torch.nn.functional.one_hot(torch.arange(kb.shape[0], device=DEV) * 7 % 64, 64)[:, None]
+        kb.copy_(torch.where(kb > 0, 2.0**-60, -(2.0**-60)) * one)
+        kb[::5] = 0
+        put(t, b, c.k, c.v, kb, vb)
+    run(saki_lib, t, c, q, off, dense, scale=2.0**127, uniform=new, rows=9)
