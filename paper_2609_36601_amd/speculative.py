@@ -21,8 +21,11 @@ the law of sequential exact-q sampling (App. F, Prop. spec_exact).
     logits_into(states, s_out, t_out)   student / teacher logits of the
                                         prefixes, written into [n, V] views
 (workloads.SyntheticARTorch is a synthetic one).  Networks that keep key-value
-caches have instead of initial, advance and logits_into
-    caches                         the networks' cache.PagedKV, B sequences each
+caches have instead of initial, advance and logits_into (an attribute `caches`
+without the three calls below it is the model's own matter)
+    caches                         the networks' cache.PagedKV, B sequences each,
+                                   with room for a prompt and max_len + k - 2
+                                   tokens behind it
     start(prompts) -> last token of each prompt, int64 [B]; each cache then
                                    holds the prompts without their last tokens
                                    (equal prompts may share pages: PagedKV.fork)
@@ -52,6 +55,14 @@ META_FIELDS = ["lambda", "kl", "tv", "logp_token", "logt_token", "teacher_argmax
 OBJECTIVE_FIELDS = ["logp_token", "logt_token", "teacher_argmax", "token", "corrected", "row_status"]
 
 
+def _caches(model):
+    """The caches that the driver keeps with the trajectories: those of a model that has the calls for them."""
+    if not all(callable(getattr(model, f, None)) for f in ("start", "draft_into", "verify_into")):
+        return ()
+    caches = getattr(model, "caches", None)
+    return () if caches is None else tuple(caches)
+
+
 def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat16,
             check_every=1, max_waves=None, stream=None, timing=None, metadata="full"):
     """Runs waves until every sequence is done; returns (trajectories, waves).
@@ -74,7 +85,7 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
     if max_len <= 0:
         traj["done"].fill_(_b.SEQ_FINISHED)
         return traj, 0
-    caches = getattr(model, "caches", ())
+    caches = _caches(model)
     if caches and stream is not None:
         raise ValueError("a model with caches runs on the current stream")
     # logits of the B * k draft prefixes, block-major rows b * k + j
