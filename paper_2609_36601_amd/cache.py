@@ -47,7 +47,8 @@ _HERE = contextlib.nullcontext()
 class PagedKV:
     """A cache: tensors k, v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (any order of the
     first four axes in memory), pages [n_seq, max_pages], length [n_seq], held [n_seq], refs [n_pages]
-    (int32; the table, see saki_kv_table).  The tensors are the caller's; PagedKV.alloc makes empty ones."""
+    (int32; the table, see saki_kv_table).  The tensors are the caller's; PagedKV.alloc makes empty ones.
+    A cache takes no part in autograd: tensors that record their history are refused (torch.no_grad())."""
 
     def __init__(self, k, v, pages, length, held, refs):
         if refs.device != k.device or pages.device != k.device:
@@ -116,6 +117,8 @@ class PagedKV:
             raise ValueError(f"{name} must be [{n_tokens}, {heads}, {self.head_dim}]: got {tuple(t.shape)}")
         if t.dtype != self.dtype or t.device != self.device:
             raise ValueError(f"{name} must be {self.dtype} on {self.device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, and a cache passes none on: call under torch.no_grad()")
 
     # -- pages -----------------------------------------------------------------
     def reserve(self, n_new, stream=None):

@@ -103,8 +103,12 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
     corr = torch.empty(B, dtype=torch.int32, device=dev)
     n_commit = torch.empty(B, dtype=torch.int32, device=dev)
     ws = torch.empty(max(_b.workspace_bytes(_b.SAKI_OP_VERIFY, B * k, V), 8), dtype=torch.uint8, device=dev)
-    # what the model continues from: its state, or with caches the last token
-    state = model.start(prompts) if caches else model.initial(prompts)
+    # what the model continues from: its state, or with caches (which take no part in autograd) the last token
+    if caches:
+        with torch.no_grad():
+            state = model.start(prompts)
+    else:
+        state = model.initial(prompts)
     if caches:
         wanting = torch.full((B,), k, dtype=torch.int32, device=dev)  # tokens of the wave
         lacking = torch.zeros((), dtype=torch.bool, device=dev)
@@ -129,7 +133,8 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
             lacking |= (timed("cache", c.reserve, wanting) != _b.KV_OK).any()
         for j in range(k):
             if caches:
-                model.draft_into(H[:, j], j, S3[:, j])
+                with torch.no_grad():
+                    model.draft_into(H[:, j], j, S3[:, j])
             else:
                 model.logits_into(H[:, j], S3[:, j], None)
             timed("sample", _b.saki_sample, S3[:, j], D[j], seed, row_offset=g0 + j, row_step=k,
@@ -138,7 +143,8 @@ def rollout(model, prompts, k, max_len, eps, seed, eos_id=-1, dtype=torch.bfloat
             H[:, j + 1] = drafted if caches else model.advance(H[:, j], drafted)
         drafts.copy_(D.t())
         if caches:
-            model.verify_into(H[:, :k], T)
+            with torch.no_grad():
+                model.verify_into(H[:, :k], T)
         else:
             model.logits_into(H[:, :k].reshape(-1), None, T)
         timed("verify", _b.saki_spec_verify, S, T, k, drafts.view(-1), eps, seed, row_offset=g0,
