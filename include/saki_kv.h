@@ -177,8 +177,10 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  * ones, or some 100 below the largest), it is open whether a value there that is not
  * finite makes the element NaN or has no influence.  Tokens of a sequence that lacks pages
  * for them get NaN.
- * Products and softmax are accumulated in 32 bits; with bf16 the weights are
- * rounded to bf16 for their product with the values.
+ * Products and softmax are accumulated in 32 bits.  With bf16 the weights are rounded for
+ * their product with the values: to 2^-17 of a weight in calls of up to 32 rows (new
+ * tokens times the query heads of a key head) a sequence on average, and with heads of
+ * more than 128 elements; to bf16, 2^-9, in others.
  *   n_q_heads  a multiple of pool->n_kv_heads, at most 65536; n_tokens * n_q_heads / 16
  *              + n_seq * n_kv_heads below 2^24 - 8192 (more may be SAKI_E_SHAPE)
  *   out        as q; may be q itself.  lse: float [n_tokens, n_q_heads] or NULL

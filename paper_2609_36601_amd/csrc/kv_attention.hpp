@@ -374,6 +374,23 @@ __device__ __forceinline__ void kv_soften(f32x4 (&s)[U], f32x4 (&acc)[NT], float
     }
 }
 
+// A lane's eight weights (>= 0, or NaN) as sums of two bf16 numbers: the largest bf16 number below a weight, and the rest,
+// which is rounded, 2^-17 of the weight at most.  Both parts of a weight that is not 0 are above 0, so that their products
+// with an infinite value are that infinity, and not the NaN of 0 or of opposite signs.
+__device__ __forceinline__ void kv_halves(const f32x4 (&s)[2], bf16x8* high, bf16x8* low) {
+  uint32_t h[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t x = __float_as_uint(s[e >> 2][e & 3]);
+    h[e] = (x > 1u ? x : 1u) - 1u;
+    (*low)[e] = static_cast<__bf16>(s[e >> 2][e & 3] - __uint_as_float(h[e] & 0xffff0000u));
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(h[2 * e + 1], h[2 * e], 0x07060302u);
+  *high = __builtin_bit_cast(bf16x8, uint4{w[0], w[1], w[2], w[3]});
+}
+
 // N elements o[i] / sum of a row, of which those below `left` are there (a multiple of 8); 0 for a row without
 // any weight (o may still not be finite: 0 times a value that is not).
 template <typename T, int N>
@@ -408,6 +425,9 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
   constexpr int NT = DP / 16;              // 16-wide tiles of the head: a lane's elements of a value row
   constexpr int QC = BF ? DP / 32 : DP / 16;  // 16-byte pieces of a lane's share of a key row
   constexpr int TOK = BF ? 8 : 4;          // tokens of a lane in a block
+  // Weights as two bf16 numbers: their second products are free where memory bounds the kernel (16 rows: 0 to 1%, 32 rows
+  // 0 to 3%), not with four row tiles (64 rows of 64-element heads 53 -> 60 us).
+  constexpr bool HALVES = BF && R <= 2;
   constexpr int VW = NT * sizeof(T) / 4;   // 32-bit words of a lane's share of a value row
   using VPiece = typename std::conditional<(VW >= 4), uint4, uint2>::type;
   constexpr int VC = VW * 4 / sizeof(VPiece), VE = sizeof(VPiece) / sizeof(T);  // its loads, elements of a load
@@ -626,12 +646,16 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
             }
         }
       }
-      bf16x8 pf[R];
-      if constexpr (BF)
+      bf16x8 pf[R], pl[R];
+      if constexpr (HALVES) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) kv_halves(s[r], &pf[r], &pl[r]);
+      } else if constexpr (BF) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int e = 0; e < 8; ++e) pf[r][e] = static_cast<__bf16>(s[r][e >> 2][e & 3]);
+      }
       // x += V^T P^T, tile t of the values
       auto multiply = [&](int t, f32x4(&x)[R]) {
         if constexpr (BF) {
@@ -642,6 +666,9 @@ __global__ __launch_bounds__(KV_ATT_NT, kv_groups_per_cu<T>(DP, R)) void kv_atte
           const bf16x8 a = __builtin_bit_cast(bf16x8, uint4{w[0], w[1], w[2], w[3]});
 #pragma unroll
           for (int r = 0; r < R; ++r) x[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[r], x[r], 0, 0, 0);
+          if constexpr (HALVES)
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl[r], x[r], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -1066,6 +1093,8 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 #pragma unroll
           for (int t = 0; t < NT; ++t) a[t] = kv_part<0>(a[t]);
       }
+      // (weights as one bf16 number: two cost 29% here, 16,384 tokens 1,260 us -> 1,625, and the rounding, 2^-9 of a
+      // weight in no common direction, adds some 8% to the error that the output's own has over 1,250 keys)
       bf16x8 pf[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
