@@ -95,10 +95,14 @@ __device__ __forceinline__ int kv_find_sequence(const KvTokens& T, int n_seq, in
 // elements pair up, so that a row may be rotated in place.  VEC: runs of 8 pair
 // up whole (half layout: rotary_dim / 2 a multiple of 8; interleaved: rotary_dim a
 // multiple of 8); else a thread takes single pairs.
+// The cosine, the sine and the rotation itself are in 32 bits, for 32-bit rows too: an element is then off by 2^-20 of
+// its pair's size at most (rms 5.6e-8, of which the row's own rounding is 2.5e-8).  64 bits take 7% to 13% more where that
+// is not hidden behind memory (a verification of 8 sequences 11.4 us -> 12.3, 33,000 tokens in single pairs 563 -> 637).
 // What bounds it: memory, and for few tokens the chain of lookups (the row's sequence, its length,
 // page and the page's count); a thread's first KV_AHEAD loads are under way meanwhile (32 ragged
 // prompts, 33,000 tokens of 32 + 8 heads of 128 bf16 elements: 203 us without, 188 with:
-// 4.3 TB/s of the 4.8 that a large copy reaches).
+// 4.3 TB/s of the 4.8 that a large copy reaches; in f32 346 us, 4.7).  Single pairs: accesses of one element
+// (heads of 96 elements, 24 of them rotated: bf16 446 us, 1.4 TB/s, f32 563, 2.2; of 80, 20 rotated, bf16 376, 1.4).
 constexpr int KV_AHEAD = 3;
 
 template <typename T, bool INTERLEAVED, bool VEC>
