@@ -411,8 +411,8 @@ __device__ __forceinline__ void kv_put_row(T* dst, const float (&o)[N], float su
 // running maximum and sum of its own until the end: no barrier between blocks, and every wave's
 // loads, a block ahead, go from memory straight to the registers that the products read.
 // What bounds it: reading the keys and values (512 drafts over 4,480 keys, 8 + 8 heads of 128 bf16
-// elements: 1,555 us, 6.0 TB/s, what a large read reaches; 128 verifications of 8 tokens by 4 query
-// heads a key head, R = 2: 440 us, 5.4); for one long sequence that and the join's launch behind
+// elements: 1,560 us, 6.0 TB/s, what a large read reaches; 128 verifications of 8 tokens by 4 query
+// heads a key head, R = 2: 444 us, 5.3); for one long sequence that and the join's launch behind
 // it (131,072 keys: 44 and 7 us); for few short ones the way to the first product (16 drafts 16 us,
 // of which the keys' bytes take 14 only if all are under way at once); in f32 the matrix products, at
 // a sixteenth of bf16's rate, and the blocks at both ends of a row's window (ragged tokens behind a
@@ -875,12 +875,14 @@ __global__ __launch_bounds__(KV_ATT_NT) void kv_join_kernel(KvAttnParams P) {
 // in memory, but its 16-byte pieces are permuted: piece p of a row is at p ^ kv_swizzle(row), so
 // that the 16 rows which a read touches lie in 16 different banks.  The values are transposed
 // by the read (ds_read_b64_tr_b16: 16 lanes read 4 tokens of 16 elements, and each gets
-// one element's 4 tokens).
+// one element's 4 tokens).  The banks differ for the reads of keys; of values, four lanes read two neighbouring pieces of a
+// row, and two rows' pieces each lie in the same banks: a two-way conflict on every read (9.5e6 of the 29.4e6 cycles
+// in which the LDS is active, 16 ragged prompts).
 // What bounds it: three pipes that a wave uses in turn and two waves a SIMD overlap in part: matrix products (a
 // third of the time), vector instructions (2.4 for a product: exponentials, their sums, the running
 // maximum) and LDS (16 KB for 32 products), and the wait for the next tokens.  One sequence of
-// 16,384 tokens, 8 key heads, 16 query heads: 1,270 us, 866 TFLOP/s; 16 ragged ones of 2 to 2,500 tokens
-// 195 us, 755, with the start of a workgroup, some 5 us, and the last ones to end.
+// 16,384 tokens, 8 key heads, 16 query heads: 1,276 us, 862 TFLOP/s; 16 ragged ones of 1 to 2,500 tokens
+// 197 us, 717, with the start of a workgroup, some 5 us, and the last ones to end.
 template <int DP>
 struct KvPromptShared {
   alignas(1024) uint16_t k[2][64 * DP];
@@ -1093,8 +1095,8 @@ __global__ __launch_bounds__(KV_ATT_NT, 2) void kv_prompt_kernel(KvAttnParams P)
 #pragma unroll
           for (int t = 0; t < NT; ++t) a[t] = kv_part<0>(a[t]);
       }
-      // (weights as one bf16 number: two cost 29% here, 16,384 tokens 1,260 us -> 1,625, and the rounding, 2^-9 of a
-      // weight in no common direction, adds some 8% to the error that the output's own has over 1,250 keys)
+      // (weights as one bf16 number: two cost 29% here, 16,384 tokens 1,260 us -> 1,625; the rounding, 2^-9 of a weight,
+      // takes the error of 16 ragged prompts from 1.6e-3, the output's own, to 1.9e-3)
       bf16x8 pf[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {

@@ -35,7 +35,8 @@ without the three calls below it is the model's own matter)
                                    [B, k], appended from position length on
 The driver then reserves the pages of a wave before it and commits the caches
 with the trajectories: the tokens behind the first rejection are dropped and
-their pages given back, and a finished sequence gives back all of its pages
+their pages given back, and a finished sequence gives back all of its pages:
+the rows of finished sequences are NaN behind append and attention, and ignored
 (workloads.SyntheticAttentionPair is a synthetic one).
 
 Keying: draft j of sequence b in wave w and its verification share the
