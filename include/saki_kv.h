@@ -173,8 +173,8 @@ saki_status saki_kv_append(const saki_kv_table *table, const saki_kv_pool *pool,
  * Keys and values at positions that a token does not see have no influence on
  * it, whatever they hold.  A token whose every score is -infinity gets out = 0,
  * lse = -infinity, whatever the values hold; one with a score of NaN or +infinity gets NaN.
- * Where a token gives a key that it sees the weight 0 (a score of -infinity beside finite
- * ones, or some 100 below the largest), it is open whether a value there that is not
+ * Where a token gives a key that it sees no weight in 32 bits (a score of -infinity beside
+ * finite ones, or some 85 below the largest), it is open whether a value there that is not
  * finite makes the element NaN or has no influence.  Tokens of a sequence that lacks pages
  * for them get NaN.
  * Products and softmax are accumulated in 32 bits.  With bf16 the weights are rounded for
