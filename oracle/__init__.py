@@ -21,6 +21,7 @@ supervision  teacher-sampled correction targets (App. C) and the Random-TM /
           TV-Weighted-TM placement controls (Sec. 4.1, placement-control
           appendix).
 probe     fixed-prefix probe metrics C_1, C_k, KL(T || S), H(S).
+distill   top logits, the divergence from them, cross entropy from hidden states.
 rollout   multi-wave speculative rollout: drafting, verification,
           first-rejection commit and rollback, token-aligned metadata
           (Sec. 3.5, App. F Prop. spec_exact, App. I).

@@ -1,4 +1,4 @@
-"""ctypes binding of libsaki.so (include/saki.h, saki_kv.h).
+"""ctypes binding of libsaki.so (include/saki.h, saki_kv.h, saki_distill.h).
 
 Argument marshalling only: every step of the path runs in the HIP library.
 Tensors are torch device tensors; the library sees their data pointers and the
@@ -16,12 +16,14 @@ LIB_PATH = os.path.join(HERE, "libsaki.so")
 SAKI_F32, SAKI_BF16 = 0, 1
 SAKI_OP_COUPLE, SAKI_OP_ROUTE, SAKI_OP_VERIFY, SAKI_OP_SELECT = 0, 1, 2, 3
 SAKI_OP_KV_RESERVE, SAKI_OP_KV_COMPACT, SAKI_OP_KV_ATTENTION = 4, 5, 6
+SAKI_OP_TOP_LOGITS, SAKI_OP_DISTILL_TOP = 7, 8
 SAKI_TARGET_MODE, SAKI_TARGET_SAMPLE = 0, 1
+SAKI_KL_FORWARD, SAKI_KL_REVERSE = 0, 1
 SAKI_SELECT_RANDOM, SAKI_SELECT_TV_WEIGHTED = 0, 1
 SAKI_MAX_VOCAB = 1 << 21
 SAKI_STATIC_MAX_ROWS = 262144
 SAKI_CHUNK = 1024
-ROW_OK, ROW_NONFINITE, ROW_BAD_DRAFT, ROW_SKIPPED = 0, 1, 2, 3
+ROW_OK, ROW_NONFINITE, ROW_BAD_DRAFT, ROW_SKIPPED, ROW_BAD_TARGET = 0, 1, 2, 3, 4
 
 STATUS = {0: "SAKI_OK", 1: "SAKI_E_NULLPTR", 2: "SAKI_E_SHAPE", 3: "SAKI_E_VALUE",
           4: "SAKI_E_DTYPE", 5: "SAKI_E_ALIGN", 6: "SAKI_E_WORKSPACE", 7: "SAKI_E_DEVICE",
@@ -32,6 +34,9 @@ EXPORTED = ["saki_workspace_bytes", "saki_couple", "saki_couple_static", "saki_r
             "saki_status_str", "saki_last_error"]
 EXPORTED_KV = ["saki_kv_reserve", "saki_kv_commit", "saki_kv_fork", "saki_kv_compact", "saki_kv_append",
                "saki_kv_attention"]  # of include/saki_kv.h
+EXPORTED_DISTILL = ["saki_top_logits", "saki_distill_top", "saki_linear_ce",
+                    "saki_linear_ce_workspace_bytes"]  # of include/saki_distill.h
+SAKI_MAX_TOP_K, SAKI_MAX_HIDDEN = 256, 65536
 KV_OK, KV_NO_PAGES, KV_TOO_LONG, KV_BAD = 0, 1, 2, 3
 SEQ_RUNNING, SEQ_FINISHED, SEQ_STOPPED = 0, 1, 2
 SAKI_MAX_PROBE_K = 64
@@ -100,6 +105,25 @@ class SakiKVHeads(ctypes.Structure):
 class SakiKVRope(ctypes.Structure):
     _fields_ = [("freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
                 ("amplitude", ctypes.c_float)]
+
+
+class SakiTopList(ctypes.Structure):
+    _fields_ = [("token", ctypes.c_void_p), ("logit", ctypes.c_void_p), ("rest_logit", ctypes.c_void_p),
+                ("stride", ctypes.c_int64), ("k", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class SakiHead(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("hidden_stride", ctypes.c_int64),
+                ("weight_stride", ctypes.c_int64), ("n_rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("hidden_size", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class SakiCEArgs(ctypes.Structure):
+    _fields_ = [("token", ctypes.c_void_p), ("row_weight", ctypes.c_void_p), ("valid_mask", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_float), ("reserved", ctypes.c_uint32)] + \
+               [(n, ctypes.c_void_p) for n in ("row_loss", "logp_token", "loss_sum", "row_status", "grad_hidden",
+                                               "grad_weight")] + \
+               [("grad_hidden_stride", ctypes.c_int64), ("grad_weight_stride", ctypes.c_int64)]
 
 
 class SakiError(RuntimeError):
@@ -171,6 +195,16 @@ def load(path=LIB_PATH):
                            ctypes.c_float, I32, I32, ptr, size, ptr])):
         f = getattr(lib, "saki_kv_" + name)
         f.restype, f.argtypes = ctypes.c_int, args
+    F32 = ctypes.c_float
+    for name, args in (
+            ("top_logits", [ptr, I32, I64, I64, I64, I32, F32, ptr, ptr, I64, ptr, ptr, ptr, size, ptr]),
+            ("distill_top", [ptr, I32, I64, I64, I64, P(SakiTopList), F32, I32, ptr, F32, ptr, ptr, ptr, I32, I64, ptr, ptr,
+                             size, ptr]),
+            ("linear_ce", [P(SakiHead), P(SakiCEArgs), ptr, size, ptr])):
+        f = getattr(lib, "saki_" + name)
+        f.restype, f.argtypes = ctypes.c_int, args
+    lib.saki_linear_ce_workspace_bytes.restype = size
+    lib.saki_linear_ce_workspace_bytes.argtypes = [P(SakiHead), I32]
     lib.saki_status_str.restype = ctypes.c_char_p
     lib.saki_status_str.argtypes = [ctypes.c_int]
     lib.saki_last_error.restype = ctypes.c_char_p
@@ -574,3 +608,187 @@ def saki_kv_attention(table, pool, layer, tokens, q, out, lse=None, scale=1.0, w
     _check(_lib.saki_kv_attention(_ref(table), _ref(pool), int(layer), _ref(tokens), q.shape[1], _heads(q), _heads(out),
                                   _addr(lse), float(scale), int(window), int(sinks), _addr(workspace),
                                   _ws_bytes(workspace), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# A teacher's top logits, distillation from them, cross entropy from hidden states.
+# ---------------------------------------------------------------------------
+def _on(device, stream, **tensors):
+    """The arguments of one call lie on one device, the current one, and take no part in autograd."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which this call does not record: pass it detached (gradients "
+                             "are outputs)")
+    if device.type != "cuda":
+        raise ValueError(f"the call's tensors are on {device}: the library runs on the GPU")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"a stream of {stream.device} for tensors on {device}")
+    if torch.cuda.current_device() != device.index:
+        raise ValueError(f"the call's tensors are on {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _typed(n, **tensors):
+    """Dense [n] arrays: name=(tensor, dtypes)."""
+    for name, (t, dtypes) in tensors.items():
+        if t is not None and (t.dtype not in dtypes or tuple(t.shape) != (n,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {' or '.join(map(str, dtypes))} tensor of shape ({n},): got "
+                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+
+
+_F32, _I32, _U8, _F64 = (torch.float32,), (torch.int32,), (torch.uint8, torch.bool), (torch.float64,)
+
+
+def _matrix(name, t, shape, dtypes):
+    """A 2-D tensor whose rows are consecutive elements, and may be strided."""
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a {' or '.join(map(str, dtypes))} tensor of shape {tuple(shape)} with "
+                         f"consecutive elements in a row: got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+
+
+def _pitch(t):
+    """Elements between rows (of one row, whose stride means nothing: its length in whole 16 bytes)."""
+    if t.shape[0] > 1:
+        return t.stride(0)
+    per = 16 // t.element_size()
+    return (t.shape[1] + per - 1) // per * per
+
+
+_LOGITS = (torch.float32, torch.bfloat16)
+
+
+def saki_top_logits(logits, k, top_logit, top_token, rest_logit=None, row_status=None, temperature=1.0, workspace=None,
+                    stream=None):
+    """Call saki_top_logits on preallocated outputs: top_logit (float32) and top_token (int32) [n, k], whose rows
+    may be strided alike; rest_logit (float32), row_status (uint8) [n] or None."""
+    _lib or load()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n_rows, vocab]")
+    n, V = logits.shape
+    _on(logits.device, stream, logits=logits, top_logit=top_logit, top_token=top_token, rest_logit=rest_logit,
+        row_status=row_status, workspace=workspace)
+    _matrix("logits", logits, (n, V), _LOGITS)
+    _matrix("top_logit", top_logit, (n, k), _F32)
+    _matrix("top_token", top_token, (n, k), _I32)
+    _typed(n, rest_logit=(rest_logit, _F32), row_status=(row_status, _U8))
+    _dense(workspace)
+    if n > 1 and top_logit.stride(0) != top_token.stride(0):
+        raise ValueError("top_logit and top_token must have rows equally far apart")
+    _check(_lib.saki_top_logits(_addr(logits), _dtype_code(logits.dtype), n, V, _pitch(logits), int(k), float(temperature),
+                                _addr(top_logit), _addr(top_token), top_logit.stride(0) if n > 1 else k,
+                                _addr(rest_logit), _addr(row_status), _addr(workspace), _ws_bytes(workspace),
+                                _stream(stream)))
+
+
+def top_logits(logits, k, temperature=1.0, stream=None):
+    """The k largest logits of each row and the others' log-sum-exp; allocates its outputs and workspace."""
+    n, V = logits.shape
+    dev = logits.device
+    out = dict(top_logit=torch.empty(n, k, dtype=torch.float32, device=dev),
+               top_token=torch.empty(n, k, dtype=torch.int32, device=dev),
+               rest_logit=torch.empty(n, dtype=torch.float32, device=dev),
+               row_status=torch.empty(n, dtype=torch.uint8, device=dev))
+    ws = torch.empty(workspace_bytes(SAKI_OP_TOP_LOGITS, n, V), dtype=torch.uint8, device=dev)
+    saki_top_logits(logits, k, temperature=temperature, workspace=ws, stream=stream, **out)
+    return out
+
+
+def saki_distill_top(student, top_token, top_logit, rest_logit=None, temperature=1.0, direction=SAKI_KL_FORWARD,
+                     valid_mask=None, grad_scale=1.0, row_loss=None, loss_sum=None, grad=None, row_status=None,
+                     workspace=None, stream=None):
+    """Call saki_distill_top on preallocated outputs: row_loss (float32), row_status (uint8) [n], loss_sum (float64,
+    one entry), grad [n, V] (float32 or bfloat16), each may be None."""
+    _lib or load()
+    if student.dim() != 2 or top_token.dim() != 2:
+        raise ValueError("student must be [n_rows, vocab], top_token [n_rows, k]")
+    n, V = student.shape
+    k = top_token.shape[1]
+    _on(student.device, stream, student=student, top_token=top_token, top_logit=top_logit, rest_logit=rest_logit,
+        valid_mask=valid_mask, row_loss=row_loss, loss_sum=loss_sum, grad=grad, row_status=row_status, workspace=workspace)
+    _matrix("student", student, (n, V), _LOGITS)
+    _matrix("top_token", top_token, (n, k), _I32)
+    _matrix("top_logit", top_logit, (n, k), _F32)
+    _typed(n, rest_logit=(rest_logit, _F32), valid_mask=(valid_mask, _U8), row_loss=(row_loss, _F32), row_status=(row_status, _U8))
+    _typed(1, loss_sum=(loss_sum, _F64))
+    if grad is not None:
+        _matrix("grad", grad, (n, V), _LOGITS)
+    _dense(workspace)
+    if n > 1 and top_logit.stride(0) != top_token.stride(0):
+        raise ValueError("top_logit and top_token must have rows equally far apart")
+    rows = SakiTopList(_addr(top_token), _addr(top_logit), _addr(rest_logit), top_token.stride(0) if n > 1 else k, k, 0)
+    _check(_lib.saki_distill_top(_addr(student), _dtype_code(student.dtype), n, V, _pitch(student), _ref(rows),
+                                 float(temperature), int(direction), _addr(valid_mask), float(grad_scale), _addr(row_loss),
+                                 _addr(loss_sum), _addr(grad), SAKI_F32 if grad is None else _dtype_code(grad.dtype),
+                                 0 if grad is None else _pitch(grad), _addr(row_status), _addr(workspace),
+                                 _ws_bytes(workspace), _stream(stream)))
+
+
+def distill_top(student, top_token, top_logit, rest_logit=None, temperature=1.0, direction=SAKI_KL_FORWARD, valid_mask=None,
+                grad_scale=1.0, grad_dtype=torch.float32, stream=None):
+    """Divergence from a teacher's top logits and its gradient (grad_dtype None: none); allocates its outputs."""
+    n, V = student.shape
+    dev = student.device
+    out = dict(row_loss=torch.empty(n, dtype=torch.float32, device=dev),
+               loss_sum=torch.empty(1, dtype=torch.float64, device=dev),
+               grad=alloc_rows(n, V, grad_dtype, dev) if grad_dtype is not None else None,
+               row_status=torch.empty(n, dtype=torch.uint8, device=dev))
+    ws = torch.empty(max(workspace_bytes(SAKI_OP_DISTILL_TOP, n, V), 8), dtype=torch.uint8, device=dev)
+    saki_distill_top(student, top_token, top_logit, rest_logit, temperature, direction, valid_mask, grad_scale,
+                     workspace=ws, stream=stream, **out)
+    return out
+
+
+def _head(hidden, weight):
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.dtype != weight.dtype:
+        raise ValueError("hidden must be [n_rows, D] and weight [vocab, D], of one dtype")
+    _matrix("hidden", hidden, hidden.shape, _LOGITS)
+    _matrix("weight", weight, (weight.shape[0], hidden.shape[1]), _LOGITS)
+    return SakiHead(_addr(hidden), _addr(weight), _pitch(hidden), _pitch(weight), hidden.shape[0], weight.shape[0],
+                    hidden.shape[1], _dtype_code(hidden.dtype), 0)
+
+
+def linear_ce_workspace_bytes(hidden, weight, train=True, grad_hidden=None, grad_weight=None):
+    """Workspace of one saki_linear_ce call; train: with both gradients, unless grad_hidden or grad_weight say otherwise."""
+    _lib or load()
+    grads = (train if grad_hidden is None else grad_hidden) * 1 + (train if grad_weight is None else grad_weight) * 2
+    return int(_lib.saki_linear_ce_workspace_bytes(_ref(_head(hidden, weight)), int(grads)))
+
+
+def saki_linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad_scale=1.0, row_loss=None, logp_token=None,
+                   loss_sum=None, row_status=None, grad_hidden=None, grad_weight=None, workspace=None, stream=None):
+    """Call saki_linear_ce on preallocated outputs: row_loss, logp_token (float32), row_status (uint8) [n], loss_sum
+    (float64, one entry), grad_hidden and grad_weight like hidden and weight; each may be None."""
+    _lib or load()
+    head = _head(hidden, weight)
+    n = hidden.shape[0]
+    _on(hidden.device, stream, hidden=hidden, weight=weight, token=token, row_weight=row_weight, valid_mask=valid_mask,
+        row_loss=row_loss, logp_token=logp_token, loss_sum=loss_sum, row_status=row_status, grad_hidden=grad_hidden,
+        grad_weight=grad_weight, workspace=workspace)
+    _typed(n, token=(token, _I32), row_weight=(row_weight, _F32), valid_mask=(valid_mask, _U8), row_loss=(row_loss, _F32),
+           logp_token=(logp_token, _F32), row_status=(row_status, _U8))
+    _typed(1, loss_sum=(loss_sum, _F64))
+    for name, g, x in (("grad_hidden", grad_hidden, hidden), ("grad_weight", grad_weight, weight)):
+        if g is not None:
+            _matrix(name, g, x.shape, (x.dtype,))
+    _dense(workspace)
+    args = SakiCEArgs(_addr(token), _addr(row_weight), _addr(valid_mask), float(grad_scale), 0, _addr(row_loss),
+                      _addr(logp_token), _addr(loss_sum), _addr(row_status), _addr(grad_hidden), _addr(grad_weight),
+                      0 if grad_hidden is None else _pitch(grad_hidden), 0 if grad_weight is None else _pitch(grad_weight))
+    _check(_lib.saki_linear_ce(_ref(head), _ref(args), _addr(workspace), _ws_bytes(workspace), _stream(stream)))
+
+
+def linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad_scale=1.0, train=True, stream=None):
+    """Cross entropy from hidden states and (train) the gradients of hidden and weight; allocates its outputs."""
+    n, dev = hidden.shape[0], hidden.device
+    out = dict(row_loss=torch.empty(n, dtype=torch.float32, device=dev),
+               logp_token=torch.empty(n, dtype=torch.float32, device=dev),
+               loss_sum=torch.empty(1, dtype=torch.float64, device=dev),
+               row_status=torch.empty(n, dtype=torch.uint8, device=dev),
+               grad_hidden=torch.empty(hidden.shape, dtype=hidden.dtype, device=dev) if train else None,
+               grad_weight=torch.empty(weight.shape, dtype=weight.dtype, device=dev) if train else None)
+    ws = torch.empty(max(linear_ce_workspace_bytes(hidden, weight, train), 8), dtype=torch.uint8, device=dev)
+    saki_linear_ce(hidden, weight, token, row_weight, valid_mask, grad_scale, workspace=ws, stream=stream, **out)
+    return out

@@ -1,4 +1,4 @@
-"""Builds libsaki.so (the gfx950 HIP library behind include/saki.h and saki_kv.h) in-tree."""
+"""Builds libsaki.so (the gfx950 HIP library behind include/saki.h, saki_kv.h and saki_distill.h) in-tree."""
 import os
 import subprocess
 import sys
@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 # (source, defines): the units of the library, compiled in parallel
 UNITS = [("saki.hip", [])] + [("couple.hip", [f"-DSAKI_PART={p}"]) for p in range(4)] + \
         [("verify.hip", [f"-DSAKI_PART={p}"]) for p in range(2)] + \
-        [("kv_cache.hip", [])] + [("kv_attention.hip", [f"-DSAKI_PART={p}"]) for p in range(6)]
+        [("kv_cache.hip", [])] + [("kv_attention.hip", [f"-DSAKI_PART={p}"]) for p in range(6)] + \
+        [("distill.hip", [])] + [("linear_ce.hip", [f"-DSAKI_PART={p}"]) for p in range(5)]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

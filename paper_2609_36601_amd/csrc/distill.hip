@@ -1,0 +1,210 @@
+// Top logits and the divergence from them: kernels and C ABI.
+#include <algorithm>
+#include <cmath>
+
+#include "abi.hpp"
+#include "distill.hpp"
+#include "top_logits.hpp"
+
+namespace {
+
+using saki::abi_fail;
+
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+saki_status check_logits(const void* x, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t stride, float temperature) {
+  if (dtype != SAKI_F32 && dtype != SAKI_BF16) return abi_fail(SAKI_E_DTYPE, "unknown logits dtype");
+  if (n_rows < 0) return abi_fail(SAKI_E_SHAPE, "n_rows < 0");
+  if (n_rows >= (int64_t{1} << 31)) return abi_fail(SAKI_E_SHAPE, "more than 2^31 - 1 rows in one call");
+  if (vocab < 1 || vocab > SAKI_MAX_VOCAB) return abi_fail(SAKI_E_SHAPE, "vocab outside [1, SAKI_MAX_VOCAB]");
+  if (stride < vocab) return abi_fail(SAKI_E_SHAPE, "row_stride < vocab");
+  if (!(temperature >= 0x1p-64f && temperature <= 0x1p64f))
+    return abi_fail(SAKI_E_VALUE, "temperature outside [2^-64, 2^64]");
+  if (n_rows == 0) return SAKI_OK;
+  if (!x) return abi_fail(SAKI_E_NULLPTR, "the logits pointer is NULL");
+  if (!aligned(x, 16) || (stride * (dtype == SAKI_BF16 ? 2 : 4)) % 16 != 0)
+    return abi_fail(SAKI_E_ALIGN, "logits base pointer and row pitch must be 16-byte aligned");
+  return SAKI_OK;
+}
+
+float log2_scale(float temperature) { return static_cast<float>(1.4426950408889634074 / static_cast<double>(temperature)); }
+
+// Parts of a row: one where the rows alone fill the card; otherwise so many that about TOP_ITEMS
+// workgroups run, of at least TOP_PART_CHUNKS chunks each.
+constexpr int64_t TOP_ITEMS = 1024, TOP_PART_CHUNKS = 8, TOP_MOST_PARTS = 64;
+int64_t top_parts(int64_t n_rows, int64_t vocab) {
+  const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
+  const int64_t want = std::min({(TOP_ITEMS + n_rows - 1) / n_rows, chunks / TOP_PART_CHUNKS, TOP_MOST_PARTS});
+  if (n_rows > TOP_ITEMS / 2 || want < 2) return 1;
+  const int64_t each = (chunks + want - 1) / want;
+  return (chunks + each - 1) / each;
+}
+
+size_t round256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+
+}  // namespace
+
+namespace saki {
+
+size_t distill_workspace_bytes(int op, int64_t n_rows, int64_t vocab) {
+  if (op == SAKI_OP_DISTILL_TOP) return 256 + round256(static_cast<size_t>(n_rows) * sizeof(double));
+  if (vocab < 1) return 0;
+  const int64_t parts = top_parts(n_rows, vocab);
+  if (parts < 2) return 0;
+  return round256(static_cast<size_t>(n_rows * parts) * (SAKI_MAX_TOP_K * sizeof(uint64_t) + sizeof(TopPart)));
+}
+
+__global__ __launch_bounds__(64) void clear_row_counter_kernel(unsigned int* counter) {
+  if (threadIdx.x == 0) *counter = 0u;
+}
+
+}  // namespace saki
+
+extern "C" {
+
+saki_status saki_top_logits(const void* logits, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                            int32_t k, float temperature, float* top_logit, int32_t* top_token, int64_t top_stride,
+                            float* rest_logit, uint8_t* row_status, void* ws, size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_logits(logits, dtype, n_rows, vocab, row_stride, temperature);
+  if (st != SAKI_OK) return st;
+  if (k < 1 || k > SAKI_MAX_TOP_K || k > vocab) return abi_fail(SAKI_E_SHAPE, "k outside [1, min(SAKI_MAX_TOP_K, vocab)]");
+  if (top_stride < k) return abi_fail(SAKI_E_SHAPE, "top_stride < k");
+  if (n_rows == 0) return saki::abi_ok();
+  if (!top_logit || !top_token) return abi_fail(SAKI_E_NULLPTR, "top_logit and top_token are required");
+  if (!aligned(top_logit, 4) || !aligned(top_token, 4) || !aligned(rest_logit, 4))
+    return abi_fail(SAKI_E_ALIGN, "outputs of 4 bytes must be 4-byte aligned");
+  const int64_t parts = top_parts(n_rows, vocab);
+  if (parts > 1) {
+    if (!ws || ws_bytes < saki_workspace_bytes(SAKI_OP_TOP_LOGITS, n_rows, vocab))
+      return abi_fail(SAKI_E_WORKSPACE, "workspace NULL or smaller than saki_workspace_bytes(SAKI_OP_TOP_LOGITS)");
+    if (!aligned(ws, 16)) return abi_fail(SAKI_E_ALIGN, "workspace must be 16-byte aligned");
+  }
+  int cus = 0;
+  st = saki::abi_cus(&cus);
+  if (st != SAKI_OK) return st;
+  saki::TopParams P{};
+  P.x = logits;
+  P.n_rows = n_rows;
+  P.stride = row_stride;
+  P.V = static_cast<int>(vocab);
+  P.k = k;
+  P.c = log2_scale(temperature);
+  P.top_logit = top_logit;
+  P.top_token = top_token;
+  P.top_stride = top_stride;
+  P.rest_logit = rest_logit;
+  P.row_status = row_status;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  const bool bf16 = dtype == SAKI_BF16;
+  const dim3 block(saki::TOP_NT);
+  const int64_t slots = static_cast<int64_t>(cus) * 8;
+  if (parts < 2) {
+    const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots)));
+    if (bf16) hipLaunchKernelGGL((saki::top_kernel<uint16_t, saki::TOP_WHOLE>), grid, block, 0, hs, P);
+    else hipLaunchKernelGGL((saki::top_kernel<float, saki::TOP_WHOLE>), grid, block, 0, hs, P);
+    st = saki::abi_launched(hipGetLastError(), "top_kernel");
+    return st != SAKI_OK ? st : saki::abi_ok();
+  }
+  const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
+  P.parts = static_cast<int>(parts);
+  P.part_len = static_cast<int>((chunks + parts - 1) / parts * SAKI_CHUNK);
+  P.info = static_cast<saki::TopPart*>(ws);
+  P.keys = reinterpret_cast<uint64_t*>(P.info + n_rows * parts);
+  const dim3 grid(static_cast<unsigned>(n_rows * parts)), rows(static_cast<unsigned>(n_rows));
+  if (bf16) hipLaunchKernelGGL((saki::top_kernel<uint16_t, saki::TOP_PART>), grid, block, 0, hs, P);
+  else hipLaunchKernelGGL((saki::top_kernel<float, saki::TOP_PART>), grid, block, 0, hs, P);
+  st = saki::abi_launched(hipGetLastError(), "top_kernel");
+  if (st != SAKI_OK) return st;
+  if (bf16) hipLaunchKernelGGL((saki::top_kernel<uint16_t, saki::TOP_MERGE>), rows, block, 0, hs, P);
+  else hipLaunchKernelGGL((saki::top_kernel<float, saki::TOP_MERGE>), rows, block, 0, hs, P);
+  st = saki::abi_launched(hipGetLastError(), "top_kernel");
+  return st != SAKI_OK ? st : saki::abi_ok();
+}
+
+saki_status saki_distill_top(const void* student, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t row_stride,
+                             const saki_top_list* list, float temperature, int32_t direction, const uint8_t* valid_mask,
+                             float grad_scale, float* row_loss, double* loss_sum, void* grad, int32_t grad_dtype,
+                             int64_t grad_stride, uint8_t* row_status, void* ws, size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_logits(student, dtype, n_rows, vocab, row_stride, temperature);
+  if (st != SAKI_OK) return st;
+  if (!list) return abi_fail(SAKI_E_NULLPTR, "list is NULL");
+  if (list->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_top_list.reserved must be 0");
+  if (list->k < 1 || list->k > SAKI_MAX_TOP_K) return abi_fail(SAKI_E_SHAPE, "k outside [1, SAKI_MAX_TOP_K]");
+  if (list->stride < list->k) return abi_fail(SAKI_E_SHAPE, "the list's stride < k");
+  if (direction != SAKI_KL_FORWARD && direction != SAKI_KL_REVERSE) return abi_fail(SAKI_E_VALUE, "unknown direction");
+  if (!std::isfinite(grad_scale)) return abi_fail(SAKI_E_VALUE, "grad_scale is not finite");
+  if (grad) {
+    if (grad_dtype != SAKI_F32 && grad_dtype != SAKI_BF16) return abi_fail(SAKI_E_DTYPE, "unknown grad dtype");
+    if (grad_stride < vocab) return abi_fail(SAKI_E_SHAPE, "grad_stride < vocab");
+    if (!aligned(grad, 16) || (grad_stride * (grad_dtype == SAKI_BF16 ? 2 : 4)) % 16 != 0)
+      return abi_fail(SAKI_E_ALIGN, "grad base pointer and row pitch must be 16-byte aligned");
+    if (grad == student && (grad_dtype != dtype || grad_stride != row_stride))
+      return abi_fail(SAKI_E_VALUE, "a gradient in the student's buffer has its dtype and stride");
+  }
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (!aligned(loss_sum, 8)) return abi_fail(SAKI_E_ALIGN, "loss_sum must be 8-byte aligned");
+  if (n_rows == 0) {  // the sum over no rows
+    if (!loss_sum) return saki::abi_ok();
+    st = saki::abi_loss_sum(nullptr, 0, loss_sum, hs);
+    return st != SAKI_OK ? st : saki::abi_ok();
+  }
+  if (!list->token || !list->logit) return abi_fail(SAKI_E_NULLPTR, "the list's token and logit are required");
+  if (direction == SAKI_KL_REVERSE && !list->rest_logit)
+    return abi_fail(SAKI_E_NULLPTR, "the reverse divergence needs rest_logit");
+  if (!aligned(list->token, 4) || !aligned(list->logit, 4) || !aligned(list->rest_logit, 4) || !aligned(row_loss, 4))
+    return abi_fail(SAKI_E_ALIGN, "an array of 4 bytes an entry is not 4-byte aligned");
+  if (!ws || ws_bytes < saki_workspace_bytes(SAKI_OP_DISTILL_TOP, n_rows, vocab))
+    return abi_fail(SAKI_E_WORKSPACE, "workspace NULL or smaller than saki_workspace_bytes(SAKI_OP_DISTILL_TOP)");
+  if (!aligned(ws, 8)) return abi_fail(SAKI_E_ALIGN, "workspace must be 8-byte aligned");
+  int cus = 0;
+  st = saki::abi_cus(&cus);
+  if (st != SAKI_OK) return st;
+  saki::DistillParams P{};
+  P.s = student;
+  P.n_rows = n_rows;
+  P.stride = row_stride;
+  P.V = static_cast<int>(vocab);
+  P.k = list->k;
+  P.token = list->token;
+  P.logit = list->logit;
+  P.rest = list->rest_logit;
+  P.list_stride = list->stride;
+  P.c = log2_scale(temperature);
+  P.inv_tau = 1.0f / temperature;
+  P.reverse = direction == SAKI_KL_REVERSE;
+  P.valid = valid_mask;
+  P.grad_scale = grad_scale;
+  P.row_loss = row_loss;
+  double* const scaled = reinterpret_cast<double*>(static_cast<char*>(ws) + 256);
+  P.scaled_loss = loss_sum ? scaled : nullptr;
+  P.grad = grad;
+  P.grad_stride = grad_stride;
+  P.row_status = row_status;
+  const int64_t slots = static_cast<int64_t>(cus) * 4;
+  const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots))), block(saki::DT_NT);
+  if (n_rows > slots) {
+    P.next_row = static_cast<unsigned int*>(ws);
+    hipLaunchKernelGGL(saki::clear_row_counter_kernel, dim3(1), dim3(64), 0, hs, P.next_row);
+    st = saki::abi_launched(hipGetLastError(), "clear_row_counter_kernel");
+    if (st != SAKI_OK) return st;
+  }
+  const bool gbf = grad_dtype == SAKI_BF16;
+  if (dtype == SAKI_BF16) {
+    if (!grad) hipLaunchKernelGGL((saki::distill_kernel<uint16_t, float, false>), grid, block, 0, hs, P);
+    else if (gbf) hipLaunchKernelGGL((saki::distill_kernel<uint16_t, uint16_t, true>), grid, block, 0, hs, P);
+    else hipLaunchKernelGGL((saki::distill_kernel<uint16_t, float, true>), grid, block, 0, hs, P);
+  } else {
+    if (!grad) hipLaunchKernelGGL((saki::distill_kernel<float, float, false>), grid, block, 0, hs, P);
+    else if (gbf) hipLaunchKernelGGL((saki::distill_kernel<float, uint16_t, true>), grid, block, 0, hs, P);
+    else hipLaunchKernelGGL((saki::distill_kernel<float, float, true>), grid, block, 0, hs, P);
+  }
+  st = saki::abi_launched(hipGetLastError(), "distill_kernel");
+  if (st != SAKI_OK) return st;
+  if (loss_sum) {
+    st = saki::abi_loss_sum(scaled, n_rows, loss_sum, hs);
+    if (st != SAKI_OK) return st;
+  }
+  return saki::abi_ok();
+}
+
+}  // extern "C"

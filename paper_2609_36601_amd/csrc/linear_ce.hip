@@ -1,0 +1,409 @@
+// Cross entropy from hidden states.  SAKI_PART 0 .. 3: the product of that CeKind; 4: the other kernels
+// and the C ABI.
+#include "linear_ce.hpp"
+
+#if SAKI_PART < 4
+
+namespace saki {
+
+template <int KIND, typename TILE>
+static hipError_t launch_tile(CeGemm A, bool three, int splits, hipStream_t st) {
+  A.p_tiles = (A.n_p + TILE::PT - 1) / TILE::PT;
+  A.q_tiles = (A.n_q + TILE::QT - 1) / TILE::QT;
+  const dim3 grid(static_cast<unsigned>(A.p_tiles * A.q_tiles), static_cast<unsigned>(splits)), block(TILE::NT);
+  if (three) hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, true>), grid, block, 0, st, A);
+  else hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, false>), grid, block, 0, st, A);
+  return hipGetLastError();
+}
+
+template <>
+hipError_t launch_ce_part<SAKI_PART>(const CeGemm& A, int tile, bool three, int splits, hipStream_t st) {
+  if (tile == 0) return launch_tile<SAKI_PART, CeLarge>(A, three, splits, st);
+  if (tile == 1) return launch_tile<SAKI_PART, CeMiddle>(A, three, splits, st);
+  return launch_tile<SAKI_PART, CeFew>(A, three, splits, st);
+}
+
+}  // namespace saki
+
+#else
+
+#include <algorithm>
+#include <cmath>
+
+#include "abi.hpp"
+
+namespace saki {
+
+template <>
+hipError_t launch_ce_part<CE_LSE>(const CeGemm&, int, bool, int, hipStream_t);
+template <>
+hipError_t launch_ce_part<CE_DL>(const CeGemm&, int, bool, int, hipStream_t);
+template <>
+hipError_t launch_ce_part<CE_DX>(const CeGemm&, int, bool, int, hipStream_t);
+template <>
+hipError_t launch_ce_part<CE_DW>(const CeGemm&, int, bool, int, hipStream_t);
+
+// The rows that take part, in order, and the outputs of those that do not.  One workgroup: a scan
+// over 1,024 rows at a time.
+__global__ __launch_bounds__(1024) void ce_rows_kernel(CeRows P) {
+  __shared__ int before[1024 / WAVE];
+  const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE;
+  int base = 0;
+  for (int64_t r0 = 0; r0 < P.n_rows; r0 += 1024) {
+    const int64_t r = r0 + threadIdx.x;
+    const bool in = r < P.n_rows && P.valid[r] != 0;
+    const uint64_t who = __ballot(in);
+    if (lane == 0) before[wave] = __popcll(who);
+    __syncthreads();
+    int at = base, all = base;
+    for (int w = 0; w < 1024 / WAVE; ++w) {
+      at += w < wave ? before[w] : 0;
+      all += before[w];
+    }
+    at += __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(who), 0));
+    if (in) P.source[at] = static_cast<int>(r);
+    if (r < P.n_rows) {
+      P.place[r] = in ? at : -1;
+      if (!in) {
+        if (P.row_loss) P.row_loss[r] = 0.0f;
+        if (P.logp_token) P.logp_token[r] = 0.0f;
+        if (P.scaled_loss) P.scaled_loss[r] = 0.0;
+        if (P.row_status) P.row_status[r] = SAKI_ROW_OK;
+      }
+    }
+    base = all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *P.count = base;
+}
+
+// The gradient of a weight to which no row adds anything.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_zero_kernel(T* grad, int64_t stride, int64_t vocab, int D) {
+  const int pieces = D / 8;
+  float g[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) g[e] = 0.0f;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < vocab * pieces; i += gridDim.x * 256ll)
+    Storer<T>::store8(grad + i / pieces * stride + i % pieces * 8, g);
+}
+
+}  // namespace saki
+
+namespace {
+
+using namespace saki;
+
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int64_t MOST_STRIDE = int64_t{1} << 22;
+constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
+// Bytes of the gradient of a piece's logits, and of a piece of the weight in three parts: what the
+// last-level cache holds, at most.
+constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
+constexpr int64_t CUS = 256;
+
+saki_status check_head(const saki_head* h) {
+  if (!h) return abi_fail(SAKI_E_NULLPTR, "head is NULL");
+  if (h->dtype != SAKI_F32 && h->dtype != SAKI_BF16) return abi_fail(SAKI_E_DTYPE, "unknown dtype of the head");
+  if (h->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_head.reserved must be 0");
+  if (h->n_rows < 0 || h->n_rows >= MOST_ROWS) return abi_fail(SAKI_E_SHAPE, "n_rows outside [0, 2^31 / 256)");
+  if (h->vocab < 1 || h->vocab > SAKI_MAX_VOCAB) return abi_fail(SAKI_E_SHAPE, "vocab outside [1, SAKI_MAX_VOCAB]");
+  if (h->hidden_size < 8 || h->hidden_size > SAKI_MAX_HIDDEN || h->hidden_size % 8 != 0)
+    return abi_fail(SAKI_E_SHAPE, "hidden_size is not a multiple of 8 in [8, SAKI_MAX_HIDDEN]");
+  if (h->hidden_stride < h->hidden_size || h->weight_stride < h->hidden_size || h->hidden_stride >= MOST_STRIDE ||
+      h->weight_stride >= MOST_STRIDE)
+    return abi_fail(SAKI_E_SHAPE, "a row stride outside [hidden_size, 2^22)");
+  return SAKI_OK;
+}
+
+// Tiles of a product of n_p x n_q entries: the large ones where they fill the card twice, the middle ones below that, and
+// where there are few rows (their side is q) those that read the weight with the least beside it.
+int tile_of(int64_t n_p, int64_t n_q, bool rows_q) {
+  if (rows_q && n_q <= 64) return 2;
+  return ceil_div(n_p, 256) * ceil_div(n_q, 256) >= CUS ? 0 : 1;
+}
+
+// The workspace of a call, and its pieces.
+struct Plan {
+  int64_t n, V, D, ld;       // ld: elements of a packed row, whole tiles of k
+  int64_t rows;              // n, padded to tiles
+  int planes;
+  int64_t slots, wave_p, piece, pieces, splits, k_split;  // wave_p: tokens of a slot
+  int tile_s, tile_l, tile_x;  // tiles of the products for the loss, for dL and for dX
+  size_t count, source, place, row, scaled, stats, x, w, dl, sums, bytes;
+};
+
+Plan plan_of(const saki_head* h, bool dx, bool dw) {
+  Plan p{};
+  p.n = h->n_rows;
+  p.V = h->vocab;
+  p.D = h->hidden_size;
+  p.ld = round_up(p.D, CE_BK);
+  p.rows = round_up(p.n, CE_PAD);
+  const bool three = h->dtype == SAKI_F32;
+  p.planes = three ? 3 : 1;
+  // pieces of the vocabulary, of equal size
+  const int64_t padded = round_up(p.V, CE_PAD);
+  int64_t most = padded;
+  if (dx || dw) most = std::min(most, PIECE_BYTES / (p.rows * 2 * p.planes));
+  if (three) most = std::min(most, PIECE_BYTES / (p.ld * 2 * p.planes));
+  most = std::max<int64_t>(most / CE_PAD * CE_PAD, CE_PAD);
+  p.pieces = ceil_div(padded, most);
+  p.piece = round_up(ceil_div(padded, p.pieces), CE_PAD);
+  p.pieces = ceil_div(padded, p.piece);
+  p.tile_l = tile_of(p.piece, p.n, true);
+  p.tile_s = three ? p.tile_l : tile_of(p.V, p.n, true);
+  const int64_t tile_p = p.tile_s == 0 ? CeLarge::PT : p.tile_s == 1 ? CeMiddle::PT : CeFew::PT;
+  p.wave_p = tile_p / (p.tile_s == 0 ? CeLarge::WP : p.tile_s == 1 ? CeMiddle::WP : CeFew::WP);
+  p.slots = ceil_div(p.V, tile_p) * (tile_p / p.wave_p);
+  p.tile_x = tile_of(p.D, p.n, true);
+  if (p.tile_x == 0 || p.tile_x == 1) p.tile_x = ceil_div(p.n, 256) * ceil_div(p.D, 256) * 2 >= CUS ? 0 : 1;
+  const int64_t t = p.tile_x == 0 ? 256 : p.tile_x == 1 ? 128 : 64, per_cu = p.tile_x == 0 ? 1 : 2;
+  const int64_t tiles = ceil_div(p.n, t) * ceil_div(p.D, t), kt = p.piece / CE_BK;
+  // dX: k, the piece's tokens, in so many splits that the tiles fill the card
+  p.splits = std::max<int64_t>(1, std::min(per_cu * CUS / std::max<int64_t>(tiles, 1), kt / 4));
+  p.k_split = ceil_div(kt, p.splits);
+  p.splits = ceil_div(kt, p.k_split);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~static_cast<size_t>(255);
+    return here;
+  };
+  const size_t n = static_cast<size_t>(p.n), rows = static_cast<size_t>(p.rows);
+  p.count = take(4);
+  p.source = take(n * 4);
+  p.place = take(n * 4);
+  p.row = take(n * sizeof(CeRow));
+  p.scaled = take(n * 8);
+  p.stats = take(n * p.slots * sizeof(float2));
+  p.x = take(n * p.ld * 2 * p.planes);
+  p.w = three ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
+  p.dl = dx || dw ? take(rows * p.piece * 2 * p.planes) : at;
+  p.sums = dx ? take(static_cast<size_t>(p.splits) * n * p.D * 4) : at;
+  p.bytes = at;
+  return p;
+}
+
+template <typename T>
+saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* ws, hipStream_t hs) {
+  constexpr bool three = sizeof(T) == 4;
+  const bool dx = a->grad_hidden != nullptr, dw = a->grad_weight != nullptr;
+  CeRows R{};
+  R.n_rows = p.n;
+  R.vocab = static_cast<int>(p.V);
+  R.D = static_cast<int>(p.D);
+  R.hidden = h->hidden;
+  R.weight = h->weight;
+  R.hidden_stride = h->hidden_stride;
+  R.weight_stride = h->weight_stride;
+  R.token = a->token;
+  R.row_weight = a->row_weight;
+  R.valid = a->valid_mask;
+  R.grad_scale = a->grad_scale;
+  R.row_loss = a->row_loss;
+  R.logp_token = a->logp_token;
+  R.scaled_loss = a->loss_sum ? reinterpret_cast<double*>(ws + p.scaled) : nullptr;
+  R.row_status = a->row_status;
+  R.grad_hidden = a->grad_hidden;
+  R.grad_stride = a->grad_hidden_stride;
+  R.source = reinterpret_cast<int*>(ws + p.source);
+  R.place = reinterpret_cast<int*>(ws + p.place);
+  R.rows = reinterpret_cast<CeRow*>(ws + p.row);
+  R.stats = reinterpret_cast<float2*>(ws + p.stats);
+  R.slots = static_cast<int>(p.slots);
+  R.sums = reinterpret_cast<float*>(ws + p.sums);
+  R.ld_sums = p.D;
+  R.split_stride = p.n * p.D;
+  R.splits = static_cast<int>(p.splits);
+  saki_status st;
+#define SAKI_LAUNCHED(what)                     \
+  st = abi_launched(hipGetLastError(), what);   \
+  if (st != SAKI_OK) return st
+  if (a->valid_mask) {
+    R.count = reinterpret_cast<int*>(ws + p.count);
+    hipLaunchKernelGGL(ce_rows_kernel, dim3(1), dim3(1024), 0, hs, R);
+    SAKI_LAUNCHED("ce_rows_kernel");
+  }
+  CeGemm G{};
+  G.count = R.count;
+  G.planes = p.planes;
+  // rows of X as the products take them: as they are, or packed
+  const bool pack = three || a->valid_mask || p.D != p.ld;
+  const uint16_t* x = static_cast<const uint16_t*>(h->hidden);
+  int64_t ldx = h->hidden_stride;
+  const int64_t x_plane = p.n * p.ld;
+  if (pack) {
+    uint16_t* const to = reinterpret_cast<uint16_t*>(ws + p.x);
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.n * p.ld / 8, 256), 8192);
+    hipLaunchKernelGGL((ce_pack_kernel<T>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs,
+                       static_cast<const T*>(h->hidden), h->hidden_stride, p.n, static_cast<int>(p.D),
+                       R.count ? R.source : nullptr, R.count, to, p.ld, x_plane);
+    SAKI_LAUNCHED("ce_pack_kernel");
+    x = to;
+    ldx = p.ld;
+  }
+  uint16_t* const w_parts = reinterpret_cast<uint16_t*>(ws + p.w);
+  const int64_t w_plane = p.piece * p.ld;
+  // tokens v0 .. v0 + nv of the weight as the products take them
+  auto weight = [&](int64_t v0, int64_t nv) {
+    if constexpr (three) {
+      const int64_t blocks = std::min<int64_t>(ceil_div(nv * p.ld / 8, 256), 8192);
+      hipLaunchKernelGGL((ce_pack_kernel<T>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs,
+                         static_cast<const T*>(h->weight) + v0 * h->weight_stride, h->weight_stride, nv,
+                         static_cast<int>(p.D), nullptr, nullptr, w_parts, p.ld, w_plane);
+      G.p = w_parts;
+      G.ldp = p.ld;
+      G.p_plane = w_plane;
+    } else {
+      G.p = static_cast<const uint16_t*>(h->weight) + v0 * h->weight_stride;
+      G.ldp = h->weight_stride;
+    }
+    return hipGetLastError();
+  };
+  auto rows_q = [&]() {
+    G.q = x;
+    G.ldq = ldx;
+    G.q_plane = x_plane;
+    G.n_q = static_cast<int>(p.n);
+    G.n_k = static_cast<int>(three ? p.ld : p.D);
+  };
+  // the log-sum-exp (bf16: of the whole vocabulary at once)
+  G.stats = reinterpret_cast<float2*>(ws + p.stats);
+  G.slots = static_cast<int>(p.slots);
+  const int64_t step = three ? p.piece : p.V;
+  for (int64_t v0 = 0; v0 < p.V; v0 += step) {
+    const int64_t nv = std::min(step, p.V - v0);
+    st = abi_launched(weight(v0, nv), "ce_pack_kernel");
+    if (st != SAKI_OK) return st;
+    rows_q();
+    G.n_p = static_cast<int>(nv);
+    G.slot0 = static_cast<int>(v0 / p.wave_p);
+    st = abi_launched(launch_ce_part<CE_LSE>(G, p.tile_s, three, 1, hs), "ce_gemm_kernel");
+    if (st != SAKI_OK) return st;
+  }
+  hipLaunchKernelGGL((ce_loss_kernel<T>), dim3(static_cast<unsigned>(ceil_div(p.n, 4))), dim3(256), 0, hs, R);
+  SAKI_LAUNCHED("ce_loss_kernel");
+  if (a->loss_sum) {
+    st = abi_loss_sum(R.scaled_loss, p.n, a->loss_sum, hs);
+    if (st != SAKI_OK) return st;
+  }
+  if (!dx && !dw) return SAKI_OK;
+  uint16_t* const dl = reinterpret_cast<uint16_t*>(ws + p.dl);
+  const int64_t dl_plane = p.rows * p.piece;
+  for (int64_t v0 = 0; v0 < p.V; v0 += p.piece) {
+    const int64_t nv = std::min(p.piece, p.V - v0);
+    st = abi_launched(weight(v0, nv), "ce_pack_kernel");
+    if (st != SAKI_OK) return st;
+    rows_q();
+    G.n_p = static_cast<int>(nv);
+    G.rows = R.rows;
+    G.dl = dl;
+    G.ld_dl = p.piece;
+    G.dl_plane = dl_plane;
+    G.v0 = static_cast<int>(v0);
+    st = abi_launched(launch_ce_part<CE_DL>(G, p.tile_l, three, 1, hs), "ce_gemm_kernel");
+    if (st != SAKI_OK) return st;
+    if (dx) {
+      CeGemm X = G;
+      X.q = dl;
+      X.ldq = p.piece;
+      X.q_plane = dl_plane;
+      X.n_p = static_cast<int>(p.D);
+      X.n_k = static_cast<int>(nv);
+      X.k_split = static_cast<int>(p.k_split);
+      X.sums = reinterpret_cast<float*>(ws + p.sums);
+      X.ld_sums = R.ld_sums;
+      X.split_stride = R.split_stride;
+      X.add = v0 > 0;
+      st = abi_launched(launch_ce_part<CE_DX>(X, p.tile_x, three, static_cast<int>(p.splits), hs), "ce_gemm_kernel");
+      if (st != SAKI_OK) return st;
+    }
+    if (dw) {
+      CeGemm W = G;
+      W.p = x;
+      W.ldp = ldx;
+      W.p_plane = x_plane;
+      W.q = dl;
+      W.ldq = p.piece;
+      W.q_plane = dl_plane;
+      W.n_p = static_cast<int>(p.D);
+      W.n_q = static_cast<int>(nv);
+      W.n_k = static_cast<int>(p.n);
+      W.grad = static_cast<T*>(a->grad_weight) + v0 * a->grad_weight_stride;
+      W.ld_grad = a->grad_weight_stride;
+      W.scale = a->grad_scale;
+      st = abi_launched(launch_ce_part<CE_DW>(W, tile_of(p.D, nv, false), three, 1, hs), "ce_gemm_kernel");
+      if (st != SAKI_OK) return st;
+    }
+  }
+  if (dx) {
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.n * p.D / 8, 256), 8192);
+    using S = std::conditional_t<three, float, uint16_t>;
+    hipLaunchKernelGGL((ce_grad_hidden_kernel<S>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs, R);
+    SAKI_LAUNCHED("ce_grad_hidden_kernel");
+  }
+#undef SAKI_LAUNCHED
+  return SAKI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t saki_linear_ce_workspace_bytes(const saki_head* head, int32_t grads) {
+  if (check_head(head) != SAKI_OK || grads < 0 || grads > 3 || head->n_rows == 0) return 0;
+  return plan_of(head, grads & 1, grads & 2).bytes;
+}
+
+saki_status saki_linear_ce(const saki_head* head, const saki_ce_args* args, void* ws, size_t ws_bytes, saki_stream_t stream) {
+  saki_status st = check_head(head);
+  if (st != SAKI_OK) return st;
+  if (!args) return abi_fail(SAKI_E_NULLPTR, "args is NULL");
+  if (args->reserved != 0) return abi_fail(SAKI_E_VALUE, "saki_ce_args.reserved must be 0");
+  if (!std::isfinite(args->grad_scale)) return abi_fail(SAKI_E_VALUE, "grad_scale is not finite");
+  const int size = head->dtype == SAKI_BF16 ? 2 : 4;
+  if ((args->grad_hidden && (args->grad_hidden_stride < head->hidden_size || args->grad_hidden_stride >= MOST_STRIDE)) ||
+      (args->grad_weight && (args->grad_weight_stride < head->hidden_size || args->grad_weight_stride >= MOST_STRIDE)))
+    return abi_fail(SAKI_E_SHAPE, "a gradient's row stride outside [hidden_size, 2^22)");
+  if (head->n_rows > 0 && (!head->hidden || !head->weight || !args->token))
+    return abi_fail(SAKI_E_NULLPTR, "hidden, weight and token are required");
+  if (!aligned(head->hidden, 16) || !aligned(head->weight, 16) || !aligned(args->grad_hidden, 16) ||
+      !aligned(args->grad_weight, 16) || head->hidden_stride * size % 16 != 0 || head->weight_stride * size % 16 != 0 ||
+      (args->grad_hidden && args->grad_hidden_stride * size % 16 != 0) ||
+      (args->grad_weight && args->grad_weight_stride * size % 16 != 0))
+    return abi_fail(SAKI_E_ALIGN, "rows of hidden, weight and their gradients must be 16-byte aligned");
+  if (!aligned(args->token, 4) || !aligned(args->row_weight, 4) || !aligned(args->row_loss, 4) ||
+      !aligned(args->logp_token, 4) || !aligned(args->loss_sum, 8))
+    return abi_fail(SAKI_E_ALIGN, "an array of 4 or 8 bytes an entry is not aligned to them");
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (head->n_rows == 0) {  // the sums over no rows
+    if (args->grad_weight) {
+      const int D = static_cast<int>(head->hidden_size);
+      const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(head->vocab * D / 8, 256), 8192))), block(256);
+      if (size == 2) hipLaunchKernelGGL((ce_zero_kernel<uint16_t>), grid, block, 0, hs, static_cast<uint16_t*>(args->grad_weight), args->grad_weight_stride, head->vocab, D);
+      else hipLaunchKernelGGL((ce_zero_kernel<float>), grid, block, 0, hs, static_cast<float*>(args->grad_weight), args->grad_weight_stride, head->vocab, D);
+      st = abi_launched(hipGetLastError(), "ce_zero_kernel");
+      if (st != SAKI_OK) return st;
+    }
+    if (args->loss_sum) {
+      st = abi_loss_sum(nullptr, 0, args->loss_sum, hs);
+      if (st != SAKI_OK) return st;
+    }
+    return abi_ok();
+  }
+  const Plan p = plan_of(head, args->grad_hidden != nullptr, args->grad_weight != nullptr);
+  if (!ws || ws_bytes < p.bytes)
+    return abi_fail(SAKI_E_WORKSPACE, "workspace NULL or smaller than saki_linear_ce_workspace_bytes()");
+  if (!aligned(ws, 256)) return abi_fail(SAKI_E_ALIGN, "workspace must be 256-byte aligned");
+  st = head->dtype == SAKI_BF16 ? run<uint16_t>(head, args, p, static_cast<char*>(ws), hs)
+                                : run<float>(head, args, p, static_cast<char*>(ws), hs);
+  return st != SAKI_OK ? st : abi_ok();
+}
+
+}  // extern "C"
+
+#endif

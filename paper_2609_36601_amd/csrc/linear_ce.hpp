@@ -1,0 +1,564 @@
+// Cross entropy from hidden states: the products, and what stands around them.
+//
+// With logits L = X W^T (X [n, D], W [V, D]), log-sum-exp lse_r and target y_r of row r, weight w_r:
+//   loss_r = -w_r (L[r, y_r] - lse_r),   dL[r, v] = w_r (exp(L[r, v] - lse_r) - [v = y_r]),
+//   dX = dL W,   dW = dL^T X.
+// Four products, 8 n V D operations where 6 would do with L kept: L is computed for the loss, whose
+// epilogue keeps a maximum and a sum for each row and LSE_P tokens, and again, a piece of the
+// vocabulary at a time, for dL, which is a bf16 array of the piece that both gradients read.
+//
+// One kernel does all four (ce_gemm_kernel), C[p, q] = sum_k P(p, k) Q(q, k):
+//   CE_LSE  P = W   (tokens; k contiguous)   Q = X   (rows; k contiguous)    epilogue: maximum and sum over p
+//   CE_DL   P = W                            Q = X                           epilogue: dL
+//   CE_DX   P = W^T (elements of D; p contiguous)   Q = dL (rows; k contiguous)   epilogue: 32-bit sums
+//   CE_DW   P = X^T (elements of D; p contiguous)   Q = dL^T (tokens; q contiguous)   epilogue: the gradient
+// p is the side of the result that a lane holds four consecutive entries of, so that a row's maximum
+// and sum are mostly in a lane's registers, and stores are 8 or 16 bytes.  Tiles of 64 k are written into
+// LDS by the memory pipeline without a detour through registers, NS - 1 tiles ahead of the matrix
+// instructions.  Their 16-byte pieces are permuted so that a read's rows lie in different banks.  An
+// operand whose k is not contiguous is transposed by the read (ds_read_b64_tr_b16).
+//
+// 32 bits: a number is the sum of three bf16 numbers (24 bits, the exponent range of f32), and a product of two the
+// six products of parts that are not below 2^-24 of it, which makes six times as many tiles of k for the same
+// kernel: 6 / 16 of bf16's rate against the 1 / 16 of the f32 matrix instructions.
+#pragma once
+
+#include "common.hpp"
+#include "../../include/saki_distill.h"
+
+namespace saki {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 ce_bf16x8;
+typedef float ce_f32x4 __attribute__((ext_vector_type(4)));
+typedef short ce_s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) ce_s16x4 ce_lds_s16x4;
+
+enum CeKind { CE_LSE, CE_DL, CE_DX, CE_DW };
+
+constexpr int CE_BK = 64;   // k of a tile
+constexpr int CE_PAD = 256;  // rows and pieces of the vocabulary are padded to it: the largest tile
+
+// What a row's gradient is made of.
+struct CeRow {
+  float lse_hi, lse_lo;  // log-sum-exp / ln 2, in two floats
+  float weight;
+  int token;
+};
+
+struct CeGemm {
+  const uint16_t* p;
+  const uint16_t* q;
+  int64_t ldp, ldq;            // elements between rows in memory
+  int64_t p_plane, q_plane;    // elements between the three parts of numbers of 32 bits
+  int n_p, n_q, n_k;           // extents; rows of X and dL are at most *count where there is a count
+  const int* count;            // rows that take part, or NULL: all
+  int planes;                  // 1 or 3
+  int p_tiles, q_tiles;
+  int k_split;                 // CE_DX: tiles of k of a split
+  // CE_LSE
+  float2* stats;               // [rows, slots] maximum and sum in units of log2
+  int slots, slot0;
+  // CE_DL
+  const CeRow* rows;
+  uint16_t* dl;                // [rows, ld_dl] (planes: dl_plane apart)
+  int64_t ld_dl, dl_plane;
+  int v0;                      // the piece's first token
+  // CE_DX
+  float* sums;                 // [splits, rows, ld_sums]
+  int64_t ld_sums, split_stride;
+  int add;                     // to the sums of the pieces before
+  // CE_DW
+  void* grad;
+  int64_t ld_grad;
+  float scale;
+};
+
+// Parts of P and Q in the products of numbers of 32 bits, largest first.
+__device__ __forceinline__ int ce_part_p(int seg) { return (0x102100 >> (4 * seg)) & 3; }  // 0 0 1 2 0 1
+__device__ __forceinline__ int ce_part_q(int seg) { return (0x120010 >> (4 * seg)) & 3; }  // 0 1 0 0 2 1
+
+// Four transfers of 16 bytes a lane from base + off[i] to LDS at `lds` + i STEP + 16 lane.  m0 holds the LDS
+// address; it is the compiler's, which takes no clobber of it, and is put back.  A transfer must come one wait state
+// after a write to m0, and base is written by a scalar instruction here (a vector instruction's would need five).
+// The compiler is not told of the transfers (every LDS read would wait for them): ce_wait does.
+template <int STEP>
+__device__ __forceinline__ void ce_to_lds4(uint32_t lds, uint64_t from, const uint32_t (&off)[4]) {
+  uint32_t m0;
+  uint64_t base;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
+      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
+      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %6, %1\n\t"
+      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %7, %1\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(m0), "=&s"(base)
+      : "s"(lds), "s"(from), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "n"(STEP)
+      : "memory", "scc");
+}
+template <int STEP>
+__device__ __forceinline__ void ce_to_lds2(uint32_t lds, uint64_t from, const uint32_t (&off)[2]) {
+  uint32_t m0;
+  uint64_t base;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
+      "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(m0), "=&s"(base)
+      : "s"(lds), "s"(from), "v"(off[0]), "v"(off[1]), "n"(STEP)
+      : "memory", "scc");
+}
+
+// All but the N youngest transfers of this wave are done, its LDS reads are, and all waves are here.
+template <int N>
+__device__ __forceinline__ void ce_wait() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ uint64_t ce_scalar(const void* p) {
+  const uint64_t f = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f)),
+                 hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f >> 32));
+  return static_cast<uint64_t>(hi) << 32 | lo;
+}
+
+// One operand's side of a workgroup: EXT entries of p (or q) and 64 of k a tile.  KC: k is
+// contiguous in memory, and a tile lies in LDS as [EXT][64], piece j of row r at j ^ (r & 7).  Otherwise
+// as [64][EXT], piece j of row r at j ^ 2 (r & 3): the four rows whose 32 bytes a transposing read takes
+// lie in different banks.
+template <bool KC, int EXT, int WAVES>
+struct CeSide {
+  static constexpr int BYTES = EXT * CE_BK * 2;
+  static constexpr int LOADS = BYTES / 1024 / WAVES;  // transfers of a wave and tile
+  static_assert(LOADS * WAVES * 1024 == BYTES && (LOADS == 2 || LOADS == 4), "whole transfers");
+  static constexpr int PIECES = KC ? CE_BK / 8 : EXT / 8;  // of a row in LDS
+  static constexpr int ROWS_PER = 64 / PIECES;
+
+  uint64_t base;       // of the tile that is transferred next (the same in all lanes)
+  int64_t ld;
+  uint32_t off[LOADS];
+  int left;            // entries from this tile's first on
+
+  // row in the tile and piece in memory of this lane's part of transfer i
+  __device__ __forceinline__ static int row_of(int i, int wave, int lane) { return (i * WAVES + wave) * ROWS_PER + lane / PIECES; }
+  __device__ __forceinline__ static int piece_of(int row, int lane) {
+    const int at = lane % PIECES;
+    return KC ? at ^ (row & 7) : at ^ ((row & 3) << 1);
+  }
+
+  // first: the tile's first entry of p (q), of `extent`
+  __device__ __forceinline__ void init(const uint16_t* data, int64_t ld_, int first, int extent, int wave, int lane) {
+    ld = ld_;
+    left = extent - first;
+    base = ce_scalar(data + (KC ? static_cast<int64_t>(first) * ld : static_cast<int64_t>(first)));
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = row_of(i, wave, lane), piece = piece_of(row, lane);
+      if (KC)  // (rows behind the last: the last)
+        off[i] = static_cast<uint32_t>(min(row, left - 1)) * static_cast<uint32_t>(ld * 2) + piece * 16;
+      else  // (entries behind the last: the tile's first)
+        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(ld * 2) + (piece * 8 < left ? piece * 16 : 0);
+    }
+  }
+  // Transfers the 64 k from k0 on, of which `k_left` exist; the base is theirs.
+  __device__ __forceinline__ void transfer(uint32_t lds, int k_left, int wave, int lane) const {
+    uint32_t o[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) o[i] = off[i];
+    if (k_left < CE_BK) {  // k behind the last: one that exists (Q, whose memory is whole tiles, holds zeros there)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = row_of(i, wave, lane), piece = piece_of(row, lane);
+        if (KC) o[i] -= piece * 8 < k_left ? 0 : piece * 16;
+        else o[i] -= static_cast<uint32_t>(max(row - (k_left - 1), 0)) * static_cast<uint32_t>(ld * 2);
+      }
+    }
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
+    if constexpr (LOADS == 4) ce_to_lds4<WAVES * 1024>(at, base, o);
+    else ce_to_lds2<WAVES * 1024>(at, base, o);
+  }
+  __device__ __forceinline__ uint64_t step() const { return static_cast<uint64_t>(KC ? CE_BK * 2 : ld * CE_BK * 2); }
+};
+
+// This lane's places in an operand's tile: the fragment of 16 entries from `from` + 16 f on, k 32 kk + 8 g .. + 7.
+template <bool KC, int EXT>
+struct CeFrag {
+  const char* at[KC ? 2 : 4];
+  __device__ __forceinline__ void init(const char* tiles, int from, int lane) {
+    const int c = lane & 15, g = lane >> 4;
+    if constexpr (KC) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) at[kk] = tiles + (from + c) * 128 + ((kk * 4 + g) ^ (c & 7)) * 16;
+    } else {
+      const int s = c >> 2;
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        at[f] = tiles + (8 * g + s) * (EXT * 2) + ((((from >> 4) + f) ^ s) * 2 + ((c >> 1) & 1)) * 16 + (c & 1) * 8;
+    }
+  }
+  __device__ __forceinline__ ce_bf16x8 read(int tile, int f, int kk) const {
+    if constexpr (KC) {
+      return *reinterpret_cast<const ce_bf16x8*>(at[kk] + tile + f * 2048);
+    } else {
+      const char* a = at[f & 3] + tile + (f >> 2) * 128 + kk * 32 * EXT * 2;
+      const ce_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ce_lds_s16x4*)a);
+      const ce_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ce_lds_s16x4*)(a + 4 * EXT * 2));
+      ce_bf16x8 r;
+      __builtin_memcpy(&r, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &hi, 8);
+      return r;
+    }
+  }
+};
+
+// x as a sum of three bf16 numbers, the largest first.
+__device__ __forceinline__ void ce_parts(float x, uint32_t (&h)[3]) {
+  h[0] = f32_to_bf16_bits(x);
+  const float a = x - __uint_as_float(h[0] << 16);
+  h[1] = f32_to_bf16_bits(a);
+  h[2] = f32_to_bf16_bits(a - __uint_as_float(h[1] << 16));
+}
+
+// PT x QT: the tile; WP x WQ waves; NS tiles of k in LDS.
+template <int PT_, int QT_, int WP_, int WQ_, int NS_>
+struct CeTile {
+  static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NS = NS_;
+  static constexpr int WAVES = WP * WQ, NT = WAVES * WAVE;
+  static constexpr int TP = PT / WP / 16, TQ = QT / WQ / 16;  // fragments of a wave
+  static constexpr int LDS = NS * (PT + QT) * CE_BK * 2;
+  static constexpr int PER_SIMD = (LDS > 81920 ? 1 : 2) * WAVES / 4 > 0 ? (LDS > 81920 ? 1 : 2) * WAVES / 4 : 1;
+};
+using CeLarge = CeTile<256, 256, 2, 4, 2>;
+using CeMiddle = CeTile<128, 128, 2, 2, 2>;
+using CeFew = CeTile<64, 64, 4, 1, 4>;
+
+template <int KIND, typename TILE, bool THREE>
+__global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGemm A) {
+  constexpr int PT = TILE::PT, QT = TILE::QT, NS = TILE::NS, TP = TILE::TP, TQ = TILE::TQ;
+  constexpr bool PKC = KIND == CE_LSE || KIND == CE_DL, QKC = KIND != CE_DW;
+  using PSide = CeSide<PKC, PT, TILE::WAVES>;
+  using QSide = CeSide<QKC, QT, TILE::WAVES>;
+  constexpr int LOADS = PSide::LOADS + QSide::LOADS;
+  constexpr int STAGE = PSide::BYTES + QSide::BYTES;
+  __shared__ alignas(1024) char tiles[NS * STAGE];
+  const int lane = threadIdx.x & (WAVE - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int wp = wave % TILE::WP, wq = wave / TILE::WP;
+  // Workgroups go round the eight dies: each die gets a run of tiles, in columns of eight q, so
+  // that those at work on it at a time (32) share 4 + 8 tiles of the operands in its L2.
+  int p_tile, q_tile;
+  {
+    const int n = A.p_tiles * A.q_tiles, die = blockIdx.x & 7, i = blockIdx.x >> 3;
+    const int each = n >> 3, more = n & 7;
+    const int t = die * each + min(die, more) + i;
+    const int column = 8 * A.p_tiles, c0 = t / column * 8, wide = min(8, A.q_tiles - c0), in = t - c0 * A.p_tiles;
+    p_tile = in / wide;
+    q_tile = c0 + in % wide;
+  }
+  const int rows = A.count ? __builtin_amdgcn_readfirstlane(*A.count) : KIND == CE_DW ? A.n_k : A.n_q;
+  const int n_q = KIND == CE_DW ? A.n_q : rows, n_k = KIND == CE_DW ? rows : A.n_k;
+  const int p0 = p_tile * PT, q0 = q_tile * QT;
+  if (q0 >= n_q) return;
+  int kt = (n_k + CE_BK - 1) / CE_BK, k_first = 0;
+  if (KIND == CE_DX) {
+    k_first = blockIdx.y * A.k_split;
+    kt = min(kt - k_first, A.k_split);
+  }
+  const int steps = THREE ? 6 * kt : kt;
+
+  PSide ps;
+  QSide qs;
+  ps.init(A.p, A.ldp, p0, A.n_p, wave, lane);
+  qs.init(A.q, A.ldq, q0, n_q, wave, lane);
+  ps.base += ps.step() * k_first;
+  qs.base += qs.step() * k_first;
+  const uint64_t p_start = ps.base, q_start = qs.base;
+  const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)tiles));
+  int k_next = 0, seg = 0, stage = 0;
+  // transfers the next tile of k (behind the last one: the last again, which nobody reads)
+  auto transfer = [&]() __attribute__((always_inline)) {
+    const int k_left = n_k - (k_first + k_next) * CE_BK;
+    ps.transfer(lds + stage * STAGE, k_left, wave, lane);
+    qs.transfer(lds + stage * STAGE + PSide::BYTES, CE_BK, wave, lane);
+    stage = stage + 1 == NS ? 0 : stage + 1;
+    if (k_next + 1 < kt) {
+      ++k_next;
+      ps.base += ps.step();
+      qs.base += qs.step();
+    } else if (THREE && seg < 5) {
+      ++seg;
+      k_next = 0;
+      ps.base = p_start + ce_part_p(seg) * A.p_plane * 2;
+      qs.base = q_start + ce_part_q(seg) * A.q_plane * 2;
+    }
+  };
+
+  CeFrag<PKC, PT> pf;
+  CeFrag<QKC, QT> qf;
+  pf.init(tiles, wp * TP * 16, lane);
+  qf.init(tiles + PSide::BYTES, wq * TQ * 16, lane);
+  ce_f32x4 acc[TP][TQ];
+#pragma unroll
+  for (int i = 0; i < TP; ++i)
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) acc[i][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  if (steps > 0) {
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) transfer();
+    int now = 0;
+    for (int t = 0; t < steps; ++t) {
+      ce_wait<(NS - 2) * LOADS>();  // this tile is there, and nobody reads the one before it any more
+      transfer();
+      const int at = now * STAGE;
+      now = now + 1 == NS ? 0 : now + 1;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        ce_bf16x8 q[TQ];
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) q[j] = qf.read(at, j, kk);
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+          const ce_bf16x8 p = pf.read(at, i, kk);
+#pragma unroll
+          for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q[j], acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+    ce_wait<0>();  // no transfer is under way when the workgroup ends
+  }
+
+  // entry (p, q): p = pw + 16 i + e, q = qw + 16 j
+  const int pw = p0 + wp * TP * 16 + (lane >> 4) * 4, qw = q0 + wq * TQ * 16 + (lane & 15);
+  if constexpr (KIND == CE_LSE) {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      float m = -finf();
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[i][j][e] = pw + 16 * i + e < A.n_p ? acc[i][j][e] * LOG2E : -finf();
+          m = fmaxf(m, acc[i][j][e]);
+        }
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      // (no token here: -infinity and 0)
+      const float ref = m == -finf() ? 0.0f : m;
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += fexp2(acc[i][j][e] - ref);
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      const int row = qw + 16 * j;
+      if (lane < 16 && row < n_q)
+        A.stats[static_cast<int64_t>(row) * A.slots + A.slot0 + p_tile * TILE::WP + wp] = make_float2(m, s);
+    }
+  } else if constexpr (KIND == CE_DL) {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
+      const bool there = row < n_q;
+      CeRow R = {0.0f, 0.0f, 0.0f, -1};
+      if (there) R = A.rows[row];
+      const int hot = R.token - A.v0;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        uint32_t h[4][3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = pw + 16 * i + e;
+          float x = fexp2(__builtin_fmaf(acc[i][j][e], LOG2E, -R.lse_hi) - R.lse_lo);
+          x = R.weight * (v == hot ? x - 1.0f : x);
+          if (!there || v >= A.n_p) x = 0.0f;
+          if constexpr (THREE) ce_parts(x, h[e]);
+          else h[e][0] = f32_to_bf16_bits(x);
+        }
+#pragma unroll
+        for (int s = 0; s < (THREE ? 3 : 1); ++s) {
+          const uint2 w = make_uint2(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16);
+          *reinterpret_cast<uint2*>(A.dl + s * A.dl_plane + row * A.ld_dl + pw + 16 * i) = w;
+        }
+      }
+    }
+  } else if constexpr (KIND == CE_DX) {
+    float* const sums = A.sums + blockIdx.y * A.split_stride;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        if (row >= n_q || pw + 16 * i >= A.n_p) continue;
+        ce_f32x4* const to = reinterpret_cast<ce_f32x4*>(sums + row * A.ld_sums + pw + 16 * i);
+        *to = A.add ? *to + acc[i][j] : acc[i][j];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int64_t v = qw + 16 * j;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        if (v >= n_q || pw + 16 * i >= A.n_p) continue;
+        const ce_f32x4 x = acc[i][j] * A.scale;
+        if constexpr (THREE) {
+          *reinterpret_cast<ce_f32x4*>(static_cast<float*>(A.grad) + v * A.ld_grad + pw + 16 * i) = x;
+        } else {
+          const uint2 w = make_uint2(f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16,
+                                     f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16);
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i) = w;
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Around the products.
+// ---------------------------------------------------------------------------
+struct CeRows {
+  int64_t n_rows;
+  int vocab;
+  int D;
+  const void* hidden;
+  const void* weight;
+  int64_t hidden_stride, weight_stride;
+  const int32_t* token;
+  const float* row_weight;
+  const uint8_t* valid;
+  float grad_scale;
+  float* row_loss;
+  float* logp_token;
+  double* scaled_loss;
+  uint8_t* row_status;
+  void* grad_hidden;
+  int64_t grad_stride;
+  // workspace
+  int* count;      // rows that take part (with a mask)
+  int* source;     // [rows that take part] their place in the call
+  int* place;      // [n_rows] the row's place among them, or -1
+  CeRow* rows;     // [rows that take part]
+  const float2* stats;
+  int slots;
+  const float* sums;
+  int64_t ld_sums, split_stride;
+  int splits;
+};
+
+// Rows of T as bf16 (T = float: as three parts), 64-element pieces whole: elements behind D are 0.
+// source: the rows to take (or NULL: all in order).
+template <typename T>
+__global__ __launch_bounds__(256) void ce_pack_kernel(const T* x, int64_t stride, int64_t n_rows, int D, const int* source,
+                                                      const int* count, uint16_t* to, int64_t ld, int64_t plane) {
+  const int64_t rows = count ? *count : n_rows;
+  const int pieces = static_cast<int>(ld / 8);
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < rows * pieces; i += gridDim.x * 256ll) {
+    const int64_t r = i / pieces;
+    const int d = static_cast<int>(i - r * pieces) * 8;
+    const T* from = x + (source ? static_cast<int64_t>(source[r]) : r) * stride + d;
+    uint4* const out = reinterpret_cast<uint4*>(to + r * ld + d);
+    if constexpr (sizeof(T) == 2) {
+      *out = d < D ? *reinterpret_cast<const uint4*>(from) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+      if (d < D) Loader<float>::load8(from, v);
+      uint32_t h[8][3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ce_parts(v[e], h[e]);
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+        out[s * (plane / 8)] = make_uint4(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16, h[4][s] | h[5][s] << 16, h[6][s] | h[7][s] << 16);
+    }
+  }
+}
+
+// A wave a row that takes part: its log-sum-exp from the tiles' maxima and sums, the target's logit as a product
+// of its own, and the row's outputs.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
+  const int lane = threadIdx.x & (WAVE - 1);
+  const int64_t i = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  if (i >= (P.count ? *P.count : P.n_rows)) return;
+  const int64_t r = P.count ? P.source[i] : i;
+  const int token = P.token[r];
+  const float weight = P.row_weight ? P.row_weight[r] : 1.0f;
+  const bool good = token >= 0 && token < P.vocab && isfinite(weight);
+  float dot = 0.0f;
+  if (good) {
+    const T* x = static_cast<const T*>(P.hidden) + r * P.hidden_stride;
+    const T* w = static_cast<const T*>(P.weight) + static_cast<int64_t>(token) * P.weight_stride;
+    for (int d = lane * 8; d < P.D; d += WAVE * 8) {
+      float a[8], b[8];
+      Loader<T>::load8(x + d, a);
+      Loader<T>::load8(w + d, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(a[e], b[e], dot);
+    }
+  }
+  dot = wave_sum(dot);
+  const float2* stats = P.stats + i * P.slots;
+  float m = -finf();
+  for (int s = lane; s < P.slots; s += WAVE) m = fmaxf(m, stats[s].x);
+  m = wave_max(m);
+  double sum = 0.0;
+  for (int s = lane; s < P.slots; s += WAVE) {
+    const float2 f = stats[s];
+    sum += static_cast<double>(f.y) * static_cast<double>(fexp2(f.x - m));
+  }
+#pragma unroll
+  for (int k = 1; k < WAVE; k *= 2) sum += __shfl_xor(sum, k);
+  const double lse2 = static_cast<double>(m) + log2(sum);
+  const double logp = static_cast<double>(dot) - lse2 / static_cast<double>(LOG2E);
+  const bool finite = isfinite(lse2) && (!good || isfinite(logp));
+  if (lane != 0) return;
+  CeRow R;
+  R.lse_hi = finite ? static_cast<float>(lse2) : nanf_();
+  R.lse_lo = finite ? static_cast<float>(lse2 - static_cast<double>(R.lse_hi)) : nanf_();
+  R.weight = good ? weight : 0.0f;
+  R.token = good ? token : -1;
+  if (!good) R.lse_hi = finf(), R.lse_lo = 0.0f;  // (the row's share is 0 at every token)
+  P.rows[i] = R;
+  const bool ok = good && finite;
+  const double loss = ok ? -static_cast<double>(weight) * logp : __builtin_nan("");
+  if (P.row_loss) P.row_loss[r] = static_cast<float>(loss);
+  if (P.logp_token) P.logp_token[r] = ok ? static_cast<float>(logp) : nanf_();
+  if (P.scaled_loss) P.scaled_loss[r] = static_cast<double>(P.grad_scale) * loss;
+  if (P.row_status) P.row_status[r] = !good ? SAKI_ROW_BAD_TARGET : finite ? SAKI_ROW_OK : SAKI_ROW_NONFINITE;
+}
+
+// grad_hidden from the splits' sums.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_grad_hidden_kernel(CeRows P) {
+  const int pieces = P.D / 8;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < P.n_rows * pieces; i += gridDim.x * 256ll) {
+    const int64_t r = i / pieces;
+    const int d = static_cast<int>(i - r * pieces) * 8;
+    const int64_t at = P.count ? P.place[r] : r;
+    float g[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = 0.0f;
+    if (at >= 0) {
+      for (int s = 0; s < P.splits; ++s) {
+        float v[8];
+        Loader<float>::load8(P.sums + s * P.split_stride + at * P.ld_sums + d, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] += v[e];
+      }
+      const float scale = P.rows[at].token < 0 ? nanf_() : P.grad_scale;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] *= scale;
+    }
+    Storer<T>::store8(static_cast<T*>(P.grad_hidden) + r * P.grad_stride + d, g);
+  }
+}
+
+// linear_ce.hip, a unit for each part (CeKind)
+template <int KIND>
+hipError_t launch_ce_part(const CeGemm& A, int tile, bool three, int splits, hipStream_t st);
+
+}  // namespace saki

@@ -307,6 +307,11 @@ saki_status abi_launched(hipError_t e, const char* kernel) {
 
 saki_status abi_cus(int* cus) { return device_cus(cus); }
 
+saki_status abi_loss_sum(const double* scaled, int64_t n, double* sum, hipStream_t st) {
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, st, scaled, n, sum);
+  return launched("loss_sum_kernel");
+}
+
 }  // namespace saki
 
 extern "C" {
@@ -328,6 +333,9 @@ size_t saki_workspace_bytes(int op, int64_t n_rows, int64_t vocab) {
     case SAKI_OP_KV_COMPACT:
     case SAKI_OP_KV_ATTENTION:
       return saki::kv_workspace_bytes(op, n_rows, vocab);
+    case SAKI_OP_TOP_LOGITS:
+    case SAKI_OP_DISTILL_TOP:
+      return saki::distill_workspace_bytes(op, n_rows, vocab);
     default:
       return 0;
   }
