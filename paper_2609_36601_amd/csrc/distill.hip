@@ -40,6 +40,19 @@ int64_t top_parts(int64_t n_rows, int64_t vocab) {
   return (chunks + each - 1) / each;
 }
 
+// The sample from which top_kernel guesses its first threshold, and the rank: the q-th of the sample's maxima has about
+// q len / sample entries of the row above it, give or take a standard deviation of that for sqrt(q).
+void top_guess(saki::TopParams* P, int64_t len) {
+  const int64_t full = len / SAKI_CHUNK;
+  P->sample = full >= 64 ? 2 : full >= 8 ? 1 : 0;
+  if (P->sample == 0) return;
+  const double want = static_cast<double>(P->k) * P->sample * saki::TOP_NW * SAKI_CHUNK / static_cast<double>(len);
+  int q = 1;
+  while (q - 3.0 * std::sqrt(static_cast<double>(q)) < want) ++q;
+  P->rank = q;
+  if (q > saki::TOP_NT / 2) P->sample = 0;  // (most lanes' maxima: the wave's own threshold does as well)
+}
+
 size_t round256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
@@ -99,6 +112,7 @@ saki_status saki_top_logits(const void* logits, int32_t dtype, int64_t n_rows, i
   const dim3 block(saki::TOP_NT);
   const int64_t slots = static_cast<int64_t>(cus) * 8;
   if (parts < 2) {
+    top_guess(&P, vocab);
     const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots)));
     if (bf16) hipLaunchKernelGGL((saki::top_kernel<uint16_t, saki::TOP_WHOLE>), grid, block, 0, hs, P);
     else hipLaunchKernelGGL((saki::top_kernel<float, saki::TOP_WHOLE>), grid, block, 0, hs, P);
@@ -108,6 +122,7 @@ saki_status saki_top_logits(const void* logits, int32_t dtype, int64_t n_rows, i
   const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
   P.parts = static_cast<int>(parts);
   P.part_len = static_cast<int>((chunks + parts - 1) / parts * SAKI_CHUNK);
+  top_guess(&P, vocab - (parts - 1) * P.part_len);  // (of the shortest part)
   P.info = static_cast<saki::TopPart*>(ws);
   P.keys = reinterpret_cast<uint64_t*>(P.info + n_rows * parts);
   const dim3 grid(static_cast<unsigned>(n_rows * parts)), rows(static_cast<unsigned>(n_rows));

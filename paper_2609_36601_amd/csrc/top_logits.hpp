@@ -1,20 +1,27 @@
 // The k largest logits of a row, best first, and the log-sum-exp of the others.
 //
-// One pass over the row.  Every wave keeps a list of candidates in LDS and a threshold L: the
-// k-th largest entry it knows (-infinity before it knows k).  An entry above L joins the
-// list; any other is not among the row's k largest and is added at once to the sum
-//   R = sum 2^((x - L) c),   c = log2(e) / tau,
-// whose terms are at most 1.  When the list is full, its k-th largest entry becomes L, the entries
-// below it go to R, and R is brought to the new reference.  So R holds exactly the entries that
-// are not listed: nothing is subtracted, and a rest of 1e-30 of the row is as exact as one of half
-// of it.  Equal entries: a candidate is the number (order-preserving image of the logit, ~index), so
-// all differ; an entry of a later chunk has to be above L, not at it, since a wave sees its chunks by
-// ascending index, and inside a chunk, where it does not, the numbers are compared.
+// One pass over the row.  Every wave keeps a list of candidates in LDS and a threshold L below which no
+// entry is among the row's k largest.  An entry above L joins the list; any other is added at once to
+//   R = sum 2^(x c - Lc),   c = log2(e) / tau,  Lc = L c rounded,
+// whose terms are at most 1.  When a list is full, its k-th largest entry becomes L, the entries below it go to
+// R, and R is brought to the new reference.  So R holds exactly the entries that are not listed: nothing is
+// subtracted, and a rest of 1e-20 of the row is as exact as one of half of it.
+//
+// The first L is a guess: from the maxima of a sample of the row, so low that the entries above it are
+// more than k with three standard deviations' certainty in a row without an order (some 200 to 600 of
+// 151,936 at k of 20 to 256; without a guess each wave would see k (1 + log(entries / k)) candidates).  A row that has fewer
+// than k entries above the guess is done again from L = -infinity.
+//
+// Candidates are rare in every lane and, k of them in 149 chunks, common in a wave: so a chunk costs the same with
+// and without.  A lane whose largest entry is above L leaves its sum out and puts its 16 entries as they are
+// into a queue in LDS; 64 such groups are looked into at a time.
+//
+// Equal entries: a candidate is the number (order-preserving image of the logit, ~index), so all differ.  An entry of a
+// later chunk has to be above L, not at it; inside a chunk, and in the queue, the numbers are compared.
+//
 // Terms below 2^-126 are lost in 32 bits: where R ends below TOP_RESCAN (everything else lies far
 // below the list, as with masked tokens), the row is read again with the reference at the largest
 // entry that is not listed.
-//
-// What bounds it: for whole rows HBM and VALU issue together, see top_kernel.
 #pragma once
 
 #include "common.hpp"
@@ -22,8 +29,8 @@
 namespace saki {
 
 struct TopPart {
-  double rest;  // sum over the part of 2^((x - ref) c), without its listed entries
-  float ref;
+  double rest;  // sum over the part of 2^(x c - reference(L)), without its listed entries
+  float L;
   int bad;  // an entry is not finite
 };
 
@@ -33,9 +40,11 @@ struct TopParams {
   int64_t stride;
   int V;
   int k;
-  int parts;      // a row's parts (TOP_PART, TOP_MERGE)
-  int part_len;   // entries of a part, whole chunks
-  float c;        // log2(e) / tau
+  int parts;     // a row's parts (TOP_PART, TOP_MERGE)
+  int part_len;  // entries of a part, whole chunks
+  float c;       // log2(e) / tau
+  int sample;    // chunks of a wave from whose maxima the first threshold is guessed (0: none),
+  int rank;      // and which of the 256 lanes' maxima it is
   float* top_logit;
   int32_t* top_token;
   int64_t top_stride;
@@ -49,8 +58,11 @@ enum TopMode { TOP_WHOLE, TOP_PART, TOP_MERGE };
 
 constexpr int TOP_NT = 256;
 constexpr int TOP_NW = TOP_NT / WAVE;
-constexpr int TOP_CAP = 512;  // candidates of a wave: more than SAKI_MAX_TOP_K + WAVE
+constexpr int TOP_CAP = 512;   // candidates of a wave
+constexpr int TOP_BEST = SAKI_MAX_TOP_K;
 static_assert(TOP_CAP >= SAKI_MAX_TOP_K + 2 * WAVE, "a list that was shortened takes another 64 entries");
+// R below this is computed again.
+constexpr double TOP_RESCAN = 0x1p-100;
 
 // The order-preserving image of a logit: BITS bits, never 0; -0 and +0 are alike.
 template <typename T>
@@ -66,10 +78,29 @@ struct TopKey {
   }
 };
 
+// Lc.  Where the product leaves the range: -3e38 keeps all terms at or below 1, +infinity makes them 0 (and the row is
+// read again).
+__device__ __forceinline__ float top_reference(float L, float c) {
+  const float r = L * c;
+  return r < -3.0e38f && L > -finf() ? -3.0e38f : r;
+}
+
+template <typename T>
 struct TopShared {
+  // groups of the queue: 64 are taken out at a time, 64 more come at most before that
+  static constexpr int GROUP = sizeof(T), QUEUE = 128;  // (16 entries: GROUP pieces of 16 bytes, by two)
   uint64_t list[TOP_NW][TOP_CAP];
-  uint64_t best[SAKI_MAX_TOP_K];  // the block's k largest, then in order
-  uint64_t sorted[SAKI_MAX_TOP_K];
+  union {
+    struct {
+      uint4 group[TOP_NW][sizeof(T) == 2 ? 2 : 4][QUEUE];
+      int place[TOP_NW][QUEUE];
+    };
+    struct {  // when the queues are empty
+      uint64_t best[TOP_BEST];
+      uint64_t sorted[TOP_BEST];
+    };
+    float maxima[TOP_NT];
+  };
   int count[TOP_NW];
   int n_best;
   double red_d[TOP_NW][RED_MAX];
@@ -81,77 +112,83 @@ __device__ __forceinline__ int lanes_below(uint64_t m) {
   return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
 }
 
-// The k-th largest of the candidates u[i] (0: none) of a wave's lanes, of which there are at
-// least k: bit by bit from the top, the largest number that k of them reach.  Every lane gets it.  The
-// index is only searched where more entries tie at the k-th value than are taken.
-template <typename T, int N>
-__device__ __forceinline__ uint64_t top_threshold(const uint64_t (&u)[N], int k) {
-  auto reach = [&](auto at_least) {
-    int n = 0;
+// How many of a wave's numbers u reach t.
+template <typename U, int N>
+__device__ __forceinline__ int top_reach(const U (&u)[N], U t) {
+  int n = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += __popcll(__ballot(at_least(u[i])));
-    return n;
-  };
-  uint32_t hi = 0;
-  for (int b = TopKey<T>::BITS - 1; b >= 0; --b) {
-    const uint32_t t = hi | (1u << b);
-    if (reach([&](uint64_t v) { return static_cast<uint32_t>(v >> 32) >= t; }) >= k) hi = t;
+  for (int i = 0; i < N; ++i) n += __popcll(__ballot(u[i] >= t));
+  return n;
+}
+
+// The largest number that k of a wave's u reach, bit by bit from `bit` down.
+template <typename U, int N>
+__device__ __forceinline__ U top_search(const U (&u)[N], int k, int bit, U found = 0) {
+  for (int b = bit; b >= 0; --b) {
+    const U t = found | (U{1} << b);
+    if (top_reach(u, t) >= k) found = t;
   }
-  const uint64_t whole = static_cast<uint64_t>(hi) << 32;
-  if (reach([&](uint64_t v) { return v >= whole; }) == k) return whole;
-  uint64_t low = whole;
-  for (int b = 31; b >= 0; --b) {
-    const uint64_t t = low | (1ull << b);
-    if (reach([&](uint64_t v) { return v >= t; }) >= k) low = t;
-  }
-  return low;
+  return found;
 }
 
 // A wave's candidates.
 template <typename T>
 struct WaveTop {
+  static constexpr int PIECES = sizeof(T) == 2 ? 2 : 4;  // 16-byte pieces of a lane's 16 entries
   uint64_t* list;  // LDS
   int lane, k;
   float c;
   int n;        // candidates in the list (the same in all lanes)
-  float L;      // the k-th largest entry so far, and the number of its candidate
-  uint64_t t;
-  double rest;  // this lane's part of R, relative to L
+  float L, Lc;  // the threshold, and R's reference
+  uint64_t t;   // a candidate's number is above it
+  double rest;  // this lane's part of R
 
-  __device__ __forceinline__ void init(uint64_t* lds, int l, int kk, float cc) {
-    list = lds;
-    lane = l;
-    k = kk;
-    c = cc;
+  __device__ __forceinline__ void start(float L_, uint64_t t_) {
     n = 0;
-    L = -finf();
-    t = 0ull;
+    L = L_;
+    Lc = top_reference(L, c);
+    t = t_;
     rest = 0.0;
   }
 
   static __device__ __forceinline__ uint64_t number(float x, int index) {
     return static_cast<uint64_t>(TopKey<T>::of(x)) << 32 | static_cast<uint32_t>(~index);
   }
+  static __device__ __forceinline__ float value(uint64_t u) { return TopKey<T>::value(static_cast<uint32_t>(u >> 32)); }
+  __device__ __forceinline__ float term(float x) const { return fexp2(__builtin_fmaf(x, c, -Lc)); }
 
   // Keeps the k largest candidates; the others go to the rest.
   __device__ __forceinline__ void shorten() {
     constexpr int N = TOP_CAP / WAVE;
-    uint64_t u[N];
+    uint32_t hi[N], lo[N];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < N; ++i) u[i] = i * WAVE + lane < n ? list[i * WAVE + lane] : 0ull;
-    t = top_threshold<T, N>(u, k);
-    const float to = TopKey<T>::value(static_cast<uint32_t>(t >> 32));
-    rest *= static_cast<double>(fexp2((L - to) * c));  // (0 stays 0: L = -infinity has no rest)
-    L = to;
+    for (int i = 0; i < N; ++i) {
+      const uint64_t u = i * WAVE + lane < n ? list[i * WAVE + lane] : 0ull;
+      hi[i] = static_cast<uint32_t>(u >> 32);
+      lo[i] = static_cast<uint32_t>(u);
+    }
+    const uint32_t th = top_search(hi, k, TopKey<T>::BITS - 1);
+    uint32_t tl = 0u;
+    const int above = top_reach(hi, th + 1u);
+    if (top_reach(hi, th) > k) {  // those at the k-th value with the lowest indices
+      uint32_t w[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = hi[i] == th ? lo[i] : 0u;
+      tl = top_search(w, k - above, 31);
+    }
+    t = static_cast<uint64_t>(th) << 32 | tl;
+    const float before = Lc;
+    L = TopKey<T>::value(th);
+    Lc = top_reference(L, c);
+    rest = rest != 0.0 ? rest * static_cast<double>(fexp2(before - Lc)) : 0.0;
     int m = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const bool keep = u[i] >= t;
+      const bool keep = hi[i] > th || (hi[i] == th && lo[i] >= tl);
       const uint64_t who = __ballot(keep);
-      if (keep) list[m + lanes_below(who)] = u[i];
-      else if (u[i] != 0ull)
-        rest += static_cast<double>(fexp2((TopKey<T>::value(static_cast<uint32_t>(u[i] >> 32)) - L) * c));
+      if (keep) list[m + lanes_below(who)] = static_cast<uint64_t>(hi[i]) << 32 | lo[i];
+      else if (hi[i] != 0u) rest += static_cast<double>(term(TopKey<T>::value(hi[i])));
       m += __popcll(who);
     }
     n = m;
@@ -166,26 +203,28 @@ struct WaveTop {
     const uint64_t who = __ballot(in);
     if (in) list[n + lanes_below(who)] = u;
     n += __popcll(who);
-    if (there && !in) rest += static_cast<double>(fexp2((x - L) * c));
+    if (there && !in) rest += static_cast<double>(term(x));
   }
 
-  // A lane's 16 entries of a chunk behind all chunks before, those with their bit in vm; base: the
-  // chunk's first index.
-  __device__ __forceinline__ void push_chunk(const float (&x)[EPL], uint32_t vm, int base) {
+  // 16 entries of each lane in `mine`, that of e at index base + elem_offset(0, e).
+  __device__ __forceinline__ void push_group(bool mine, const float (&x)[EPL], uint32_t vm, int base) {
     int more = 0;
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) more += __popcll(__ballot(((vm >> e) & 1u) && x[e] > L));
+    for (int e = 0; e < EPL; ++e) more += __popcll(__ballot(mine && x[e] >= L));
     if (n + more <= TOP_CAP) {
       float s = 0.0f;
 #pragma unroll
       for (int e = 0; e < EPL; ++e) {
-        const bool there = (vm >> e) & 1u, in = there && x[e] > L;
-        const uint64_t who = __ballot(in);
-        if (who != 0ull) {
-          if (in) list[n + lanes_below(who)] = number(x[e], base + elem_offset(lane, e));
+        const bool there = mine && ((vm >> e) & 1u);
+        bool in = there && x[e] >= L;
+        if (__ballot(in) != 0ull) {
+          const uint64_t u = number(x[e], base + elem_offset(0, e));
+          in = in && u > t;
+          const uint64_t who = __ballot(in);
+          if (in) list[n + lanes_below(who)] = u;
           n += __popcll(who);
         }
-        s += there && !in ? fexp2((x[e] - L) * c) : 0.0f;
+        s += there && !in ? term(x[e]) : 0.0f;
       }
       rest += static_cast<double>(s);
     } else {
@@ -194,160 +233,234 @@ struct WaveTop {
         float xe = x[0];
 #pragma unroll
         for (int i = 1; i < EPL; ++i) xe = i == e ? x[i] : xe;
-        push((vm >> e) & 1u, xe, base + elem_offset(lane, e));
+        push(mine && ((vm >> e) & 1u), xe, base + elem_offset(0, e));
       }
     }
   }
 };
 
-// R below this is computed again.
-constexpr double TOP_RESCAN = 0x1p-100;
-
 // TOP_WHOLE: a workgroup a row.  Few rows: TOP_PART, a workgroup for each part of a row, whose list
 // and rest go to the workspace, and TOP_MERGE, a workgroup a row that joins the parts.
 template <typename T, int MODE>
-__global__ __launch_bounds__(TOP_NT) void top_kernel(TopParams P) {
-  __shared__ TopShared sh;
-  Block<TOP_NT, TopShared> B(sh);
+__global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(TopParams P) {
+  __shared__ TopShared<T> sh;
+  Block<TOP_NT, TopShared<T>> B(sh);
+  constexpr int PIECES = WaveTop<T>::PIECES;
   const int k = P.k, lane = B.lane;
   const int wave = __builtin_amdgcn_readfirstlane(B.wave);
   const int64_t items = MODE == TOP_PART ? P.n_rows * P.parts : P.n_rows;
+  WaveTop<T> W;
+  W.list = sh.list[wave];
+  W.lane = lane;
+  W.k = k;
+  W.c = P.c;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t r = MODE == TOP_PART ? it / P.parts : it;
     const int part = MODE == TOP_PART ? static_cast<int>(it - r * P.parts) : 0;
-    WaveTop<T> W;
-    W.init(sh.list[wave], lane, k, P.c);
+    const int first = MODE == TOP_PART ? part * P.part_len : 0;
+    const int len = MODE == TOP_PART ? min(P.part_len, P.V - first) : P.V;
+    const T* row = static_cast<const T*>(P.x) + r * P.stride + first;
+    const int chunks = (len + CHUNK - 1) / CHUNK, full = len / CHUNK;
     float lo = finf(), hi = -finf();
     bool bad = false;
-    float ref = -finf();      // TOP_MERGE: the parts' largest reference, which is no more than the
-    double parts_rest = 0.0;  // row's k-th largest entry, and their rests relative to it
+    float ref = -finf();      // TOP_MERGE: the parts' largest reference, and their rests relative to it
+    double parts_rest = 0.0;
+    int total;
+    W.start(-finf(), 0ull);
     if constexpr (MODE == TOP_MERGE) {
-      for (int p = B.tid; p < P.parts; p += TOP_NT) ref = fmaxf(ref, P.info[r * P.parts + p].ref);
-      ref = B.max(ref);
+      // the parts' largest threshold is the row's
+      float L = -finf();
+      for (int p = B.tid; p < P.parts; p += TOP_NT) L = fmaxf(L, P.info[r * P.parts + p].L);
+      L = B.max(L);
+      ref = top_reference(L, P.c);
       for (int p = B.tid; p < P.parts; p += TOP_NT) {
         const TopPart f = P.info[r * P.parts + p];
         bad |= f.bad != 0;
-        if (f.rest != 0.0) parts_rest += f.rest * exp2((static_cast<double>(f.ref) - ref) * P.c);
+        if (f.rest != 0.0) parts_rest += f.rest * exp2(static_cast<double>(top_reference(f.L, P.c)) - ref);
       }
+      if (L > -finf()) W.start(L, static_cast<uint64_t>(TopKey<T>::of(L)) << 32);
       for (int p = wave; p < P.parts; p += TOP_NW)
         for (int i0 = 0; i0 < k; i0 += WAVE) {
           const int i = i0 + lane;
           const uint64_t u = i < k ? P.keys[(r * P.parts + p) * k + i] : 0ull;
-          W.push(u != 0ull, TopKey<T>::value(static_cast<uint32_t>(u >> 32)), static_cast<int>(~static_cast<uint32_t>(u)));
+          W.push(u != 0ull, WaveTop<T>::value(u), static_cast<int>(~static_cast<uint32_t>(u)));
         }
-    } else {
-      const int first = MODE == TOP_PART ? part * P.part_len : 0;
-      const int len = MODE == TOP_PART ? min(P.part_len, P.V - first) : P.V;
-      const T* row = static_cast<const T*>(P.x) + r * P.stride + first;
-      const int chunks = (len + CHUNK - 1) / CHUNK, full = len / CHUNK;
-      Frag<T> next;
-      if (wave < full) frag_load<true>(next, row, wave, lane);
-      for (int ch = wave; ch < chunks; ch += TOP_NW) {
+    } else if (P.sample > 0 && full >= TOP_NW * P.sample) {
+      // the guess
+      float m = -finf();
+      for (int s = 0; s < P.sample; ++s) {
+        Frag<T> f;
         float x[EPL];
-        uint32_t vm = 0xffffu;
-        if (ch < full) {
-          frag_unpack(next, x);
-          if (ch + TOP_NW < full) frag_load<true>(next, row, ch + TOP_NW, lane);
-        } else {
-          load_lane<T, true>(row, ch, lane, len, x, &vm);
-        }
-        float lm = -finf();
-        if (ch < full) {
+        frag_load<false>(f, row, static_cast<int>(static_cast<int64_t>(s * TOP_NW + wave) * full / (TOP_NW * P.sample)), lane);
+        frag_unpack(f, x);
 #pragma unroll
-          for (int e = 0; e < EPL; e += 2) {
+        for (int e = 0; e < EPL; e += 2) m = max3_raw(m, x[e], x[e + 1]);
+      }
+      sh.maxima[B.tid] = m;
+      __syncthreads();
+      uint32_t u[TOP_NW];
+#pragma unroll
+      for (int w = 0; w < TOP_NW; ++w) u[w] = TopKey<T>::of(sh.maxima[w * WAVE + lane]);
+      const uint32_t g = top_search(u, P.rank, TopKey<T>::BITS - 1);
+      const float L = TopKey<T>::value(g);
+      if (L > -finf() && L < finf()) W.start(L, static_cast<uint64_t>(g) << 32 | 0xffffffffu);
+      __syncthreads();
+    }
+    for (int attempt = 0;; ++attempt) {
+      if constexpr (MODE != TOP_MERGE) {
+        int queued = 0;
+        // looks into 64 groups of the queue (the last ones)
+        auto take_groups = [&]() __attribute__((always_inline)) {
+          __builtin_amdgcn_wave_barrier();
+          const int from = max(queued - WAVE, 0), at = from + lane;
+          const bool mine = at < queued;
+          Frag<T> f;
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) f.q[i] = sh.group[wave][i][at];
+          const int place = sh.place[wave][at];
+          float x[EPL];
+          frag_unpack(f, x);
+          __builtin_amdgcn_wave_barrier();
+          W.push_group(mine, x, 0xffffu, first + place);
+          queued = from;
+        };
+        Frag<T> next;
+        if (wave < full) frag_load<false>(next, row, wave, lane);
+        for (int ch = wave; ch < full; ch += TOP_NW) {
+          const Frag<T> now = next;
+          if (ch + TOP_NW < full) frag_load<false>(next, row, ch + TOP_NW, lane);
+          float x[EPL];
+          frag_unpack(now, x);
+          float lm = max3_raw(x[0], x[1], x[2]), s = 0.0f;
+          lo = min3_raw(lo, x[0], x[1]);
+#pragma unroll
+          for (int e = 2; e < EPL; e += 2) {
             lm = max3_raw(lm, x[e], x[e + 1]);
             lo = min3_raw(lo, x[e], x[e + 1]);
           }
-        } else {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) s += W.term(x[e]);
+          hi = fmaxf(hi, lm);
+          const bool in = lm > W.L;
+          W.rest += static_cast<double>(in ? 0.0f : s);
+          const uint64_t who = __ballot(in);
+          if (who != 0ull) {
+            if (in) {
+              const int at = queued + lanes_below(who);
+#pragma unroll
+              for (int i = 0; i < PIECES; ++i) sh.group[wave][i][at] = now.q[i];
+              sh.place[wave][at] = ch * CHUNK + 8 * lane;
+            }
+            queued += __popcll(who);
+            if (queued >= WAVE) take_groups();
+          }
+        }
+        while (queued > 0) take_groups();
+        if (full < chunks && full % TOP_NW == wave) {  // the last entries
+          float x[EPL];
+          uint32_t vm;
+          load_lane<T, true>(row, full, lane, len, x, &vm);
 #pragma unroll
           for (int e = 0; e < EPL; ++e)
             if ((vm >> e) & 1u) {
-              lm = fmaxf(lm, x[e]);
               lo = fminf(lo, x[e]);
+              hi = fmaxf(hi, x[e]);
             }
-        }
-        hi = fmaxf(hi, lm);
-        if (ch < full && !wave_any(lm > W.L)) {
-          float s = 0.0f;
-#pragma unroll
-          for (int e = 0; e < EPL; ++e) s += fexp2((x[e] - W.L) * P.c);
-          W.rest += static_cast<double>(s);
-        } else {
-          W.push_chunk(x, vm, first + ch * CHUNK);
+          W.push_group(true, x, vm, first + full * CHUNK + 8 * lane);
         }
       }
-    }
-    if (W.n > k) W.shorten();
-    // the block: its k largest of at most TOP_NW k
-    if (lane == 0) sh.count[wave] = W.n;
-    if (B.tid == 0) sh.n_best = 0;
-    __syncthreads();
-    int total = 0;
+      if (W.n > max(k, WAVE)) W.shorten();
+      __syncthreads();  // (the queues' place is the block's list's)
+      if (lane == 0) sh.count[wave] = W.n;
+      if (B.tid == 0) sh.n_best = 0;
+      __syncthreads();
+      total = 0;
 #pragma unroll
-    for (int w = 0; w < TOP_NW; ++w) total += sh.count[w];
+      for (int w = 0; w < TOP_NW; ++w) total += sh.count[w];
+      // fewer than there are: the guess was too high
+      if (MODE == TOP_MERGE || attempt > 0 || uniform(total >= min(k, len))) break;
+      W.start(-finf(), 0ull);
+      __syncthreads();
+    }
+    // the block's k largest: those that reach the k-th value, or where more than LDS holds tie at it, those
+    // with the lowest indices
     uint64_t t = 1ull;
     float to;
     auto threshold = [&](auto entries) {
       constexpr int N = decltype(entries)::value;
-      uint64_t u[N];
+      uint32_t v[N], low[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int w = i / (N / TOP_NW), j = (i % (N / TOP_NW)) * WAVE + lane;
-        u[i] = j < sh.count[w] ? sh.list[w][j] : 0ull;
+        const uint64_t u = j < sh.count[w] ? sh.list[w][j] : 0ull;
+        v[i] = static_cast<uint32_t>(u >> 32);
+        low[i] = static_cast<uint32_t>(u);
       }
-      return top_threshold<T, N>(u, k);
+      const uint32_t th = top_search(v, k, TopKey<T>::BITS - 1);
+      uint32_t tl = 0u;
+      if (top_reach(v, th) > TOP_BEST) {
+        const int above = top_reach(v, th + 1u);
+#pragma unroll
+        for (int i = 0; i < N; ++i) low[i] = v[i] == th ? low[i] : 0u;
+        tl = top_search(low, k - above, 31);
+      }
+      return static_cast<uint64_t>(th) << 32 | tl;
     };
     if (total > k) {
-      t = k <= WAVE ? threshold(std::integral_constant<int, TOP_NW>())
-                    : threshold(std::integral_constant<int, TOP_NW * SAKI_MAX_TOP_K / WAVE>());
-      to = TopKey<T>::value(static_cast<uint32_t>(t >> 32));
+      const bool few = max(max(sh.count[0], sh.count[1]), max(sh.count[2], sh.count[3])) <= WAVE;
+      t = few ? threshold(std::integral_constant<int, TOP_NW>())
+              : threshold(std::integral_constant<int, TOP_NW * SAKI_MAX_TOP_K / WAVE>());
+      to = WaveTop<T>::value(t);
     } else {
-      to = B.max(fmaxf(W.L, ref));  // (one wave, or one part, has all that there is)
+      to = B.max(W.L);  // (one wave, or one part, has all that there is)
     }
     // this wave's entries: to the block's list, or to the rest
-    double rest = W.rest != 0.0 ? W.rest * exp2((static_cast<double>(W.L) - to) * P.c) : 0.0;
+    const float to_c = top_reference(to, P.c);
+    double rest = W.rest != 0.0 ? W.rest * exp2(static_cast<double>(W.Lc) - to_c) : 0.0;
     for (int i0 = 0; i0 < W.n; i0 += WAVE) {
       const int i = i0 + lane;
       const uint64_t u = i < W.n ? sh.list[wave][i] : 0ull;
       if (u >= t) {
         sh.best[atomicAdd(&sh.n_best, 1)] = u;
       } else if (u != 0ull) {
-        rest += static_cast<double>(fexp2((TopKey<T>::value(static_cast<uint32_t>(u >> 32)) - to) * P.c));
+        rest += static_cast<double>(fexp2(__builtin_fmaf(WaveTop<T>::value(u), P.c, -to_c)));
       }
     }
-    if (MODE == TOP_MERGE && parts_rest != 0.0) rest += parts_rest * exp2((static_cast<double>(ref) - to) * P.c);
+    if (MODE == TOP_MERGE && parts_rest != 0.0) rest += parts_rest * exp2(static_cast<double>(ref) - to_c);
     double v[2];
     v[0] = rest;
     v[1] = (MODE != TOP_MERGE && !(lo > -finf() && hi < finf())) || bad ? 1.0 : 0.0;
     B.sum(v);
-    const int n = sh.n_best;
+    const int found = sh.n_best, n = min(found, k);
+    // ranks by counting: all numbers differ; what ties behind the k-th place is at `to`, a term of 1 (or of what the
+    // rounding of the reference leaves)
+    if (B.tid < found) {
+      const uint64_t mine = sh.best[B.tid];
+      int rank = 0;
+      for (int j = 0; j < found; ++j) rank += sh.best[j] > mine ? 1 : 0;
+      sh.sorted[rank] = mine;
+    }
+    __syncthreads();
+    if (found > n) v[0] += static_cast<double>(found - n) * static_cast<double>(fexp2(__builtin_fmaf(to, P.c, -to_c)));
     const bool wrong = v[1] != 0.0 || !(v[0] < __builtin_huge_val());
     if constexpr (MODE == TOP_PART) {
       uint64_t* keys = P.keys + it * k;
-      for (int i = B.tid; i < k; i += TOP_NT) keys[i] = i < n ? sh.best[i] : 0ull;
+      for (int i = B.tid; i < k; i += TOP_NT) keys[i] = i < n ? sh.sorted[i] : 0ull;
       if (B.tid == 0) P.info[it] = TopPart{v[0], to, wrong ? 1 : 0};
     } else {
-      // ranks by counting: all keys differ
-      if (B.tid < n) {
-        const uint64_t mine = sh.best[B.tid];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh.best[j] > mine ? 1 : 0;
-        sh.sorted[rank] = mine;
-      }
-      __syncthreads();
       if (B.tid < k) {
         const uint64_t u = B.tid < n ? sh.sorted[B.tid] : 0ull;
         const bool none = wrong || u == 0ull;
-        P.top_logit[r * P.top_stride + B.tid] = none ? nanf_() : TopKey<T>::value(static_cast<uint32_t>(u >> 32));
+        P.top_logit[r * P.top_stride + B.tid] = none ? nanf_() : WaveTop<T>::value(u);
         P.top_token[r * P.top_stride + B.tid] = none ? -1 : static_cast<int32_t>(~static_cast<uint32_t>(u));
       }
-      double other = static_cast<double>(to) + log2(v[0]) / P.c;
+      double other = (static_cast<double>(to_c) + log2(v[0])) / P.c;
       if (P.rest_logit && !wrong && v[0] < TOP_RESCAN && n < P.V) {
-        const T* row = static_cast<const T*>(P.x) + r * P.stride;
+        const T* whole = static_cast<const T*>(P.x) + r * P.stride;
         const uint64_t least = sh.sorted[n - 1];
         float m = -finf();
         auto others = [&](auto&& take) {
-          for_chunks1<T, TOP_NW>(row, P.V, wave, lane, [&](auto tail, const float* x, uint32_t vm, int ch) {
+          for_chunks1<T, TOP_NW>(whole, P.V, wave, lane, [&](auto tail, const float* x, uint32_t vm, int ch) {
             constexpr bool TAIL = decltype(tail)::value;
 #pragma unroll
             for (int e = 0; e < EPL; ++e)

@@ -68,12 +68,15 @@ def test_temperatures(saki_lib, dtype, tau):
 
 
 @pytest.mark.parametrize("n", [2, 600])
-@pytest.mark.parametrize("kind", ["equal", "two_values", "rising", "falling", "zeros", "blocks", "peak"])
+@pytest.mark.parametrize("kind", ["equal", "two_values", "rising", "falling", "zeros", "blocks", "peak", "sampled", "sampled_ties"])
 def test_orders_and_ties(saki_lib, kind, n):
     V = 20011
     i = np.arange(V)
     x = {"equal": np.full(V, 2.5), "two_values": (i % 3 == 0) * 1.0, "rising": i * 0.125, "falling": -i * 0.125,
-         "zeros": np.where(i % 2 == 0, 0.0, -0.0), "blocks": np.floor(i / 700) % 5, "peak": np.where(i == 15000, 30.0, 0.0)}[kind]
+         "zeros": np.where(i % 2 == 0, 0.0, -0.0), "blocks": np.floor(i / 700) % 5, "peak": np.where(i == 15000, 30.0, 0.0),
+         # (a first chunk whose 64 lanes each hold a large entry: a threshold guessed from it leaves fewer than 90)
+         "sampled": np.where((i < 512) & (i % 8 == 0), 5.0 + i / 64, i * -0.001),
+         "sampled_ties": np.where((i < 512) & (i % 8 == 0), 5.0, (i % 11) * 0.25)}[kind]
     for dtype in (torch.bfloat16, torch.float32):
         check(rows(np.tile(x, (n, 1)), dtype), 90)
 
