@@ -35,22 +35,7 @@ constexpr int64_t TOP_ITEMS = 1024, TOP_PART_CHUNKS = 8, TOP_MOST_PARTS = 64;
 int64_t top_parts(int64_t n_rows, int64_t vocab) {
   const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
   const int64_t want = std::min({(TOP_ITEMS + n_rows - 1) / n_rows, chunks / TOP_PART_CHUNKS, TOP_MOST_PARTS});
-  if (n_rows > TOP_ITEMS / 2 || want < 2) return 1;
-  const int64_t each = (chunks + want - 1) / want;
-  return (chunks + each - 1) / each;
-}
-
-// The sample from which top_kernel guesses its first threshold, and the rank: the q-th of the sample's maxima has about
-// q len / sample entries of the row above it, give or take a standard deviation of that for sqrt(q).
-void top_guess(saki::TopParams* P, int64_t len) {
-  const int64_t full = len / SAKI_CHUNK;
-  P->sample = full >= 64 ? 2 : full >= 8 ? 1 : 0;
-  if (P->sample == 0) return;
-  const double want = static_cast<double>(P->k) * P->sample * saki::TOP_NW * SAKI_CHUNK / static_cast<double>(len);
-  int q = 1;
-  while (q - 3.0 * std::sqrt(static_cast<double>(q)) < want) ++q;
-  P->rank = q;
-  if (q > saki::TOP_NT / 2) P->sample = 0;  // (most lanes' maxima: the wave's own threshold does as well)
+  return n_rows > TOP_ITEMS / 2 || want < 2 ? 1 : want;
 }
 
 size_t round256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
@@ -92,9 +77,6 @@ saki_status saki_top_logits(const void* logits, int32_t dtype, int64_t n_rows, i
       return abi_fail(SAKI_E_WORKSPACE, "workspace NULL or smaller than saki_workspace_bytes(SAKI_OP_TOP_LOGITS)");
     if (!aligned(ws, 16)) return abi_fail(SAKI_E_ALIGN, "workspace must be 16-byte aligned");
   }
-  int cus = 0;
-  st = saki::abi_cus(&cus);
-  if (st != SAKI_OK) return st;
   saki::TopParams P{};
   P.x = logits;
   P.n_rows = n_rows;
@@ -110,19 +92,15 @@ saki_status saki_top_logits(const void* logits, int32_t dtype, int64_t n_rows, i
   hipStream_t hs = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == SAKI_BF16;
   const dim3 block(saki::TOP_NT);
-  const int64_t slots = static_cast<int64_t>(cus) * 8;
   if (parts < 2) {
-    top_guess(&P, vocab);
-    const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots)));
+    // (a workgroup a row: several a workgroup that stays leave the last of them to fewer)
+    const dim3 grid(static_cast<unsigned>(std::min(n_rows, int64_t{1} << 22)));
     if (bf16) hipLaunchKernelGGL((saki::top_kernel<uint16_t, saki::TOP_WHOLE>), grid, block, 0, hs, P);
     else hipLaunchKernelGGL((saki::top_kernel<float, saki::TOP_WHOLE>), grid, block, 0, hs, P);
     st = saki::abi_launched(hipGetLastError(), "top_kernel");
     return st != SAKI_OK ? st : saki::abi_ok();
   }
-  const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
   P.parts = static_cast<int>(parts);
-  P.part_len = static_cast<int>((chunks + parts - 1) / parts * SAKI_CHUNK);
-  top_guess(&P, vocab - (parts - 1) * P.part_len);  // (of the shortest part)
   P.info = static_cast<saki::TopPart*>(ws);
   P.keys = reinterpret_cast<uint64_t*>(P.info + n_rows * parts);
   const dim3 grid(static_cast<unsigned>(n_rows * parts)), rows(static_cast<unsigned>(n_rows));

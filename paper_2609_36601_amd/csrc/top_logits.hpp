@@ -41,10 +41,7 @@ struct TopParams {
   int V;
   int k;
   int parts;     // a row's parts (TOP_PART, TOP_MERGE)
-  int part_len;  // entries of a part, whole chunks
   float c;       // log2(e) / tau
-  int sample;    // chunks of a wave from whose maxima the first threshold is guessed (0: none),
-  int rank;      // and which of the 256 lanes' maxima it is
   float* top_logit;
   int32_t* top_token;
   int64_t top_stride;
@@ -54,11 +51,21 @@ struct TopParams {
   TopPart* info;   // [n_rows, parts]
 };
 
-enum TopMode { TOP_WHOLE, TOP_PART, TOP_MERGE };
-
 constexpr int TOP_NT = 256;
 constexpr int TOP_NW = TOP_NT / WAVE;
-constexpr int TOP_CAP = 512;   // candidates of a wave
+// The sample of a row (or part) of `full` whole chunks: so many chunks of each wave.  Which of the 256 lanes' maxima is the
+// guess: the q-th has about q len / sample entries above it, give or take a standard deviation of that for sqrt(q), and
+// k <= (q - 3 sqrt(q)) len / sample.
+__device__ __forceinline__ int top_sample(int full) { return full >= 64 ? 2 : full >= TOP_NW ? 1 : 0; }
+__device__ __forceinline__ int top_rank(int k, int sample, int len) {
+  const float want = static_cast<float>(k) * static_cast<float>(sample * TOP_NW * CHUNK) / static_cast<float>(len);
+  const float root = 0.5f * (3.0f + __builtin_sqrtf(9.0f + 4.0f * want));
+  return static_cast<int>(root * root) + 1;
+}
+
+enum TopMode { TOP_WHOLE, TOP_PART, TOP_MERGE };
+
+constexpr int TOP_CAP = 384;   // candidates of a wave
 constexpr int TOP_BEST = SAKI_MAX_TOP_K;
 static_assert(TOP_CAP >= SAKI_MAX_TOP_K + 2 * WAVE, "a list that was shortened takes another 64 entries");
 // R below this is computed again.
@@ -87,8 +94,9 @@ __device__ __forceinline__ float top_reference(float L, float c) {
 
 template <typename T>
 struct TopShared {
-  // groups of the queue: 64 are taken out at a time, 64 more come at most before that
-  static constexpr int GROUP = sizeof(T), QUEUE = 128;  // (16 entries: GROUP pieces of 16 bytes, by two)
+  // Groups of the queue: TAKE at least (and 64 at most) are taken out at a time, 64 more come at most before that.
+  // (f32: so that four workgroups fit a CU)
+  static constexpr int TAKE = sizeof(T) == 2 ? 64 : 32, QUEUE = TAKE + WAVE;
   uint64_t list[TOP_NW][TOP_CAP];
   union {
     struct {
@@ -110,6 +118,20 @@ struct TopShared {
 
 __device__ __forceinline__ int lanes_below(uint64_t m) {
   return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0));
+}
+
+// frag_unpack's inverse.
+__device__ __forceinline__ void frag_pack(Frag<uint16_t>& f, const float (&x)[EPL]) {
+  uint32_t w[EPL / 2];
+#pragma unroll
+  for (int i = 0; i < EPL / 2; ++i) w[i] = __float_as_uint(x[2 * i]) >> 16 | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
+  f.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  f.q[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+__device__ __forceinline__ void frag_pack(Frag<float>& f, const float (&x)[EPL]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f.q[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
 }
 
 // How many of a wave's numbers u reach t.
@@ -206,8 +228,8 @@ struct WaveTop {
     if (there && !in) rest += static_cast<double>(term(x));
   }
 
-  // 16 entries of each lane in `mine`, that of e at index base + elem_offset(0, e).
-  __device__ __forceinline__ void push_group(bool mine, const float (&x)[EPL], uint32_t vm, int base) {
+  // 16 entries of each lane in `mine` (-infinity: none), that of e at index base + elem_offset(0, e).
+  __device__ __forceinline__ void push_group(bool mine, const float (&x)[EPL], int base) {
     int more = 0;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) more += __popcll(__ballot(mine && x[e] >= L));
@@ -215,7 +237,7 @@ struct WaveTop {
       float s = 0.0f;
 #pragma unroll
       for (int e = 0; e < EPL; ++e) {
-        const bool there = mine && ((vm >> e) & 1u);
+        const bool there = mine && x[e] != -finf();
         bool in = there && x[e] >= L;
         if (__ballot(in) != 0ull) {
           const uint64_t u = number(x[e], base + elem_offset(0, e));
@@ -233,16 +255,28 @@ struct WaveTop {
         float xe = x[0];
 #pragma unroll
         for (int i = 1; i < EPL; ++i) xe = i == e ? x[i] : xe;
-        push(mine && ((vm >> e) & 1u), xe, base + elem_offset(0, e));
+        push(mine && xe != -finf(), xe, base + elem_offset(0, e));
       }
     }
   }
 };
 
+// 2^d to 32 bits' precision, of any size.
+__device__ __forceinline__ double top_exp2(double d) {
+  const double whole = rint(fmax(d, -2000.0));
+  return ldexp(static_cast<double>(fexp2(static_cast<float>(d - whole))), static_cast<int>(whole));
+}
+// log2 of x > 0, off by some 2^-23.
+__device__ __forceinline__ double top_log2(double x) {
+  int e;
+  const double m = frexp(x, &e);
+  return static_cast<double>(flog2(static_cast<float>(m))) + e;
+}
+
 // TOP_WHOLE: a workgroup a row.  Few rows: TOP_PART, a workgroup for each part of a row, whose list
 // and rest go to the workspace, and TOP_MERGE, a workgroup a row that joins the parts.
 template <typename T, int MODE>
-__global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(TopParams P) {
+__global__ __launch_bounds__(TOP_NT, 4) void top_kernel(TopParams P) {
   __shared__ TopShared<T> sh;
   Block<TOP_NT, TopShared<T>> B(sh);
   constexpr int PIECES = WaveTop<T>::PIECES;
@@ -257,8 +291,10 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t r = MODE == TOP_PART ? it / P.parts : it;
     const int part = MODE == TOP_PART ? static_cast<int>(it - r * P.parts) : 0;
-    const int first = MODE == TOP_PART ? part * P.part_len : 0;
-    const int len = MODE == TOP_PART ? min(P.part_len, P.V - first) : P.V;
+    // (parts of whole chunks, as even as they can be)
+    const int all_chunks = (P.V + CHUNK - 1) / CHUNK;
+    const int first = MODE == TOP_PART ? part * all_chunks / P.parts * CHUNK : 0;
+    const int len = MODE == TOP_PART ? min((part + 1) * all_chunks / P.parts * CHUNK, P.V) - first : P.V;
     const T* row = static_cast<const T*>(P.x) + r * P.stride + first;
     const int chunks = (len + CHUNK - 1) / CHUNK, full = len / CHUNK;
     float lo = finf(), hi = -finf();
@@ -276,7 +312,7 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
       for (int p = B.tid; p < P.parts; p += TOP_NT) {
         const TopPart f = P.info[r * P.parts + p];
         bad |= f.bad != 0;
-        if (f.rest != 0.0) parts_rest += f.rest * exp2(static_cast<double>(top_reference(f.L, P.c)) - ref);
+        if (f.rest != 0.0) parts_rest += f.rest * top_exp2(static_cast<double>(top_reference(f.L, P.c)) - ref);
       }
       if (L > -finf()) W.start(L, static_cast<uint64_t>(TopKey<T>::of(L)) << 32);
       for (int p = wave; p < P.parts; p += TOP_NW)
@@ -285,13 +321,13 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
           const uint64_t u = i < k ? P.keys[(r * P.parts + p) * k + i] : 0ull;
           W.push(u != 0ull, WaveTop<T>::value(u), static_cast<int>(~static_cast<uint32_t>(u)));
         }
-    } else if (P.sample > 0 && full >= TOP_NW * P.sample) {
-      // the guess
+    } else if (const int sample = top_sample(full), rank = top_rank(k, sample, len); sample > 0 && rank <= TOP_NT / 2) {
+      // the guess (of more maxima it would be no better than a wave's own threshold)
       float m = -finf();
-      for (int s = 0; s < P.sample; ++s) {
+      for (int s = 0; s < sample; ++s) {
         Frag<T> f;
         float x[EPL];
-        frag_load<false>(f, row, static_cast<int>(static_cast<int64_t>(s * TOP_NW + wave) * full / (TOP_NW * P.sample)), lane);
+        frag_load<false>(f, row, static_cast<int>(static_cast<int64_t>(s * TOP_NW + wave) * full / (TOP_NW * sample)), lane);
         frag_unpack(f, x);
 #pragma unroll
         for (int e = 0; e < EPL; e += 2) m = max3_raw(m, x[e], x[e + 1]);
@@ -301,75 +337,80 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
       uint32_t u[TOP_NW];
 #pragma unroll
       for (int w = 0; w < TOP_NW; ++w) u[w] = TopKey<T>::of(sh.maxima[w * WAVE + lane]);
-      const uint32_t g = top_search(u, P.rank, TopKey<T>::BITS - 1);
+      const uint32_t g = top_search(u, rank, TopKey<T>::BITS - 1);
       const float L = TopKey<T>::value(g);
       if (L > -finf() && L < finf()) W.start(L, static_cast<uint64_t>(g) << 32 | 0xffffffffu);
       __syncthreads();
     }
     for (int attempt = 0;; ++attempt) {
       if constexpr (MODE != TOP_MERGE) {
-        int queued = 0;
-        // looks into 64 groups of the queue (the last ones)
-        auto take_groups = [&]() __attribute__((always_inline)) {
-          __builtin_amdgcn_wave_barrier();
-          const int from = max(queued - WAVE, 0), at = from + lane;
-          const bool mine = at < queued;
-          Frag<T> f;
-#pragma unroll
-          for (int i = 0; i < PIECES; ++i) f.q[i] = sh.group[wave][i][at];
-          const int place = sh.place[wave][at];
-          float x[EPL];
-          frag_unpack(f, x);
-          __builtin_amdgcn_wave_barrier();
-          W.push_group(mine, x, 0xffffu, first + place);
-          queued = from;
-        };
-        Frag<T> next;
-        if (wave < full) frag_load<false>(next, row, wave, lane);
-        for (int ch = wave; ch < full; ch += TOP_NW) {
-          const Frag<T> now = next;
-          if (ch + TOP_NW < full) frag_load<false>(next, row, ch + TOP_NW, lane);
-          float x[EPL];
-          frag_unpack(now, x);
-          float lm = max3_raw(x[0], x[1], x[2]), s = 0.0f;
-          lo = min3_raw(lo, x[0], x[1]);
-#pragma unroll
-          for (int e = 2; e < EPL; e += 2) {
-            lm = max3_raw(lm, x[e], x[e + 1]);
-            lo = min3_raw(lo, x[e], x[e + 1]);
-          }
-#pragma unroll
-          for (int e = 0; e < EPL; ++e) s += W.term(x[e]);
-          hi = fmaxf(hi, lm);
-          const bool in = lm > W.L;
-          W.rest += static_cast<double>(in ? 0.0f : s);
-          const uint64_t who = __ballot(in);
-          if (who != 0ull) {
-            if (in) {
-              const int at = queued + lanes_below(who);
-#pragma unroll
-              for (int i = 0; i < PIECES; ++i) sh.group[wave][i][at] = now.q[i];
-              sh.place[wave][at] = ch * CHUNK + 8 * lane;
-            }
-            queued += __popcll(who);
-            if (queued >= WAVE) take_groups();
-          }
+        int queued = 0, ch = wave;
+        // two chunks under way (on every path a load, of the last chunk again: see for_chunks)
+        Frag<T> next, later;
+        if (ch < full) {
+          frag_load<false>(next, row, ch, lane);
+          frag_load<false>(later, row, ch + TOP_NW < full ? ch + TOP_NW : ch, lane);
         }
-        while (queued > 0) take_groups();
-        if (full < chunks && full % TOP_NW == wave) {  // the last entries
-          float x[EPL];
-          uint32_t vm;
-          load_lane<T, true>(row, full, lane, len, x, &vm);
+        for (;;) {
+          if (ch < chunks) {
+            Frag<T> now = next;
+            float x[EPL];
+            uint32_t vm = 0xffffu;
+            if (ch < full) {
+              next = later;
+              frag_load<false>(later, row, ch + 2 * TOP_NW < full ? ch + 2 * TOP_NW : ch, lane);
+              frag_unpack(now, x);
+              lo = min3_raw(lo, x[0], x[1]);
 #pragma unroll
-          for (int e = 0; e < EPL; ++e)
-            if ((vm >> e) & 1u) {
-              lo = fminf(lo, x[e]);
-              hi = fmaxf(hi, x[e]);
+              for (int e = 2; e < EPL; e += 2) lo = min3_raw(lo, x[e], x[e + 1]);
+            } else {  // the last entries; -infinity where there are none
+              load_lane<T, true>(row, ch, lane, len, x, &vm);
+#pragma unroll
+              for (int e = 0; e < EPL; ++e) {
+                const bool there = (vm >> e) & 1u;
+                lo = there ? fminf(lo, x[e]) : lo;
+                x[e] = there ? x[e] : -finf();
+              }
+              frag_pack(now, x);
             }
-          W.push_group(true, x, vm, first + full * CHUNK + 8 * lane);
+            float lm = max3_raw(x[0], x[1], x[2]), s = 0.0f;
+#pragma unroll
+            for (int e = 2; e < EPL; e += 2) lm = max3_raw(lm, x[e], x[e + 1]);
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) s += W.term(x[e]);
+            hi = fmaxf(hi, lm);
+            const bool in = lm > W.L;
+            W.rest += static_cast<double>(in || vm == 0u ? 0.0f : s);
+            const uint64_t who = __ballot(in);
+            if (who != 0ull) {
+              if (in) {
+                const int at = queued + lanes_below(who);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) sh.group[wave][i][at] = now.q[i];
+                sh.place[wave][at] = ch * CHUNK + 8 * lane;
+              }
+              queued += __popcll(who);
+            }
+            ch += TOP_NW;
+          }
+          if (queued >= TopShared<T>::TAKE || (ch >= chunks && queued > 0)) {  // looks into 64 groups (the last ones)
+            __builtin_amdgcn_wave_barrier();
+            const int from = max(queued - WAVE, 0), at = min(from + lane, queued - 1);
+            const bool mine = from + lane < queued;
+            Frag<T> f;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) f.q[i] = sh.group[wave][i][at];
+            const int place = sh.place[wave][at];
+            float x[EPL];
+            frag_unpack(f, x);
+            __builtin_amdgcn_wave_barrier();
+            W.push_group(mine, x, first + place);
+            queued = from;
+          } else if (ch >= chunks) {
+            break;
+          }
         }
       }
-      if (W.n > max(k, WAVE)) W.shorten();
       __syncthreads();  // (the queues' place is the block's list's)
       if (lane == 0) sh.count[wave] = W.n;
       if (B.tid == 0) sh.n_best = 0;
@@ -407,16 +448,16 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
       return static_cast<uint64_t>(th) << 32 | tl;
     };
     if (total > k) {
-      const bool few = max(max(sh.count[0], sh.count[1]), max(sh.count[2], sh.count[3])) <= WAVE;
-      t = few ? threshold(std::integral_constant<int, TOP_NW>())
-              : threshold(std::integral_constant<int, TOP_NW * SAKI_MAX_TOP_K / WAVE>());
+      const bool few = max(max(sh.count[0], sh.count[1]), max(sh.count[2], sh.count[3])) <= 2 * WAVE;
+      t = uniform(few) ? threshold(std::integral_constant<int, 2 * TOP_NW>())
+                       : threshold(std::integral_constant<int, TOP_NW * TOP_CAP / WAVE>());
       to = WaveTop<T>::value(t);
     } else {
       to = B.max(W.L);  // (one wave, or one part, has all that there is)
     }
     // this wave's entries: to the block's list, or to the rest
     const float to_c = top_reference(to, P.c);
-    double rest = W.rest != 0.0 ? W.rest * exp2(static_cast<double>(W.Lc) - to_c) : 0.0;
+    double rest = W.rest != 0.0 ? W.rest * top_exp2(static_cast<double>(W.Lc) - to_c) : 0.0;
     for (int i0 = 0; i0 < W.n; i0 += WAVE) {
       const int i = i0 + lane;
       const uint64_t u = i < W.n ? sh.list[wave][i] : 0ull;
@@ -426,7 +467,7 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
         rest += static_cast<double>(fexp2(__builtin_fmaf(WaveTop<T>::value(u), P.c, -to_c)));
       }
     }
-    if (MODE == TOP_MERGE && parts_rest != 0.0) rest += parts_rest * exp2(static_cast<double>(ref) - to_c);
+    if (MODE == TOP_MERGE && parts_rest != 0.0) rest += parts_rest * top_exp2(static_cast<double>(ref) - to_c);
     double v[2];
     v[0] = rest;
     v[1] = (MODE != TOP_MERGE && !(lo > -finf() && hi < finf())) || bad ? 1.0 : 0.0;
@@ -454,25 +495,34 @@ __global__ __launch_bounds__(TOP_NT, sizeof(T) == 2 ? 4 : 3) void top_kernel(Top
         P.top_logit[r * P.top_stride + B.tid] = none ? nanf_() : WaveTop<T>::value(u);
         P.top_token[r * P.top_stride + B.tid] = none ? -1 : static_cast<int32_t>(~static_cast<uint32_t>(u));
       }
-      double other = (static_cast<double>(to_c) + log2(v[0])) / P.c;
-      if (P.rest_logit && !wrong && v[0] < TOP_RESCAN && n < P.V) {
+      double other = (static_cast<double>(to_c) + top_log2(v[0])) / P.c;
+      if (P.rest_logit && uniform(!wrong && v[0] < TOP_RESCAN && n < P.V)) {
         const T* whole = static_cast<const T*>(P.x) + r * P.stride;
         const uint64_t least = sh.sorted[n - 1];
         float m = -finf();
-        auto others = [&](auto&& take) {
-          for_chunks1<T, TOP_NW>(whole, P.V, wave, lane, [&](auto tail, const float* x, uint32_t vm, int ch) {
-            constexpr bool TAIL = decltype(tail)::value;
+        double s[1] = {0.0};
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+          for (int ch = wave; ch < (P.V + CHUNK - 1) / CHUNK; ch += TOP_NW) {
+            float x[EPL];
+            uint32_t vm;
+            load_lane<T, true>(whole, ch, lane, P.V, x, &vm);
+            float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < EPL; ++e)
-              if ((!TAIL || ((vm >> e) & 1u)) && WaveTop<T>::number(x[e], ch * CHUNK + elem_offset(lane, e)) < least) take(x[e]);
-          });
-        };
-        others([&](float x) { m = fmaxf(m, x); });
-        m = B.max(m);
-        double s[1] = {0.0};
-        others([&](float x) { s[0] += static_cast<double>(fexp2((x - m) * P.c)); });
+              if (((vm >> e) & 1u) && WaveTop<T>::number(x[e], ch * CHUNK + elem_offset(lane, e)) < least) {
+                if (pass == 0) m = fmaxf(m, x[e]);
+                sum += fexp2((x[e] - m) * P.c);
+              }
+            s[0] += static_cast<double>(sum);
+          }
+          if (pass == 0) {
+            m = B.max(m);
+            s[0] = 0.0;
+          }
+        }
         B.sum(s);
-        other = static_cast<double>(m) + log2(s[0]) / P.c;
+        other = static_cast<double>(m) + top_log2(s[0]) / P.c;
       }
       if (B.tid == 0) {
         if (P.rest_logit) P.rest_logit[r] = wrong ? nanf_() : n < P.V ? static_cast<float>(other) : -finf();
