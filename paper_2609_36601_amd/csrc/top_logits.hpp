@@ -233,11 +233,17 @@ struct WaveTop {
     int more = 0;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) more += __popcll(__ballot(mine && x[e] >= L));
-    if (n + more <= TOP_CAP) {
+    // all lanes, or where the list might overflow, so few at a time that a list that was shortened holds theirs
+    constexpr int FEW = (TOP_CAP - SAKI_MAX_TOP_K) / EPL;
+    const int step = n + more <= TOP_CAP ? WAVE : FEW;
+#pragma unroll 1
+    for (int l0 = 0; l0 < WAVE; l0 += step) {
+      if (step < WAVE && n + FEW * EPL > TOP_CAP) shorten();
+      const bool now = mine && lane >= l0 && lane < l0 + step;
       float s = 0.0f;
 #pragma unroll
       for (int e = 0; e < EPL; ++e) {
-        const bool there = mine && x[e] != -finf();
+        const bool there = now && x[e] != -finf();
         bool in = there && x[e] >= L;
         if (__ballot(in) != 0ull) {
           const uint64_t u = number(x[e], base + elem_offset(0, e));
@@ -249,14 +255,6 @@ struct WaveTop {
         s += there && !in ? term(x[e]) : 0.0f;
       }
       rest += static_cast<double>(s);
-    } else {
-#pragma unroll 1
-      for (int e = 0; e < EPL; ++e) {
-        float xe = x[0];
-#pragma unroll
-        for (int i = 1; i < EPL; ++i) xe = i == e ? x[i] : xe;
-        push(mine && xe != -finf(), xe, base + elem_offset(0, e));
-      }
     }
   }
 };
@@ -345,73 +343,84 @@ __global__ __launch_bounds__(TOP_NT, 4) void top_kernel(TopParams P) {
     for (int attempt = 0;; ++attempt) {
       if constexpr (MODE != TOP_MERGE) {
         int queued = 0, ch = wave;
-        // two chunks under way (on every path a load, of the last chunk again: see for_chunks)
-        Frag<T> next, later;
+        // looks into 64 groups of the queue (the last ones)
+        auto take = [&]() __attribute__((always_inline)) {
+          __builtin_amdgcn_wave_barrier();
+          const int from = max(queued - WAVE, 0), at = min(from + lane, queued - 1);
+          const bool mine = from + lane < queued;
+          Frag<T> f;
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) f.q[i] = sh.group[wave][i][at];
+          const int place = sh.place[wave][at];
+          float x[EPL];
+          frag_unpack(f, x);
+          __builtin_amdgcn_wave_barrier();
+          W.push_group(mine, x, first + place);
+          queued = from;
+        };
+        // a chunk of which lanes in `some` have entries
+        auto chunk = [&](const Frag<T>& f, const float (&x)[EPL], bool some, int c) __attribute__((always_inline)) {
+          float lm = max3_raw(x[0], x[1], x[2]), s = 0.0f;
+          lm = max3_raw(lm, x[3], x[3]);
+#pragma unroll
+          for (int e = 4; e < EPL; e += 2) lm = max3_raw(lm, x[e], x[e + 1]);
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) s += W.term(x[e]);
+          hi = fmaxf(hi, lm);
+          const bool in = lm > W.L;
+          W.rest += static_cast<double>(in || !some ? 0.0f : s);
+          const uint64_t who = __ballot(in);
+          if (who != 0ull) {
+            if (in) {
+              const int at = queued + lanes_below(who);
+#pragma unroll
+              for (int i = 0; i < PIECES; ++i) sh.group[wave][i][at] = f.q[i];
+              sh.place[wave][at] = c * CHUNK + 8 * lane;
+            }
+            queued += __popcll(who);
+          }
+        };
+        auto whole = [&](const Frag<T>& f, int c) __attribute__((always_inline)) {
+          float x[EPL];
+          frag_unpack(f, x);
+#pragma unroll
+          for (int e = 0; e < EPL; e += 2) lo = min3_raw(lo, x[e], x[e + 1]);
+          chunk(f, x, true, c);
+        };
+        // two buffers in turn, loads on every path (see for_chunks)
         if (ch < full) {
-          frag_load<false>(next, row, ch, lane);
-          frag_load<false>(later, row, ch + TOP_NW < full ? ch + TOP_NW : ch, lane);
-        }
-        for (;;) {
-          if (ch < chunks) {
-            Frag<T> now = next;
-            float x[EPL];
-            uint32_t vm = 0xffffu;
-            if (ch < full) {
-              next = later;
-              frag_load<false>(later, row, ch + 2 * TOP_NW < full ? ch + 2 * TOP_NW : ch, lane);
-              frag_unpack(now, x);
-              lo = min3_raw(lo, x[0], x[1]);
-#pragma unroll
-              for (int e = 2; e < EPL; e += 2) lo = min3_raw(lo, x[e], x[e + 1]);
-            } else {  // the last entries; -infinity where there are none
-              load_lane<T, true>(row, ch, lane, len, x, &vm);
-#pragma unroll
-              for (int e = 0; e < EPL; ++e) {
-                const bool there = (vm >> e) & 1u;
-                lo = there ? fminf(lo, x[e]) : lo;
-                x[e] = there ? x[e] : -finf();
-              }
-              frag_pack(now, x);
-            }
-            float lm = max3_raw(x[0], x[1], x[2]), s = 0.0f;
-#pragma unroll
-            for (int e = 2; e < EPL; e += 2) lm = max3_raw(lm, x[e], x[e + 1]);
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) s += W.term(x[e]);
-            hi = fmaxf(hi, lm);
-            const bool in = lm > W.L;
-            W.rest += static_cast<double>(in || vm == 0u ? 0.0f : s);
-            const uint64_t who = __ballot(in);
-            if (who != 0ull) {
-              if (in) {
-                const int at = queued + lanes_below(who);
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) sh.group[wave][i][at] = now.q[i];
-                sh.place[wave][at] = ch * CHUNK + 8 * lane;
-              }
-              queued += __popcll(who);
-            }
+          Frag<T> a, b;
+          frag_load<false>(a, row, ch, lane);
+          frag_load<false>(b, row, ch + TOP_NW < full ? ch + TOP_NW : ch, lane);
+          for (;;) {
+            whole(a, ch);
+            frag_load<false>(a, row, ch + 2 * TOP_NW < full ? ch + 2 * TOP_NW : ch, lane);
+            if (queued >= TopShared<T>::TAKE) take();
             ch += TOP_NW;
-          }
-          if (queued >= TopShared<T>::TAKE || (ch >= chunks && queued > 0)) {  // looks into 64 groups (the last ones)
-            __builtin_amdgcn_wave_barrier();
-            const int from = max(queued - WAVE, 0), at = min(from + lane, queued - 1);
-            const bool mine = from + lane < queued;
-            Frag<T> f;
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) f.q[i] = sh.group[wave][i][at];
-            const int place = sh.place[wave][at];
-            float x[EPL];
-            frag_unpack(f, x);
-            __builtin_amdgcn_wave_barrier();
-            W.push_group(mine, x, first + place);
-            queued = from;
-          } else if (ch >= chunks) {
-            break;
+            if (ch >= full) break;
+            whole(b, ch);
+            frag_load<false>(b, row, ch + 2 * TOP_NW < full ? ch + 2 * TOP_NW : ch, lane);
+            if (queued >= TopShared<T>::TAKE) take();
+            ch += TOP_NW;
+            if (ch >= full) break;
           }
         }
+        if (ch == full && ch < chunks) {  // the last entries; -infinity where there are none
+          float x[EPL];
+          uint32_t vm;
+          load_lane<T, true>(row, ch, lane, len, x, &vm);
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) {
+            const bool there = (vm >> e) & 1u;
+            lo = there ? fminf(lo, x[e]) : lo;
+            x[e] = there ? x[e] : -finf();
+          }
+          Frag<T> f;
+          frag_pack(f, x);
+          chunk(f, x, vm != 0u, ch);
+        }
+        while (queued > 0) take();
       }
-      __syncthreads();  // (the queues' place is the block's list's)
       if (lane == 0) sh.count[wave] = W.n;
       if (B.tid == 0) sh.n_best = 0;
       __syncthreads();
