@@ -164,6 +164,24 @@ struct Block {
     return m;
   }
 
+  // The maxima of N (up to 4) numbers at once.
+  template <int N>
+  __device__ __forceinline__ void max(float (&v)[N]) {
+    static_assert(N <= 4, "block maximum wider than the LDS buffer");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = wave_max(v[i]);
+      if (lane == 0) sh.red_f[wave][i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = -finf();
+      for (int w = 0; w < NW; ++w) v[i] = fmaxf(v[i], sh.red_f[w][i]);
+    }
+    __syncthreads();
+  }
+
   template <typename K>
   __device__ __forceinline__ void argmin(K& key, int& idx) {
     wave_argmin(key, idx);
@@ -312,8 +330,9 @@ __device__ __forceinline__ void for_chunks(const T* srow, const T* trow, int V, 
 // The chunk loop over one array: body(tail, x, vm, c) gets this lane's 16
 // entries of chunk c; full chunks with the next chunk's loads in flight.  The
 // row cache works as in for_chunks, with two slots (the two halves of the
-// array) per cached chunk: the wave's last kc full chunks.
-template <typename T, int NW, int CM = CACHE_NONE, typename Body>
+// array) per cached chunk: the wave's last kc full chunks.  BACK: the wave's chunks from its last to its first (a second
+// sweep then starts with what the first has read last, which the last-level cache still holds), the ragged one at the end.
+template <typename T, int NW, int CM = CACHE_NONE, bool BACK = false, typename Body>
 __device__ __forceinline__ void for_chunks1(const T* row, int V, int wave, int lane, Body&& body,
                                             RowCache rc = RowCache{nullptr, 0}) {
   static_assert(CM == CACHE_NONE || sizeof(T) == 2, "the row cache holds bf16 chunks");
@@ -335,8 +354,9 @@ __device__ __forceinline__ void for_chunks1(const T* row, int V, int wave, int l
     frag_unpack(f, x);
     body(std::integral_constant<bool, false>(), x, 0xffffu, c);
   };
+  static_assert(!BACK || CM == CACHE_NONE, "backwards without a row cache");
   Frag<T> fa, fb;
-  if (nmem > 0) frag_load<false>(fa, row, wave, lane);
+  if (nmem > 0) frag_load<false>(fa, row, BACK ? wave + (nmem - 1) * NW : wave, lane);
   if constexpr (CM == CACHE_USE) {
     for (int i = first_cached; i < nw; ++i) {
       Frag<T> cf;
@@ -348,19 +368,20 @@ __device__ __forceinline__ void for_chunks1(const T* row, int V, int wave, int l
     }
   }
   if (nmem > 0) {
-    const int clast = wave + (nmem - 1) * NW;  // the wave's last chunk read from memory
-    int c = wave;
+    constexpr int STEP = BACK ? -NW : NW;
+    const int clast = BACK ? wave : wave + (nmem - 1) * NW;  // the wave's last chunk read from memory
+    int c = BACK ? wave + (nmem - 1) * NW : wave;
     for (;;) {
-      const bool more_b = c < clast;
-      frag_load<false>(fb, row, more_b ? c + NW : c, lane);
+      const bool more_b = c != clast;
+      frag_load<false>(fb, row, more_b ? c + STEP : c, lane);
       run(fa, c);
       if (!more_b) break;
-      c += NW;
-      const bool more_a = c < clast;
-      frag_load<false>(fa, row, more_a ? c + NW : c, lane);
+      c += STEP;
+      const bool more_a = c != clast;
+      frag_load<false>(fa, row, more_a ? c + STEP : c, lane);
       run(fb, c);
       if (!more_a) break;
-      c += NW;
+      c += STEP;
     }
   }
   if ((V % CHUNK) != 0 && (nfull % NW) == wave) {
