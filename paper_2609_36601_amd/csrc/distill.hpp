@@ -5,7 +5,7 @@
 // entry of U is one number times e^{z_j - m_U}:
 //   forward  (p_R - t_R) / S_U,   reverse  p_R (log(p_R / t_R) - l) / S_U     (times grad_scale / tau).
 // So the row needs two sweeps: S_U, then the gradient; the listed tokens, left out of S_U by a bit
-// mask in LDS, are a thread each and are written over the second sweep's values.  S_U has its own
+// mask in LDS, are a thread each and are written over the second sweep's values, by the lanes that stored those.  S_U has its own
 // reference, hence neither p_R nor a gradient entry is a difference of the row's whole
 // sum and the listed part of it, and a bucket of 1e-30 of the row has full precision.
 #pragma once
@@ -44,99 +44,89 @@ template <int NT>
 struct DistillShared {
   static constexpr int NW = NT / WAVE;
   uint32_t mask[DT_SEG / 32];
+  int2 patch[SAKI_MAX_TOP_K];  // listed tokens and their gradients
   double red_d[NW][RED_MAX];
   float red_f[NW][4];
   int red_i[NW][4];
   unsigned int next;
 };
 
-// What a row comes to: its loss, and what its gradient is made of.
+// What a row comes to: what its gradient is made of.
 struct DistillRow {
-  float coef;     // the gradient at tokens that are not listed is coef 2^((x - mU) c)
-  float mU;       // the largest of their logits
-  float listed;   // the gradient at this thread's token
-  bool take;      // the row has a loss (else its gradient is coef: 0, or NaN)
+  float coef;  // the gradient at tokens that are not listed is coef 2^((x - mU) c)
+  float mU;    // the largest of their logits
+  bool take;   // the row has a loss (else its gradient is coef: 0, or NaN)
 };
 
-// From the block's sums: this thread's entry of the list (held: token, its logit with the student s_tok and the
-// teacher), this wave's largest unlisted logit m, this thread's part S of sum 2^((x - m) c) and smallest logit lo;
-// wrong: the entry, or rest, cannot be used.  Writes the row's outputs but the gradient.  Logarithms in natural units, in 64 bits:
-// a divergence near 0 is a difference of large ones.
-// Only the waves that hold entries compute with them, and one posts what comes out.
+// From the block's sums: `slot`, this thread's place in the list (held: it has an entry, `token`, whose logits are s_tok with
+// the student and `logit` with the teacher), this wave's largest unlisted logit m, this thread's part S of
+// sum 2^((x - m) c) and smallest logit lo; wrong: the entry, or rest, cannot be used.  The bucket of the other tokens is
+// the entry behind the list's last.  Writes the row's outputs but the gradient; that of the listed tokens goes to sh.patch.
+// Logarithms in natural units, in 64 bits: a divergence near 0 is a difference of large ones.  Only the waves that hold
+// entries compute with them.
 template <typename BLOCK>
-__device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParams& P, int64_t r, bool part, bool held, bool wrong,
-                                                    float s_tok, float logit, float rest, float m, double S, float lo) {
+__device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParams& P, int64_t r, int slot, bool part, bool held,
+                                                    bool wrong, int token, float s_tok, float logit, float rest, float m, double S,
+                                                    float lo) {
   const double c64 = static_cast<double>(P.c) * LN2_D;
-  const bool lists = uniform(B.wave * WAVE < P.k);  // this wave holds entries (the first one always)
+  const bool lists = uniform(slot / WAVE * WAVE <= P.k), bucket = slot == P.k;
   float mm[3] = {m, held ? s_tok : -finf(), held && !wrong ? logit : -finf()};
   B.max(mm);
   const float mU = mm[0], mP = fmaxf(mm[1], mU), mT = fmaxf(mm[2], rest);
-  double v[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, z = 0.0, y = 0.0, zU = 0.0, yR = 0.0, eU = 0.0, eR = 0.0;
+  const float teach = bucket ? rest : logit;
+  const bool has_t = (held || bucket) && teach > -finf() && mT > -finf();
+  double v[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, z = 0.0, y = 0.0, own_p = 0.0, own_t = 0.0;
   v[0] = S > 0.0 ? S * static_cast<double>(fexp2((m - mU) * P.c)) : S;
-  v[4] = lo > -finf() && mU < finf() ? 0.0 : 1.0;
+  v[3] = wrong ? 1.0 : 0.0;
+  v[4] = (lo > -finf() && mU < finf() ? 0.0 : 1024.0) + (held ? 1.0 : 0.0);  // (fewer than 1,024 threads)
   if (lists) {
-    z = (static_cast<double>(s_tok) - mP) * c64;
-    y = (static_cast<double>(logit) - mT) * c64;
-    zU = (static_cast<double>(mU) - mP) * c64;
-    yR = (static_cast<double>(rest) - mT) * c64;
-    v[1] = held ? exp(z) : 0.0;
-    v[2] = held && mT > -finf() ? exp(y) : 0.0;
-    v[3] = wrong ? 1.0 : 0.0;
-    v[5] = held ? 1.0 : 0.0;
-    eU = exp(zU);
-    eR = rest > -finf() ? exp(yR) : 0.0;
+    z = (static_cast<double>(bucket ? mU : s_tok) - mP) * c64;
+    y = (static_cast<double>(teach) - mT) * c64;
+    own_p = held || bucket ? exp(z) : 0.0;
+    own_t = has_t ? exp(y) : 0.0;
+    v[1] = bucket ? 0.0 : own_p;
+    v[2] = own_t;
+    v[5] = bucket ? own_p : 0.0;
   }
-  const double own_p = v[1], own_t = v[2];
   B.sum(v);
   const double SU = v[0];
-  const bool some = mT > -finf(), others = v[5] < static_cast<double>(P.V);
-  double lt = 0.0, lp = 0.0, ltR = 0.0, lpR = 0.0, log_p = 0.0, p = 0.0, t = 0.0, pR = 0.0, tR = 0.0;
+  const int n_held = static_cast<int>(v[4]) & 1023;
+  const bool some = mT > -finf(), others = n_held < P.V;
+  double lt = 0.0, lp = 0.0, log_p = 0.0, p = 0.0, t = 0.0;
   // infinite divergences: forward, a share of the teacher's where the student has no token; reverse, the
   // other way round
   double l[2] = {0.0, 0.0};
   if (lists) {
-    const double eP = others ? SU * eU : 0.0, all_p = v[1] + eP, all_t = v[2] + eR;
+    if (bucket) own_p = others ? own_p * SU : 0.0;
+    const double all_p = v[1] + (others ? v[5] * SU : 0.0), all_t = v[2];
     const double log_t = log(all_t);
     log_p = log(all_p);
     lt = y - log_t;
-    lp = z - log_p;
-    ltR = yR - log_t;
-    lpR = zU + log(SU) - log_p;
+    lp = z - log_p + (bucket ? log(SU) : 0.0);
     p = own_p / all_p;
     t = own_t / all_t;
-    pR = eP / all_p;
-    tR = eR / all_t;
-    if (held && some) {
+    if (some && (held || (bucket && others))) {
       if (P.reverse) {
         l[0] = p > 0.0 ? p * (lp - lt) : 0.0;
-        l[1] = logit > -finf() ? 0.0 : 1.0;
+        l[1] = teach > -finf() ? 0.0 : 1.0;
       } else {
         l[0] = t > 0.0 ? t * (lt - lp) : 0.0;
       }
     }
+    if (some && bucket && !others && !P.reverse) l[1] = rest > -finf() ? 1.0 : 0.0;
   }
   B.sum(l);
-  DistillRow R;
-  R.mU = mU;
-  R.listed = 0.0f;
   if (lists) {
     double loss = l[0];
-    bool bad = v[3] != 0.0 || l[1] != 0.0;
-    if (P.reverse) {
-      if (others) loss += pR > 0.0 ? pR * (lpR - ltR) : 0.0;
-      bad |= some && others && !(rest > -finf());
-    } else {
-      if (tR > 0.0 && others) loss += tR * (ltR - lpR);
-      bad |= rest > -finf() && !others;
-    }
-    const bool finite = v[4] == 0.0 && SU == SU && isfinite(log_p);
+    const bool bad = v[3] != 0.0 || l[1] != 0.0;
+    const bool finite = v[4] < 1024.0 && SU == SU && isfinite(log_p);
     const bool take = part && some && !bad && finite, nan = part && (bad || !finite);
     if (!take) loss = nan ? __builtin_nan("") : 0.0;
     const double scale = static_cast<double>(P.grad_scale) * P.inv_tau;
-    R.listed = static_cast<float>((P.reverse ? p * (lp - lt - loss) : p - t) * scale);
-    if (B.tid == 0) {
-      const double gR = others ? (P.reverse ? pR * (lpR - ltR - loss) : pR - tR) * scale / SU : 0.0;
-      B.sh.red_f[0][0] = take ? static_cast<float>(gR) : nan ? nanf_() : 0.0f;
+    const double g = (P.reverse ? p * (lp - lt - loss) : p - t) * scale;
+    if (slot < P.k) B.sh.patch[slot] = make_int2(take && held ? token : -1, __float_as_int(static_cast<float>(g)));
+    if (bucket) {
+      B.sh.red_f[0][0] = take ? (others ? static_cast<float>(g / SU) : 0.0f) : nan ? nanf_() : 0.0f;
       B.sh.red_i[0][0] = take ? 1 : 0;
       if (P.row_loss) P.row_loss[r] = static_cast<float>(loss);
       if (P.scaled_loss) P.scaled_loss[r] = static_cast<double>(P.grad_scale) * loss;
@@ -145,6 +135,8 @@ __device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParam
     }
   }
   __syncthreads();
+  DistillRow R;
+  R.mU = mU;
   R.coef = B.sh.red_f[0][0];
   R.take = uniform(B.sh.red_i[0][0] != 0);
   return R;
@@ -168,7 +160,6 @@ __device__ __forceinline__ void distill_store8(G* p, const float* x) {
 
 template <typename T, typename G, bool GRAD, int NT>
 __global__ __launch_bounds__(NT, 4) void distill_kernel(DistillParams P) {
-  static_assert(SAKI_MAX_TOP_K <= NT, "a thread for each listed token");
   constexpr int NW = NT / WAVE;
   __shared__ DistillShared<NT> sh;
   Block<NT, DistillShared<NT>> B(sh);
@@ -176,6 +167,9 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(DistillParams P) {
   const int wave = __builtin_amdgcn_readfirstlane(B.wave);
   const float c = P.c;
   const unsigned int n = static_cast<unsigned int>(P.n_rows);
+  // this thread's place in the list; the waves that hold it are others in each of a CU's workgroups, whose first
+  // waves share a SIMD
+  const int slot = (B.tid + static_cast<int>(blockIdx.x >> 8) * WAVE) % NT;
   // What is read of a row's list while the row before it is written; what it holds is looked at when its turn comes.
   unsigned int r = blockIdx.x;  // (the counter's rows come behind the workgroups' first)
   int token_in = -1;
@@ -183,9 +177,9 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(DistillParams P) {
   uint8_t valid_in = 1;
   auto entry = [&](unsigned int row) __attribute__((always_inline)) {
     if (row >= n) return;
-    if (B.tid < k) {
-      token_in = P.token[static_cast<int64_t>(row) * P.list_stride + B.tid];
-      logit_in = P.logit[static_cast<int64_t>(row) * P.list_stride + B.tid];
+    if (slot < k) {
+      token_in = P.token[static_cast<int64_t>(row) * P.list_stride + slot];
+      logit_in = P.logit[static_cast<int64_t>(row) * P.list_stride + slot];
     }
     if (P.rest) rest_in = P.rest[row];
     if (P.valid) valid_in = P.valid[row];
@@ -261,7 +255,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(DistillParams P) {
       }
     }
     if (B.tid == 0) sh.next = next;
-    const DistillRow R = distill_solve(B, P, r, part, held, wrong, s_tok, logit, rest, m, S, lo);
+    const DistillRow R = distill_solve(B, P, r, slot, part, held, wrong, token, s_tok, logit, rest, m, S, lo);
     const unsigned int after = static_cast<unsigned int>(__builtin_amdgcn_readfirstlane(static_cast<int>(sh.next)));
     entry(after);
     if (GRAD) {
@@ -285,10 +279,18 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(DistillParams P) {
           }
         });
       }
-      // the listed tokens over it, once the row's stores are done
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (R.take && held) Storer<G>::store1(out + token, R.listed);
+      // the listed tokens of this wave's chunks, each by the lane that stored the chunk's entry there
+      for (int i0 = 0; R.take && i0 < k; i0 += WAVE) {
+        const int2 p = i0 + lane < k ? sh.patch[i0 + lane] : make_int2(-1, 0);
+        uint64_t mine = __ballot(p.x >= 0 && (p.x / CHUNK) % NW == wave);
+        while (mine != 0ull) {
+          const int e = __builtin_ctzll(mine);
+          mine &= mine - 1;
+          const int v = __builtin_amdgcn_readlane(p.x, e);
+          const float g = __int_as_float(__builtin_amdgcn_readlane(p.y, e));
+          if (lane == (v >> 3) % WAVE) Storer<G>::store1(out + v, g);
+        }
+      }
     }
     r = after;
   }
