@@ -189,7 +189,7 @@ saki_status saki_distill_top(const void* student, int32_t dtype, int64_t n_rows,
   const bool bf16 = dtype == SAKI_BF16;
   const int64_t row_bytes = vocab * ((bf16 ? 2 : 4) + (!grad ? 0 : grad_dtype == SAKI_BF16 ? 2 : 4));
   const int threads = row_bytes <= DISTILL_LONG && list->k < 256 ? 256 : 512;  // (a thread for each token, and one for the others)
-  const int64_t slots = static_cast<int64_t>(cus) * (1024 / threads);
+  const int64_t slots = static_cast<int64_t>(cus) * (threads == 512 ? 2 : row_bytes <= DISTILL_LONG / 4 ? 5 : 4);
   const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots)));
   if (n_rows > slots) {
     P.next_row = static_cast<unsigned int*>(ws);

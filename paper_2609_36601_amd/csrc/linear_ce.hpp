@@ -304,27 +304,50 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 #pragma unroll
     for (int j = 0; j < TQ; ++j) acc[i][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  if (steps > 0) {
+  // The fragments of half a tile (32 k) are read while those of the half before are multiplied; the barrier that
+  // changes tiles stands between a tile's last read and its last products, which then need nothing from LDS.
+  struct Half {
+    ce_bf16x8 p[TP], q[TQ];
+  };
+  auto read = [&](Half& h, int at, int kk) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) transfer();
+    for (int j = 0; j < TQ; ++j) h.q[j] = qf.read(at, j, kk);
+#pragma unroll
+    for (int i = 0; i < TP; ++i) h.p[i] = pf.read(at, i, kk);
+  };
+  auto multiply = [&](const Half& h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+      for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.p[i], h.q[j], acc[i][j], 0, 0, 0);
+  };
+  // (reads and products in turn)
+  auto mix = [&]() __attribute__((always_inline)) {
+    constexpr int READS = (PKC ? TP : 2 * TP) + (QKC ? TQ : 2 * TQ), EACH = TP * TQ / READS > 0 ? TP * TQ / READS : 1;
+#pragma unroll
+    for (int i = 0; i < READS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (steps > 0) {
+    Half a, b;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) transfer();
+    ce_wait<(NS - 1) * LOADS>();
+    read(a, 0, 0);
     int now = 0;
     for (int t = 0; t < steps; ++t) {
-      ce_wait<(NS - 2) * LOADS>();  // this tile is there, and nobody reads the one before it any more
+      read(b, now * STAGE, 1);
+      multiply(a);
+      mix();
+      ce_wait<(NS - 2) * LOADS>();  // the next tile is there, and nobody reads this one any more
       transfer();
-      const int at = now * STAGE;
       now = now + 1 == NS ? 0 : now + 1;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        ce_bf16x8 q[TQ];
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) q[j] = qf.read(at, j, kk);
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
-          const ce_bf16x8 p = pf.read(at, i, kk);
-#pragma unroll
-          for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q[j], acc[i][j], 0, 0, 0);
-        }
-      }
+      read(a, now * STAGE, 0);  // (behind the last tile: the last again, unused)
+      multiply(b);
+      mix();
     }
     ce_wait<0>();  // no transfer is under way when the workgroup ends
   }
