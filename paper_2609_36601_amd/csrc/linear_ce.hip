@@ -104,6 +104,7 @@ constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
 // last-level cache holds, at most.
 constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
 constexpr int64_t CUS = 256;
+constexpr int64_t MOST_SPLITS = 64;
 
 saki_status check_head(const saki_head* h) {
   if (!h) return abi_fail(SAKI_E_NULLPTR, "head is NULL");
@@ -159,12 +160,27 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   const int64_t tile_p = p.tile_s == 0 ? CeLarge::PT : p.tile_s == 1 ? CeMiddle::PT : CeFew::PT;
   p.wave_p = tile_p / (p.tile_s == 0 ? CeLarge::WP : p.tile_s == 1 ? CeMiddle::WP : CeFew::WP);
   p.slots = ceil_div(p.V, tile_p) * (tile_p / p.wave_p);
-  p.tile_x = tile_of(p.D, p.n, true);
-  if (p.tile_x == 0 || p.tile_x == 1) p.tile_x = ceil_div(p.n, 256) * ceil_div(p.D, 256) * 2 >= CUS ? 0 : 1;
-  const int64_t t = p.tile_x == 0 ? 256 : p.tile_x == 1 ? 128 : 64, per_cu = p.tile_x == 0 ? 1 : 2;
-  const int64_t tiles = ceil_div(p.n, t) * ceil_div(p.D, t), kt = p.piece / CE_BK;
-  // dX: k, the piece's tokens, in so many splits that the tiles fill the card
-  p.splits = std::max<int64_t>(1, std::min(per_cu * CUS / std::max<int64_t>(tiles, 1), kt / 4));
+  // dX: k, the piece's tokens, may be split between workgroups, whose sums are added up afterwards.  The tiles and the
+  // splits that cost least, in microseconds: a CU takes STEP for a tile of k (of two workgroups, where two fit), rounds
+  // that leave CUs idle cost like others, starting and ending a tile takes 3, and a split's sums are written and read.
+  const int64_t kt = p.piece / CE_BK;
+  double least = 0.0;
+  p.splits = 0;
+  for (int tile = p.n <= CeFew::QT ? 2 : 0; tile < 3; ++tile) {
+    const int64_t t = tile == 0 ? CeLarge::QT : tile == 1 ? CeMiddle::QT : CeFew::QT, per_cu = tile == 0 ? 1 : 2;
+    const double step = tile == 0 ? 1.7 : tile == 1 ? 1.1 : 0.6;
+    const int64_t tiles = ceil_div(p.n, t) * ceil_div(p.D, t);
+    for (int64_t s = 1; s <= std::min<int64_t>(MOST_SPLITS, std::max<int64_t>(kt / 4, 1)); ++s) {
+      const double rounds = static_cast<double>(ceil_div(tiles * s, per_cu * CUS));
+      const double cost = rounds * (3.0 + static_cast<double>(ceil_div(kt, s)) * p.planes * (three ? 2 : 1) * step) +
+                          static_cast<double>(s) * p.n * p.D * 8 / 4.5e6;
+      if (p.splits == 0 || cost < least) {
+        least = cost;
+        p.tile_x = tile;
+        p.splits = s;
+      }
+    }
+  }
   p.k_split = ceil_div(kt, p.splits);
   p.splits = ceil_div(kt, p.k_split);
   size_t at = 0;
@@ -249,8 +265,11 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   uint16_t* const w_parts = reinterpret_cast<uint16_t*>(ws + p.w);
   const int64_t w_plane = p.piece * p.ld;
   // tokens v0 .. v0 + nv of the weight as the products take them
+  bool parts_there = false;
   auto weight = [&](int64_t v0, int64_t nv) {
     if constexpr (three) {
+      if (parts_there && p.pieces == 1) return hipSuccess;
+      parts_there = true;
       const int64_t blocks = std::min<int64_t>(ceil_div(nv * p.ld / 8, 256), 8192);
       hipLaunchKernelGGL((ce_pack_kernel<T>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs,
                          static_cast<const T*>(h->weight) + v0 * h->weight_stride, h->weight_stride, nv,
@@ -285,7 +304,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     st = abi_launched(launch_ce_part<CE_LSE>(G, p.tile_s, three, 1, hs), "ce_gemm_kernel");
     if (st != SAKI_OK) return st;
   }
-  hipLaunchKernelGGL((ce_loss_kernel<T>), dim3(static_cast<unsigned>(ceil_div(p.n, 4))), dim3(256), 0, hs, R);
+  hipLaunchKernelGGL((ce_loss_kernel<T>), dim3(static_cast<unsigned>(p.n)), dim3(256), 0, hs, R);
   SAKI_LAUNCHED("ce_loss_kernel");
   if (a->loss_sum) {
     st = abi_loss_sum(R.scaled_loss, p.n, a->loss_sum, hs);
@@ -341,7 +360,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     }
   }
   if (dx) {
-    const int64_t blocks = std::min<int64_t>(ceil_div(p.n * p.D / 8, 256), 8192);
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.n * p.D / 4, 256), 16384);
     using S = std::conditional_t<three, float, uint16_t>;
     hipLaunchKernelGGL((ce_grad_hidden_kernel<S>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs, R);
     SAKI_LAUNCHED("ce_grad_hidden_kernel");

@@ -500,22 +500,43 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* x, int64_t stride
   }
 }
 
-// A wave a row that takes part: its log-sum-exp from the tiles' maxima and sums, the target's logit as a product
-// of its own, and the row's outputs.
+// A workgroup a row that takes part: its log-sum-exp from the tiles' maxima and sums, the target's logit as a product
+// of its own, and the row's outputs.  What bounds it: latency; every thread has four of its row's loads under way.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
-  const int lane = threadIdx.x & (WAVE - 1);
-  const int64_t i = blockIdx.x * 4ll + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  if (i >= (P.count ? *P.count : P.n_rows)) return;
+  constexpr int DEEP = 4;
+  __shared__ float part_m[4], part_dot[4];
+  __shared__ double part_s[4];
+  const int tid = threadIdx.x, lane = tid & (WAVE - 1), wave = tid / WAVE;
+  const int64_t i = blockIdx.x;
+  if (P.count && i >= *P.count) return;
   const int64_t r = P.count ? P.source[i] : i;
   const int token = P.token[r];
   const float weight = P.row_weight ? P.row_weight[r] : 1.0f;
   const bool good = token >= 0 && token < P.vocab && isfinite(weight);
+  const float2* stats = P.stats + i * P.slots;
+  float m = -finf();
+  double sum = 0.0;
+  for (int s0 = tid; s0 < P.slots; s0 += 256 * DEEP) {
+    float2 f[DEEP];
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e) f[e] = stats[min(s0 + e * 256, P.slots - 1)];
+    float to = m;
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e) to = fmaxf(to, f[e].x);
+    // (-infinity and 0: no token, or logits of -infinity or NaN alone, whose sum is NaN)
+    sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - to));
+    m = to;
+    const float ref = m == -finf() ? 0.0f : m;
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e)
+      if (s0 + e * 256 < P.slots) sum += static_cast<double>(f[e].y) * static_cast<double>(fexp2(f[e].x - ref));
+  }
   float dot = 0.0f;
   if (good) {
     const T* x = static_cast<const T*>(P.hidden) + r * P.hidden_stride;
     const T* w = static_cast<const T*>(P.weight) + static_cast<int64_t>(token) * P.weight_stride;
-    for (int d = lane * 8; d < P.D; d += WAVE * 8) {
+    for (int d = tid * 8; d < P.D; d += 256 * 8) {
       float a[8], b[8];
       Loader<T>::load8(x + d, a);
       Loader<T>::load8(w + d, b);
@@ -524,21 +545,26 @@ __global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
     }
   }
   dot = wave_sum(dot);
-  const float2* stats = P.stats + i * P.slots;
-  float m = -finf();
-  for (int s = lane; s < P.slots; s += WAVE) m = fmaxf(m, stats[s].x);
-  m = wave_max(m);
-  double sum = 0.0;
-  for (int s = lane; s < P.slots; s += WAVE) {
-    const float2 f = stats[s];
-    sum += static_cast<double>(f.y) * static_cast<double>(fexp2(f.x - m));
-  }
+  const float wm = wave_max(m);
+  sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - wm));
 #pragma unroll
   for (int k = 1; k < WAVE; k *= 2) sum += __shfl_xor(sum, k);
+  if (lane == 0) {
+    part_m[wave] = wm;
+    part_s[wave] = sum;
+    part_dot[wave] = dot;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  m = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
+  sum = 0.0;
+  dot = (part_dot[0] + part_dot[1]) + (part_dot[2] + part_dot[3]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += part_m[w] == -finf() ? part_s[w] : part_s[w] * static_cast<double>(fexp2(part_m[w] - m));
+  // (a row of -infinity alone: m and so the result)
   const double lse2 = static_cast<double>(m) + log2(sum);
   const double logp = static_cast<double>(dot) - lse2 / static_cast<double>(LOG2E);
   const bool finite = isfinite(lse2) && (!good || isfinite(logp));
-  if (lane != 0) return;
   CeRow R;
   R.lse_hi = finite ? static_cast<float>(lse2) : nanf_();
   R.lse_lo = finite ? static_cast<float>(lse2 - static_cast<double>(R.lse_hi)) : nanf_();
@@ -554,29 +580,35 @@ __global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
   if (P.row_status) P.row_status[r] = !good ? SAKI_ROW_BAD_TARGET : finite ? SAKI_ROW_OK : SAKI_ROW_NONFINITE;
 }
 
-// grad_hidden from the splits' sums.
+// grad_hidden from the splits' sums.  Four of a thread's loads are under way.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_grad_hidden_kernel(CeRows P) {
-  const int pieces = P.D / 8;
+  const int pieces = P.D / 4;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < P.n_rows * pieces; i += gridDim.x * 256ll) {
     const int64_t r = i / pieces;
-    const int d = static_cast<int>(i - r * pieces) * 8;
+    const int d = static_cast<int>(i - r * pieces) * 4;
     const int64_t at = P.count ? P.place[r] : r;
-    float g[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) g[e] = 0.0f;
+    ce_f32x4 g = {0.0f, 0.0f, 0.0f, 0.0f};
     if (at >= 0) {
-      for (int s = 0; s < P.splits; ++s) {
-        float v[8];
-        Loader<float>::load8(P.sums + s * P.split_stride + at * P.ld_sums + d, v);
+      const float* from = P.sums + at * P.ld_sums + d;
+      int s = 0;
+      for (; s + 4 <= P.splits; s += 4) {
+        ce_f32x4 v[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] += v[e];
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const ce_f32x4*>(from + (s + e) * P.split_stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g += v[e];
       }
-      const float scale = P.rows[at].token < 0 ? nanf_() : P.grad_scale;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] *= scale;
+      for (; s < P.splits; ++s) g += *reinterpret_cast<const ce_f32x4*>(from + s * P.split_stride);
+      g *= P.rows[at].token < 0 ? nanf_() : P.grad_scale;
     }
-    Storer<T>::store8(static_cast<T*>(P.grad_hidden) + r * P.grad_stride + d, g);
+    T* const to = static_cast<T*>(P.grad_hidden) + r * P.grad_stride + d;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<ce_f32x4*>(to) = g;
+    } else {
+      *reinterpret_cast<uint2*>(to) = make_uint2(f32_to_bf16_bits(g[0]) | f32_to_bf16_bits(g[1]) << 16,
+                                                 f32_to_bf16_bits(g[2]) | f32_to_bf16_bits(g[3]) << 16);
+    }
   }
 }
 
