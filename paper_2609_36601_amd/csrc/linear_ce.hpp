@@ -77,37 +77,21 @@ struct CeGemm {
 __device__ __forceinline__ int ce_part_p(int seg) { return (0x102100 >> (4 * seg)) & 3; }  // 0 0 1 2 0 1
 __device__ __forceinline__ int ce_part_q(int seg) { return (0x120010 >> (4 * seg)) & 3; }  // 0 1 0 0 2 1
 
-// Four transfers of 16 bytes a lane from base + off[i] to LDS at `lds` + i STEP + 16 lane.  m0 holds the LDS
-// address; it is the compiler's, which takes no clobber of it, and is put back.  A transfer must come one wait state
-// after a write to m0, and base is written by a scalar instruction here (a vector instruction's would need five).
-// The compiler is not told of the transfers (every LDS read would wait for them): ce_wait does.
-template <int STEP>
-__device__ __forceinline__ void ce_to_lds4(uint32_t lds, uint64_t from, const uint32_t (&off)[4]) {
+// 16 bytes a lane from `from` + off to LDS at `lds` + 16 lane.  m0 holds the LDS address; it is the compiler's, which
+// takes no clobber of it, and is put back.  A transfer must come one wait state after a write to m0, and five after a
+// vector instruction that wrote its base: the scalar copy of the base is that wait state, and what the transfer reads is
+// then written by a scalar instruction.  The compiler is not told of the transfers (every LDS read would wait for them):
+// ce_wait does.
+__device__ __forceinline__ void ce_to_lds(uint32_t lds, uint64_t from, uint32_t off) {
   uint32_t m0;
   uint64_t base;
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %2\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
-      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
-      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %6, %1\n\t"
-      "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %7, %1\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(m0), "=&s"(base)
-      : "s"(lds), "s"(from), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "n"(STEP)
-      : "memory", "scc");
-}
-template <int STEP>
-__device__ __forceinline__ void ce_to_lds2(uint32_t lds, uint64_t from, const uint32_t (&off)[2]) {
-  uint32_t m0;
-  uint64_t base;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %2\n\ts_mov_b64 %1, %3\n\tglobal_load_lds_dwordx4 %4, %1\n\t"
-      "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %1\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(m0), "=&s"(base)
-      : "s"(lds), "s"(from), "v"(off[0]), "v"(off[1]), "n"(STEP)
-      : "memory", "scc");
+      : "s"(lds), "s"(from), "v"(off)
+      : "memory");
 }
 
 // All but the N youngest transfers of this wave are done, its LDS reads are, and all waves are here.
@@ -125,83 +109,78 @@ __device__ __forceinline__ uint64_t ce_scalar(const void* p) {
 
 // One operand's side of a workgroup: EXT entries of p (or q) and 64 of k a tile.  KC: k is
 // contiguous in memory, and a tile lies in LDS as [EXT][64], piece j of row r at j ^ (r & 7).  Otherwise
-// as [64][EXT], piece j of row r at j ^ 2 (r & 3): the four rows whose 32 bytes a transposing read takes
-// lie in different banks.
+// as [64][EXT], piece j of row r at j ^ 2 (r & 3) ^ (r & 8): the 32 bytes of four rows that 16 lanes of a transposing
+// read take, and those of the next 16 lanes, eight rows on, lie in different banks (where two rows fill the banks,
+// without the last).
 template <bool KC, int EXT, int WAVES>
 struct CeSide {
   static constexpr int BYTES = EXT * CE_BK * 2;
   static constexpr int LOADS = BYTES / 1024 / WAVES;  // transfers of a wave and tile
-  static_assert(LOADS * WAVES * 1024 == BYTES && (LOADS == 2 || LOADS == 4), "whole transfers");
+  static_assert(LOADS * WAVES * 1024 == BYTES, "whole transfers");
   static constexpr int PIECES = KC ? CE_BK / 8 : EXT / 8;  // of a row in LDS
   static constexpr int ROWS_PER = 64 / PIECES;
 
   uint64_t base;       // of the tile that is transferred next (the same in all lanes)
   int64_t ld;
-  uint32_t off[LOADS];
-  int left;            // entries from this tile's first on
+  uint32_t off[LOADS], off_last[LOADS];  // of this lane's parts; in the last tile of k
 
   // row in the tile and piece in memory of this lane's part of transfer i
   __device__ __forceinline__ static int row_of(int i, int wave, int lane) { return (i * WAVES + wave) * ROWS_PER + lane / PIECES; }
   __device__ __forceinline__ static int piece_of(int row, int lane) {
     const int at = lane % PIECES;
-    return KC ? at ^ (row & 7) : at ^ ((row & 3) << 1);
+    return KC ? at ^ (row & 7) : at ^ ((row & 3) << 1) ^ (EXT >= 128 ? row & 8 : 0);
   }
 
-  // first: the tile's first entry of p (q), of `extent`
-  __device__ __forceinline__ void init(const uint16_t* data, int64_t ld_, int first, int extent, int wave, int lane) {
+  // first: the tile's first entry of p (q), of `extent`; n_k: how many k there are, whole tiles or not
+  __device__ __forceinline__ void init(const uint16_t* data, int64_t ld_, int first, int extent, int n_k, int wave, int lane) {
     ld = ld_;
-    left = extent - first;
+    const int left = extent - first, k_left = n_k % CE_BK == 0 ? CE_BK : n_k % CE_BK;
     base = ce_scalar(data + (KC ? static_cast<int64_t>(first) * ld : static_cast<int64_t>(first)));
+    const uint32_t pitch = static_cast<uint32_t>(ld * 2);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = row_of(i, wave, lane), piece = piece_of(row, lane);
-      if (KC)  // (rows behind the last: the last)
-        off[i] = static_cast<uint32_t>(min(row, left - 1)) * static_cast<uint32_t>(ld * 2) + piece * 16;
-      else  // (entries behind the last: the tile's first)
-        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(ld * 2) + (piece * 8 < left ? piece * 16 : 0);
-    }
-  }
-  // Transfers the 64 k from k0 on, of which `k_left` exist; the base is theirs.
-  __device__ __forceinline__ void transfer(uint32_t lds, int k_left, int wave, int lane) const {
-    uint32_t o[LOADS];
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) o[i] = off[i];
-    if (k_left < CE_BK) {  // k behind the last: one that exists (Q, whose memory is whole tiles, holds zeros there)
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int row = row_of(i, wave, lane), piece = piece_of(row, lane);
-        if (KC) o[i] -= piece * 8 < k_left ? 0 : piece * 16;
-        else o[i] -= static_cast<uint32_t>(max(row - (k_left - 1), 0)) * static_cast<uint32_t>(ld * 2);
+      // behind the last row (entry): the last (the tile's first); k behind the last: one that exists
+      if (KC) {
+        off[i] = static_cast<uint32_t>(min(row, left - 1)) * pitch + piece * 16;
+        off_last[i] = off[i] - (piece * 8 < k_left ? 0 : piece * 16);
+      } else {
+        const uint32_t at = piece * 8 < left ? piece * 16 : 0;
+        off[i] = static_cast<uint32_t>(row) * pitch + at;
+        off_last[i] = static_cast<uint32_t>(min(row, k_left - 1)) * pitch + at;
       }
     }
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + wave * 1024);
-    if constexpr (LOADS == 4) ce_to_lds4<WAVES * 1024>(at, base, o);
-    else ce_to_lds2<WAVES * 1024>(at, base, o);
+  }
+  // This wave's i-th transfer of the tile of k at `base`.
+  __device__ __forceinline__ void transfer(int i, uint32_t lds, bool last, int wave) const {
+    ce_to_lds(__builtin_amdgcn_readfirstlane(lds + (i * WAVES + wave) * 1024), base, last ? off_last[i] : off[i]);
   }
   __device__ __forceinline__ uint64_t step() const { return static_cast<uint64_t>(KC ? CE_BK * 2 : ld * CE_BK * 2); }
 };
 
-// This lane's places in an operand's tile: the fragment of 16 entries from `from` + 16 f on, k 32 kk + 8 g .. + 7.
-template <bool KC, int EXT>
+// This lane's places in an operand's tile: the fragment of 16 entries from `from` + 16 f on (f < N), k 32 kk + 8 g .. + 7.
+template <bool KC, int EXT, int N>
 struct CeFrag {
-  const char* at[KC ? 2 : 4];
+  const char* at[KC ? 2 : N];
   __device__ __forceinline__ void init(const char* tiles, int from, int lane) {
     const int c = lane & 15, g = lane >> 4;
     if constexpr (KC) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) at[kk] = tiles + (from + c) * 128 + ((kk * 4 + g) ^ (c & 7)) * 16;
     } else {
-      const int s = c >> 2;
+      const int row = 8 * g + (c >> 2);
 #pragma unroll
-      for (int f = 0; f < 4; ++f)
-        at[f] = tiles + (8 * g + s) * (EXT * 2) + ((((from >> 4) + f) ^ s) * 2 + ((c >> 1) & 1)) * 16 + (c & 1) * 8;
+      for (int f = 0; f < N; ++f) {
+        const int piece = ((from >> 4) + f) * 2 + (c >> 1 & 1);
+        at[f] = tiles + row * (EXT * 2) + (piece ^ ((row & 3) << 1) ^ (EXT >= 128 ? row & 8 : 0)) * 16 + (c & 1) * 8;
+      }
     }
   }
   __device__ __forceinline__ ce_bf16x8 read(int tile, int f, int kk) const {
     if constexpr (KC) {
       return *reinterpret_cast<const ce_bf16x8*>(at[kk] + tile + f * 2048);
     } else {
-      const char* a = at[f & 3] + tile + (f >> 2) * 128 + kk * 32 * EXT * 2;
+      const char* a = at[f] + tile + kk * 32 * EXT * 2;
       const ce_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ce_lds_s16x4*)a);
       const ce_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ce_lds_s16x4*)(a + 4 * EXT * 2));
       ce_bf16x8 r;
@@ -269,33 +248,44 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 
   PSide ps;
   QSide qs;
-  ps.init(A.p, A.ldp, p0, A.n_p, wave, lane);
-  qs.init(A.q, A.ldq, q0, n_q, wave, lane);
+  ps.init(A.p, A.ldp, p0, A.n_p, n_k, wave, lane);
+  // (Q's memory is whole tiles of k, and holds zeros behind the last: what P has there does not matter)
+  qs.init(A.q, A.ldq, q0, n_q, 0, wave, lane);
   ps.base += ps.step() * k_first;
   qs.base += qs.step() * k_first;
   const uint64_t p_start = ps.base, q_start = qs.base;
   const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)tiles));
+  const int k_last = (n_k + CE_BK - 1) / CE_BK - 1 - k_first;
   int k_next = 0, seg = 0, stage = 0;
-  // transfers the next tile of k (behind the last one: the last again, which nobody reads)
-  auto transfer = [&]() __attribute__((always_inline)) {
-    const int k_left = n_k - (k_first + k_next) * CE_BK;
-    ps.transfer(lds + stage * STAGE, k_left, wave, lane);
-    qs.transfer(lds + stage * STAGE + PSide::BYTES, CE_BK, wave, lane);
+  // The i-th transfer of the next tile of k; the last one done, moves on (behind the last tile: the last again, which
+  // nobody reads).
+  auto transfer = [&](int i) __attribute__((always_inline)) {
+    if (i < PSide::LOADS) ps.transfer(i, lds + stage * STAGE, k_next == k_last, wave);
+    else qs.transfer(i - PSide::LOADS, lds + stage * STAGE + PSide::BYTES, false, wave);
+  };
+  auto transferred = [&]() __attribute__((always_inline)) {
     stage = stage + 1 == NS ? 0 : stage + 1;
-    if (k_next + 1 < kt) {
-      ++k_next;
-      ps.base += ps.step();
-      qs.base += qs.step();
-    } else if (THREE && seg < 5) {
-      ++seg;
-      k_next = 0;
-      ps.base = p_start + ce_part_p(seg) * A.p_plane * 2;
-      qs.base = q_start + ce_part_q(seg) * A.q_plane * 2;
+    const bool more = k_next + 1 < kt;
+    if constexpr (THREE) {
+      if (more) {
+        ++k_next;
+        ps.base += ps.step();
+        qs.base += qs.step();
+      } else if (seg < 5) {
+        ++seg;
+        k_next = 0;
+        ps.base = p_start + ce_part_p(seg) * A.p_plane * 2;
+        qs.base = q_start + ce_part_q(seg) * A.q_plane * 2;
+      }
+    } else {
+      k_next += more ? 1 : 0;
+      ps.base += more ? ps.step() : 0;
+      qs.base += more ? qs.step() : 0;
     }
   };
 
-  CeFrag<PKC, PT> pf;
-  CeFrag<QKC, QT> qf;
+  CeFrag<PKC, PT, TP> pf;
+  CeFrag<QKC, QT, TQ> qf;
   pf.init(tiles, wp * TP * 16, lane);
   qf.init(tiles + PSide::BYTES, wq * TQ * 16, lane);
   ce_f32x4 acc[TP][TQ];
@@ -304,50 +294,56 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 #pragma unroll
     for (int j = 0; j < TQ; ++j) acc[i][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // The fragments of half a tile (32 k) are read while those of the half before are multiplied; the barrier that
-  // changes tiles stands between a tile's last read and its last products, which then need nothing from LDS.
+  // A tile is two halves of 32 k.  The fragments of one are read while those of the other are multiplied, and the barrier that
+  // changes tiles stands between the last read of a tile and its last products, which need nothing from LDS.  What
+  // else a wave has to issue, reads and transfers, is spread between the products.
   struct Half {
     ce_bf16x8 p[TP], q[TQ];
   };
-  auto read = [&](Half& h, int at, int kk) __attribute__((always_inline)) {
+  // step i of TP: 4 (TQ) products of `have`, and its share of the reads of `next`
+  auto step = [&](int i, const Half& have, Half& next, int at, int kk) __attribute__((always_inline)) {
+    if (i == 0) {
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) h.q[j] = qf.read(at, j, kk);
-#pragma unroll
-    for (int i = 0; i < TP; ++i) h.p[i] = pf.read(at, i, kk);
-  };
-  auto multiply = [&](const Half& h) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < TP; ++i)
-#pragma unroll
-      for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h.p[i], h.q[j], acc[i][j], 0, 0, 0);
-  };
-  // (reads and products in turn)
-  auto mix = [&]() __attribute__((always_inline)) {
-    constexpr int READS = (PKC ? TP : 2 * TP) + (QKC ? TQ : 2 * TQ), EACH = TP * TQ / READS > 0 ? TP * TQ / READS : 1;
-#pragma unroll
-    for (int i = 0; i < READS; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+      for (int j = 0; j < TQ; j += 2) next.q[j] = qf.read(at, j, kk);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    if (i == (TP > 1 ? 1 : 0)) {
+#pragma unroll
+      for (int j = 1; j < TQ; j += 2) next.q[j] = qf.read(at, j, kk);
+    }
+    next.p[i] = pf.read(at, i, kk);
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(have.p[i], have.q[j], acc[i][j], 0, 0, 0);
   };
   if (steps > 0) {
     Half a, b;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) transfer();
+    for (int s = 0; s < NS; ++s) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) transfer(i);
+      transferred();
+    }
     ce_wait<(NS - 1) * LOADS>();
-    read(a, 0, 0);
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) a.q[j] = qf.read(0, j, 0);
+#pragma unroll
+    for (int i = 0; i < TP; ++i) a.p[i] = pf.read(0, i, 0);
     int now = 0;
     for (int t = 0; t < steps; ++t) {
-      read(b, now * STAGE, 1);
-      multiply(a);
-      mix();
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        step(i, a, b, now * STAGE, 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       ce_wait<(NS - 2) * LOADS>();  // the next tile is there, and nobody reads this one any more
-      transfer();
       now = now + 1 == NS ? 0 : now + 1;
-      read(a, now * STAGE, 0);  // (behind the last tile: the last again, unused)
-      multiply(b);
-      mix();
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        step(i, b, a, now * STAGE, 0);  // (behind the last tile: the last again, unused)
+#pragma unroll
+        for (int k = i * LOADS / TP; k < (i + 1) * LOADS / TP; ++k) transfer(k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      transferred();
     }
     ce_wait<0>();  // no transfer is under way when the workgroup ends
   }
