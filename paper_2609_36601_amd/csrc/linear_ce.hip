@@ -10,7 +10,7 @@ template <int KIND, typename TILE>
 static hipError_t launch_tile(CeGemm A, bool three, int splits, hipStream_t st) {
   A.p_tiles = (A.n_p + TILE::PT - 1) / TILE::PT;
   A.q_tiles = (A.n_q + TILE::QT - 1) / TILE::QT;
-  const dim3 grid(static_cast<unsigned>(A.p_tiles * A.q_tiles), static_cast<unsigned>(splits)), block(TILE::NT);
+  const dim3 grid(static_cast<unsigned>(A.p_tiles * A.q_tiles * splits)), block(TILE::NT);
   if (three) hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, true>), grid, block, 0, st, A);
   else hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, false>), grid, block, 0, st, A);
   return hipGetLastError();

@@ -224,13 +224,15 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wp = wave % TILE::WP, wq = wave / TILE::WP;
-  // Workgroups go round the eight dies: each die gets a run of tiles, in columns of eight q, so
-  // that those at work on it at a time (32) share 4 + 8 tiles of the operands in its L2.
-  int p_tile, q_tile;
+  // Workgroups go round the eight dies: each die gets a run of tiles, splits one after the other (whose slices of both
+  // operands its L2 then holds), in columns of eight q, so that those at work on it at a time (32) share 4 + 8 tiles.
+  int p_tile, q_tile, split;
   {
-    const int n = A.p_tiles * A.q_tiles, die = blockIdx.x & 7, i = blockIdx.x >> 3;
+    const int tiles = A.p_tiles * A.q_tiles, n = gridDim.x, die = blockIdx.x & 7, i = blockIdx.x >> 3;
     const int each = n >> 3, more = n & 7;
-    const int t = die * each + min(die, more) + i;
+    int t = die * each + min(die, more) + i;
+    split = t / tiles;
+    t -= split * tiles;
     const int column = 8 * A.p_tiles, c0 = t / column * 8, wide = min(8, A.q_tiles - c0), in = t - c0 * A.p_tiles;
     p_tile = in / wide;
     q_tile = c0 + in % wide;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
   if (q0 >= n_q) return;
   int kt = (n_k + CE_BK - 1) / CE_BK, k_first = 0;
   if (KIND == CE_DX) {
-    k_first = blockIdx.y * A.k_split;
+    k_first = split * A.k_split;
     kt = min(kt - k_first, A.k_split);
   }
   const int steps = THREE ? 6 * kt : kt;
@@ -404,7 +406,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
       }
     }
   } else if constexpr (KIND == CE_DX) {
-    float* const sums = A.sums + blockIdx.y * A.split_stride;
+    float* const sums = A.sums + split * A.split_stride;
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
       const int row = qw + 16 * j;
