@@ -77,6 +77,70 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRows P) {
   if (threadIdx.x == 0) *P.count = base;
 }
 
+// A workgroup a row that takes part: its log-sum-exp from the tiles' maxima and sums, and the row's outputs.  What bounds it: latency; every thread has four of its row's loads under way.
+__global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
+  constexpr int DEEP = 4;
+  __shared__ float part_m[4];
+  __shared__ double part_s[4];
+  const int tid = threadIdx.x, lane = tid & (WAVE - 1), wave = tid / WAVE;
+  const int64_t i = blockIdx.x;
+  if (P.count && i >= *P.count) return;
+  const int64_t r = P.count ? P.source[i] : i;
+  const int token = P.token[r];
+  const float weight = P.row_weight ? P.row_weight[r] : 1.0f;
+  const bool good = token >= 0 && token < P.vocab && isfinite(weight);
+  const float target = good ? P.target[i] : 0.0f;
+  const float2* stats = P.stats + i * P.slots;
+  float m = -finf();
+  double sum = 0.0;
+  for (int s0 = tid; s0 < P.slots; s0 += 256 * DEEP) {
+    float2 f[DEEP];
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e) f[e] = stats[min(s0 + e * 256, P.slots - 1)];
+    float to = m;
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e) to = fmaxf(to, f[e].x);
+    // (-infinity and 0: no token, or logits of -infinity or NaN alone, whose sum is NaN)
+    sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - to));
+    m = to;
+    const float ref = m == -finf() ? 0.0f : m;
+#pragma unroll
+    for (int e = 0; e < DEEP; ++e)
+      if (s0 + e * 256 < P.slots) sum += static_cast<double>(f[e].y) * static_cast<double>(fexp2(f[e].x - ref));
+  }
+  const float wm = wave_max(m);
+  sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - wm));
+#pragma unroll
+  for (int k = 1; k < WAVE; k *= 2) sum += __shfl_xor(sum, k);
+  if (lane == 0) {
+    part_m[wave] = wm;
+    part_s[wave] = sum;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  m = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += part_m[w] == -finf() ? part_s[w] : part_s[w] * static_cast<double>(fexp2(part_m[w] - m));
+  // (a row of -infinity alone: m and so the result)
+  const double lse2 = static_cast<double>(m) + log2(sum);
+  const double logp = (static_cast<double>(target) - lse2) / static_cast<double>(LOG2E);
+  const bool finite = isfinite(lse2) && (!good || isfinite(logp));
+  CeRow R;
+  R.lse_hi = finite ? static_cast<float>(lse2) : nanf_();
+  R.lse_lo = finite ? static_cast<float>(lse2 - static_cast<double>(R.lse_hi)) : nanf_();
+  R.weight = good ? weight : 0.0f;
+  R.token = good ? token : -1;
+  if (!good) R.lse_hi = finf(), R.lse_lo = 0.0f;  // (the row's share is 0 at every token)
+  P.rows[i] = R;
+  const bool ok = good && finite;
+  const double loss = ok ? -static_cast<double>(weight) * logp : __builtin_nan("");
+  if (P.row_loss) P.row_loss[r] = static_cast<float>(loss);
+  if (P.logp_token) P.logp_token[r] = ok ? static_cast<float>(logp) : nanf_();
+  if (P.scaled_loss) P.scaled_loss[r] = static_cast<double>(P.grad_scale) * loss;
+  if (P.row_status) P.row_status[r] = !good ? SAKI_ROW_BAD_TARGET : finite ? SAKI_ROW_OK : SAKI_ROW_NONFINITE;
+}
+
 // The gradient of a weight to which no row adds anything.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_zero_kernel(T* grad, int64_t stride, int64_t vocab, int D) {
@@ -134,7 +198,7 @@ struct Plan {
   int planes;
   int64_t slots, wave_p, piece, pieces, splits, k_split;  // wave_p: tokens of a slot
   int tile_s, tile_l, tile_x;  // tiles of the products for the loss, for dL and for dX
-  size_t count, source, place, row, scaled, stats, x, w, dl, sums, bytes;
+  size_t count, source, place, row, scaled, target, stats, x, w, dl, sums, bytes;
 };
 
 Plan plan_of(const saki_head* h, bool dx, bool dw) {
@@ -195,6 +259,7 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.place = take(n * 4);
   p.row = take(n * sizeof(CeRow));
   p.scaled = take(n * 8);
+  p.target = take(n * 4);
   p.stats = take(n * p.slots * sizeof(float2));
   p.x = take(n * p.ld * 2 * p.planes);
   p.w = three ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
@@ -212,10 +277,6 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   R.n_rows = p.n;
   R.vocab = static_cast<int>(p.V);
   R.D = static_cast<int>(p.D);
-  R.hidden = h->hidden;
-  R.weight = h->weight;
-  R.hidden_stride = h->hidden_stride;
-  R.weight_stride = h->weight_stride;
   R.token = a->token;
   R.row_weight = a->row_weight;
   R.valid = a->valid_mask;
@@ -230,6 +291,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   R.place = reinterpret_cast<int*>(ws + p.place);
   R.rows = reinterpret_cast<CeRow*>(ws + p.row);
   R.stats = reinterpret_cast<float2*>(ws + p.stats);
+  R.target = reinterpret_cast<float*>(ws + p.target);
   R.slots = static_cast<int>(p.slots);
   R.sums = reinterpret_cast<float*>(ws + p.sums);
   R.ld_sums = p.D;
@@ -292,6 +354,9 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   };
   // the log-sum-exp (bf16: of the whole vocabulary at once)
   G.stats = reinterpret_cast<float2*>(ws + p.stats);
+  G.token = a->token;
+  G.source = R.source;
+  G.target = reinterpret_cast<float*>(ws + p.target);
   G.slots = static_cast<int>(p.slots);
   const int64_t step = three ? p.piece : p.V;
   for (int64_t v0 = 0; v0 < p.V; v0 += step) {
@@ -301,10 +366,11 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     rows_q();
     G.n_p = static_cast<int>(nv);
     G.slot0 = static_cast<int>(v0 / p.wave_p);
+    G.v0 = static_cast<int>(v0);
     st = abi_launched(launch_ce_part<CE_LSE>(G, p.tile_s, three, 1, hs), "ce_gemm_kernel");
     if (st != SAKI_OK) return st;
   }
-  hipLaunchKernelGGL((ce_loss_kernel<T>), dim3(static_cast<unsigned>(p.n)), dim3(256), 0, hs, R);
+  hipLaunchKernelGGL(ce_loss_kernel, dim3(static_cast<unsigned>(p.n)), dim3(256), 0, hs, R);
   SAKI_LAUNCHED("ce_loss_kernel");
   if (a->loss_sum) {
     st = abi_loss_sum(R.scaled_loss, p.n, a->loss_sum, hs);

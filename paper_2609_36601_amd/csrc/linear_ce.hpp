@@ -58,6 +58,9 @@ struct CeGemm {
   // CE_LSE
   float2* stats;               // [rows, slots] maximum and sum in units of log2
   int slots, slot0;
+  const int32_t* token;        // the call's; of the rows that take part, source[row] where there is a count
+  const int* source;
+  float* target;               // [rows] the token's logit in units of log2
   // CE_DL
   const CeRow* rows;
   uint16_t* dl;                // [rows, ld_dl] (planes: dl_plane apart)
@@ -355,6 +358,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
   if constexpr (KIND == CE_LSE) {
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
       float m = -finf();
 #pragma unroll
       for (int i = 0; i < TP; ++i)
@@ -363,6 +367,19 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
           acc[i][j][e] = pw + 16 * i + e < A.n_p ? acc[i][j][e] * LOG2E : -finf();
           m = fmaxf(m, acc[i][j][e]);
         }
+      // The token's logit: the very number that the sum has, so that a row which is certain of its token has a log-probability as
+      // exact as its other logits' shares.
+      int at = -1;  // place of the token among this lane's 4 TP, if it is there
+      if (row < n_q) {
+        const int v = A.token[A.count ? A.source[row] : row] - A.v0 - pw;
+        at = v >= 0 && v < TP * 16 && (v & 12) == 0 ? (v >> 4) * 4 + (v & 3) : -1;
+      }
+      if (__ballot(at >= 0) != 0ull) {
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TP * 4; ++i) x = at == i ? acc[i / 4][j][i % 4] : x;
+        if (at >= 0 && pw + (at >> 2) * 16 + (at & 3) < A.n_p) A.target[row] = x;
+      }
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
       // (no token here: -infinity and 0)
@@ -374,7 +391,6 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
         for (int e = 0; e < 4; ++e) s += fexp2(acc[i][j][e] - ref);
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
-      const int row = qw + 16 * j;
       if (lane < 16 && row < n_q)
         A.stats[static_cast<int64_t>(row) * A.slots + A.slot0 + p_tile * TILE::WP + wp] = make_float2(m, s);
     }
@@ -444,9 +460,6 @@ struct CeRows {
   int64_t n_rows;
   int vocab;
   int D;
-  const void* hidden;
-  const void* weight;
-  int64_t hidden_stride, weight_stride;
   const int32_t* token;
   const float* row_weight;
   const uint8_t* valid;
@@ -463,6 +476,7 @@ struct CeRows {
   int* place;      // [n_rows] the row's place among them, or -1
   CeRow* rows;     // [rows that take part]
   const float2* stats;
+  const float* target;
   int slots;
   const float* sums;
   int64_t ld_sums, split_stride;
@@ -496,86 +510,6 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* x, int64_t stride
         out[s * (plane / 8)] = make_uint4(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16, h[4][s] | h[5][s] << 16, h[6][s] | h[7][s] << 16);
     }
   }
-}
-
-// A workgroup a row that takes part: its log-sum-exp from the tiles' maxima and sums, the target's logit as a product
-// of its own, and the row's outputs.  What bounds it: latency; every thread has four of its row's loads under way.
-template <typename T>
-__global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
-  constexpr int DEEP = 4;
-  __shared__ float part_m[4], part_dot[4];
-  __shared__ double part_s[4];
-  const int tid = threadIdx.x, lane = tid & (WAVE - 1), wave = tid / WAVE;
-  const int64_t i = blockIdx.x;
-  if (P.count && i >= *P.count) return;
-  const int64_t r = P.count ? P.source[i] : i;
-  const int token = P.token[r];
-  const float weight = P.row_weight ? P.row_weight[r] : 1.0f;
-  const bool good = token >= 0 && token < P.vocab && isfinite(weight);
-  const float2* stats = P.stats + i * P.slots;
-  float m = -finf();
-  double sum = 0.0;
-  for (int s0 = tid; s0 < P.slots; s0 += 256 * DEEP) {
-    float2 f[DEEP];
-#pragma unroll
-    for (int e = 0; e < DEEP; ++e) f[e] = stats[min(s0 + e * 256, P.slots - 1)];
-    float to = m;
-#pragma unroll
-    for (int e = 0; e < DEEP; ++e) to = fmaxf(to, f[e].x);
-    // (-infinity and 0: no token, or logits of -infinity or NaN alone, whose sum is NaN)
-    sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - to));
-    m = to;
-    const float ref = m == -finf() ? 0.0f : m;
-#pragma unroll
-    for (int e = 0; e < DEEP; ++e)
-      if (s0 + e * 256 < P.slots) sum += static_cast<double>(f[e].y) * static_cast<double>(fexp2(f[e].x - ref));
-  }
-  float dot = 0.0f;
-  if (good) {
-    const T* x = static_cast<const T*>(P.hidden) + r * P.hidden_stride;
-    const T* w = static_cast<const T*>(P.weight) + static_cast<int64_t>(token) * P.weight_stride;
-    for (int d = tid * 8; d < P.D; d += 256 * 8) {
-      float a[8], b[8];
-      Loader<T>::load8(x + d, a);
-      Loader<T>::load8(w + d, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(a[e], b[e], dot);
-    }
-  }
-  dot = wave_sum(dot);
-  const float wm = wave_max(m);
-  sum = m == -finf() ? sum : sum * static_cast<double>(fexp2(m - wm));
-#pragma unroll
-  for (int k = 1; k < WAVE; k *= 2) sum += __shfl_xor(sum, k);
-  if (lane == 0) {
-    part_m[wave] = wm;
-    part_s[wave] = sum;
-    part_dot[wave] = dot;
-  }
-  __syncthreads();
-  if (tid != 0) return;
-  m = fmaxf(fmaxf(part_m[0], part_m[1]), fmaxf(part_m[2], part_m[3]));
-  sum = 0.0;
-  dot = (part_dot[0] + part_dot[1]) + (part_dot[2] + part_dot[3]);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) sum += part_m[w] == -finf() ? part_s[w] : part_s[w] * static_cast<double>(fexp2(part_m[w] - m));
-  // (a row of -infinity alone: m and so the result)
-  const double lse2 = static_cast<double>(m) + log2(sum);
-  const double logp = static_cast<double>(dot) - lse2 / static_cast<double>(LOG2E);
-  const bool finite = isfinite(lse2) && (!good || isfinite(logp));
-  CeRow R;
-  R.lse_hi = finite ? static_cast<float>(lse2) : nanf_();
-  R.lse_lo = finite ? static_cast<float>(lse2 - static_cast<double>(R.lse_hi)) : nanf_();
-  R.weight = good ? weight : 0.0f;
-  R.token = good ? token : -1;
-  if (!good) R.lse_hi = finf(), R.lse_lo = 0.0f;  // (the row's share is 0 at every token)
-  P.rows[i] = R;
-  const bool ok = good && finite;
-  const double loss = ok ? -static_cast<double>(weight) * logp : __builtin_nan("");
-  if (P.row_loss) P.row_loss[r] = static_cast<float>(loss);
-  if (P.logp_token) P.logp_token[r] = ok ? static_cast<float>(logp) : nanf_();
-  if (P.scaled_loss) P.scaled_loss[r] = static_cast<double>(P.grad_scale) * loss;
-  if (P.row_status) P.row_status[r] = !good ? SAKI_ROW_BAD_TARGET : finite ? SAKI_ROW_OK : SAKI_ROW_NONFINITE;
 }
 
 // grad_hidden from the splits' sums.  Four of a thread's loads are under way.
