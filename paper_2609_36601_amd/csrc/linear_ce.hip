@@ -18,8 +18,18 @@ static hipError_t launch_tile(CeGemm A, bool three, int splits, hipStream_t st) 
 
 template <>
 hipError_t launch_ce_part<SAKI_PART>(const CeGemm& A, int tile, bool three, int splits, hipStream_t st) {
-  if (tile == 0) return launch_tile<SAKI_PART, CeLarge>(A, three, splits, st);
-  if (tile == 1) return launch_tile<SAKI_PART, CeMiddle>(A, three, splits, st);
+  if constexpr (SAKI_PART != CE_DW) {
+    if (tile == CE_DIRECT) {
+      CeGemm B = A;
+      B.p_tiles = (A.n_p + CeDirect::PT - 1) / CeDirect::PT;
+      B.q_tiles = (A.n_q + CeDirect::QT - 1) / CeDirect::QT;
+      hipLaunchKernelGGL((ce_direct_kernel<SAKI_PART>), dim3(static_cast<unsigned>(B.p_tiles * B.q_tiles * splits)),
+                         dim3(CeDirect::NT), 0, st, B);
+      return hipGetLastError();
+    }
+  }
+  if (tile == CE_LARGE) return launch_tile<SAKI_PART, CeLarge>(A, three, splits, st);
+  if (tile == CE_MIDDLE) return launch_tile<SAKI_PART, CeMiddle>(A, three, splits, st);
   return launch_tile<SAKI_PART, CeFew>(A, three, splits, st);
 }
 
@@ -169,6 +179,8 @@ constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
 constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
 constexpr int64_t CUS = 256;
 constexpr int64_t MOST_SPLITS = 64;
+// f32: up to so many rows the weight is read as it is.
+constexpr int64_t DIRECT_ROWS = 128;
 
 saki_status check_head(const saki_head* h) {
   if (!h) return abi_fail(SAKI_E_NULLPTR, "head is NULL");
@@ -187,8 +199,8 @@ saki_status check_head(const saki_head* h) {
 // Tiles of a product of n_p x n_q entries: the large ones where they fill the card twice, the middle ones below that, and
 // where there are few rows (their side is q) those that read the weight with the least beside it.
 int tile_of(int64_t n_p, int64_t n_q, bool rows_q) {
-  if (rows_q && n_q <= 64) return 2;
-  return ceil_div(n_p, 256) * ceil_div(n_q, 256) >= CUS ? 0 : 1;
+  if (rows_q && n_q <= CeFew::QT) return CE_FEW;
+  return ceil_div(n_p, CeLarge::PT) * ceil_div(n_q, CeLarge::QT) >= CUS ? CE_LARGE : CE_MIDDLE;
 }
 
 // The workspace of a call, and its pieces.
@@ -197,6 +209,7 @@ struct Plan {
   int64_t rows;              // n, padded to tiles
   int planes;
   int64_t slots, wave_p, piece, pieces, splits, k_split;  // wave_p: tokens of a slot
+  bool direct;               // f32 weights as they are (ce_direct_kernel)
   int tile_s, tile_l, tile_x;  // tiles of the products for the loss, for dL and for dX
   size_t count, source, place, row, scaled, target, stats, x, w, dl, sums, bytes;
 };
@@ -210,19 +223,21 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.rows = round_up(p.n, CE_PAD);
   const bool three = h->dtype == SAKI_F32;
   p.planes = three ? 3 : 1;
+  p.direct = three && p.n <= DIRECT_ROWS;
   // pieces of the vocabulary, of equal size
   const int64_t padded = round_up(p.V, CE_PAD);
   int64_t most = padded;
   if (dx || dw) most = std::min(most, PIECE_BYTES / (p.rows * 2 * p.planes));
-  if (three) most = std::min(most, PIECE_BYTES / (p.ld * 2 * p.planes));
+  if (three && !p.direct) most = std::min(most, PIECE_BYTES / (p.ld * 2 * p.planes));
   most = std::max<int64_t>(most / CE_PAD * CE_PAD, CE_PAD);
   p.pieces = ceil_div(padded, most);
   p.piece = round_up(ceil_div(padded, p.pieces), CE_PAD);
   p.pieces = ceil_div(padded, p.piece);
-  p.tile_l = tile_of(p.piece, p.n, true);
+  p.tile_l = p.direct ? CE_DIRECT : tile_of(p.piece, p.n, true);
   p.tile_s = three ? p.tile_l : tile_of(p.V, p.n, true);
-  const int64_t tile_p = p.tile_s == 0 ? CeLarge::PT : p.tile_s == 1 ? CeMiddle::PT : CeFew::PT;
-  p.wave_p = tile_p / (p.tile_s == 0 ? CeLarge::WP : p.tile_s == 1 ? CeMiddle::WP : CeFew::WP);
+  const int64_t tile_p = p.tile_s == CE_LARGE ? CeLarge::PT : p.tile_s == CE_MIDDLE ? CeMiddle::PT : CeFew::PT;
+  p.wave_p = tile_p / (p.tile_s == CE_LARGE ? CeLarge::WP : p.tile_s == CE_MIDDLE ? CeMiddle::WP : CeFew::WP);
+  static_assert(CeDirect::PT == CeFew::PT && CeDirect::WP == CeFew::WP, "slots alike");
   p.slots = ceil_div(p.V, tile_p) * (tile_p / p.wave_p);
   // dX: k, the piece's tokens, may be split between workgroups, whose sums are added up afterwards.  The tiles and the
   // splits that cost least, in microseconds: a CU takes STEP for a tile of k (of two workgroups, where two fit), rounds
@@ -230,13 +245,14 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   const int64_t kt = p.piece / CE_BK;
   double least = 0.0;
   p.splits = 0;
-  for (int tile = p.n <= CeFew::QT ? 2 : 0; tile < 3; ++tile) {
-    const int64_t t = tile == 0 ? CeLarge::QT : tile == 1 ? CeMiddle::QT : CeFew::QT, per_cu = tile == 0 ? 1 : 2;
-    const double step = tile == 0 ? 1.7 : tile == 1 ? 1.1 : 0.6;
+  for (int tile = p.direct ? CE_DIRECT : p.n <= CeFew::QT ? CE_FEW : CE_LARGE; tile <= (p.direct ? CE_DIRECT : CE_FEW); ++tile) {
+    const int64_t t = tile == CE_LARGE ? CeLarge::QT : tile == CE_MIDDLE ? CeMiddle::QT : CeFew::QT, per_cu = tile == CE_LARGE ? 1 : 2;
+    const double step = tile == CE_LARGE ? 1.7 : tile == CE_MIDDLE ? 1.1 : tile == CE_FEW ? 0.6 : 1.5;
+    const double segments = p.direct || !three ? 1.0 : 6.0;
     const int64_t tiles = ceil_div(p.n, t) * ceil_div(p.D, t);
     for (int64_t s = 1; s <= std::min<int64_t>(MOST_SPLITS, std::max<int64_t>(kt / 4, 1)); ++s) {
       const double rounds = static_cast<double>(ceil_div(tiles * s, per_cu * CUS));
-      const double cost = rounds * (3.0 + static_cast<double>(ceil_div(kt, s)) * p.planes * (three ? 2 : 1) * step) +
+      const double cost = rounds * (3.0 + static_cast<double>(ceil_div(kt, s)) * segments * step) +
                           static_cast<double>(s) * p.n * p.D * 8 / 4.5e6;
       if (p.splits == 0 || cost < least) {
         least = cost;
@@ -262,7 +278,7 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.target = take(n * 4);
   p.stats = take(n * p.slots * sizeof(float2));
   p.x = take(n * p.ld * 2 * p.planes);
-  p.w = three ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
+  p.w = three && !p.direct ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
   p.dl = dx || dw ? take(rows * p.piece * 2 * p.planes) : at;
   p.sums = dx ? take(static_cast<size_t>(p.splits) * n * p.D * 4) : at;
   p.bytes = at;
@@ -330,6 +346,11 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   bool parts_there = false;
   auto weight = [&](int64_t v0, int64_t nv) {
     if constexpr (three) {
+      if (p.direct) {
+        G.p = static_cast<const T*>(h->weight) + v0 * h->weight_stride;
+        G.ldp = h->weight_stride;
+        return hipSuccess;
+      }
       if (parts_there && p.pieces == 1) return hipSuccess;
       parts_there = true;
       const int64_t blocks = std::min<int64_t>(ceil_div(nv * p.ld / 8, 256), 8192);
@@ -350,7 +371,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     G.ldq = ldx;
     G.q_plane = x_plane;
     G.n_q = static_cast<int>(p.n);
-    G.n_k = static_cast<int>(three ? p.ld : p.D);
+    G.n_k = static_cast<int>(three && !p.direct ? p.ld : p.D);
   };
   // the log-sum-exp (bf16: of the whole vocabulary at once)
   G.stats = reinterpret_cast<float2*>(ws + p.stats);
@@ -358,7 +379,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   G.source = R.source;
   G.target = reinterpret_cast<float*>(ws + p.target);
   G.slots = static_cast<int>(p.slots);
-  const int64_t step = three ? p.piece : p.V;
+  const int64_t step = three && !p.direct ? p.piece : p.V;
   for (int64_t v0 = 0; v0 < p.V; v0 += step) {
     const int64_t nv = std::min(step, p.V - v0);
     st = abi_launched(weight(v0, nv), "ce_pack_kernel");

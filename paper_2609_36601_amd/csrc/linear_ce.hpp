@@ -46,7 +46,7 @@ struct CeRow {
 };
 
 struct CeGemm {
-  const uint16_t* p;
+  const void* p;               // bf16, or (ce_direct_kernel) f32
   const uint16_t* q;
   int64_t ldp, ldq;            // elements between rows in memory
   int64_t p_plane, q_plane;    // elements between the three parts of numbers of 32 bits
@@ -115,12 +115,14 @@ __device__ __forceinline__ uint64_t ce_scalar(const void* p) {
 // as [64][EXT], piece j of row r at j ^ 2 (r & 3) ^ (r & 8): the 32 bytes of four rows that 16 lanes of a transposing
 // read take, and those of the next 16 lanes, eight rows on, lie in different banks (where two rows fill the banks,
 // without the last).
-template <bool KC, int EXT, int WAVES>
+// SIZE: bytes of an element; of 4, as [EXT][64] with piece j of row r at j ^ (r & 15), or [64][EXT] with piece j of row r at
+// j ^ 4 (r / 8 & 3) (EXT = 64: the 16 entries that each 16 lanes read, 8 rows apart, lie in different banks).
+template <bool KC, int EXT, int WAVES, int SIZE = 2>
 struct CeSide {
-  static constexpr int BYTES = EXT * CE_BK * 2;
+  static constexpr int BYTES = EXT * CE_BK * SIZE;
   static constexpr int LOADS = BYTES / 1024 / WAVES;  // transfers of a wave and tile
   static_assert(LOADS * WAVES * 1024 == BYTES, "whole transfers");
-  static constexpr int PIECES = KC ? CE_BK / 8 : EXT / 8;  // of a row in LDS
+  static constexpr int PER = 16 / SIZE, PIECES = (KC ? CE_BK : EXT) / PER;  // entries of a piece, pieces of a row in LDS
   static constexpr int ROWS_PER = 64 / PIECES;
 
   uint64_t base;       // of the tile that is transferred next (the same in all lanes)
@@ -131,24 +133,25 @@ struct CeSide {
   __device__ __forceinline__ static int row_of(int i, int wave, int lane) { return (i * WAVES + wave) * ROWS_PER + lane / PIECES; }
   __device__ __forceinline__ static int piece_of(int row, int lane) {
     const int at = lane % PIECES;
+    if (SIZE == 4) return KC ? at ^ (row & 15) : at ^ ((row >> 3 & 3) << 2);
     return KC ? at ^ (row & 7) : at ^ ((row & 3) << 1) ^ (EXT >= 128 ? row & 8 : 0);
   }
 
   // first: the tile's first entry of p (q), of `extent`; n_k: how many k there are, whole tiles or not
-  __device__ __forceinline__ void init(const uint16_t* data, int64_t ld_, int first, int extent, int n_k, int wave, int lane) {
+  __device__ __forceinline__ void init(const void* data, int64_t ld_, int first, int extent, int n_k, int wave, int lane) {
     ld = ld_;
     const int left = extent - first, k_left = n_k % CE_BK == 0 ? CE_BK : n_k % CE_BK;
-    base = ce_scalar(data + (KC ? static_cast<int64_t>(first) * ld : static_cast<int64_t>(first)));
-    const uint32_t pitch = static_cast<uint32_t>(ld * 2);
+    base = ce_scalar(static_cast<const char*>(data) + (KC ? static_cast<int64_t>(first) * ld : static_cast<int64_t>(first)) * SIZE);
+    const uint32_t pitch = static_cast<uint32_t>(ld * SIZE);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = row_of(i, wave, lane), piece = piece_of(row, lane);
       // behind the last row (entry): the last (the tile's first); k behind the last: one that exists
       if (KC) {
         off[i] = static_cast<uint32_t>(min(row, left - 1)) * pitch + piece * 16;
-        off_last[i] = off[i] - (piece * 8 < k_left ? 0 : piece * 16);
+        off_last[i] = off[i] - (piece * PER < k_left ? 0 : piece * 16);
       } else {
-        const uint32_t at = piece * 8 < left ? piece * 16 : 0;
+        const uint32_t at = piece * PER < left ? piece * 16 : 0;
         off[i] = static_cast<uint32_t>(row) * pitch + at;
         off_last[i] = static_cast<uint32_t>(min(row, k_left - 1)) * pitch + at;
       }
@@ -158,7 +161,7 @@ struct CeSide {
   __device__ __forceinline__ void transfer(int i, uint32_t lds, bool last, int wave) const {
     ce_to_lds(__builtin_amdgcn_readfirstlane(lds + (i * WAVES + wave) * 1024), base, last ? off_last[i] : off[i]);
   }
-  __device__ __forceinline__ uint64_t step() const { return static_cast<uint64_t>(KC ? CE_BK * 2 : ld * CE_BK * 2); }
+  __device__ __forceinline__ uint64_t step() const { return static_cast<uint64_t>(KC ? CE_BK : ld * CE_BK) * SIZE; }
 };
 
 // This lane's places in an operand's tile: the fragment of 16 entries from `from` + 16 f on (f < N), k 32 kk + 8 g .. + 7.
@@ -215,6 +218,125 @@ using CeLarge = CeTile<256, 256, 2, 4, 2>;
 using CeMiddle = CeTile<128, 128, 2, 2, 2>;
 using CeFew = CeTile<64, 64, 4, 1, 4>;
 
+// Which tile and split a workgroup takes.  Workgroups go round the eight dies: each die gets a run of tiles, splits one after
+// the other (whose slices of both operands its L2 then holds), in columns of eight q, so that those at work on it at a
+// time (32) share 4 + 8 tiles.
+__device__ __forceinline__ void ce_place(const CeGemm& A, int* p_tile, int* q_tile, int* split) {
+  const int tiles = A.p_tiles * A.q_tiles, n = gridDim.x, die = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const int each = n >> 3, more = n & 7;
+  int t = die * each + min(die, more) + i;
+  *split = t / tiles;
+  t -= *split * tiles;
+  const int column = 8 * A.p_tiles, c0 = t / column * 8, wide = min(8, A.q_tiles - c0), in = t - c0 * A.p_tiles;
+  *p_tile = in / wide;
+  *q_tile = c0 + in % wide;
+}
+
+// What a wave does with its products: entry (p, q) of acc[i][j][e] is p = pw + 16 i + e, q = qw + 16 j.
+template <int KIND, typename TILE, bool THREE>
+__device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE::TP][TILE::TQ], int p_tile, int pw, int qw, int wp,
+                                          int split, int n_q, int lane) {
+  constexpr int TP = TILE::TP, TQ = TILE::TQ;
+  if constexpr (KIND == CE_LSE) {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
+      float m = -finf();
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[i][j][e] = pw + 16 * i + e < A.n_p ? acc[i][j][e] * LOG2E : -finf();
+          m = fmaxf(m, acc[i][j][e]);
+        }
+      // The token's logit: the very number that the sum has, so that a row which is certain of its token has a log-probability as
+      // exact as its other logits' shares.
+      int at = -1;  // place of the token among this lane's 4 TP, if it is there
+      if (row < n_q) {
+        const int v = A.token[A.count ? A.source[row] : row] - A.v0 - pw;
+        at = v >= 0 && v < TP * 16 && (v & 12) == 0 ? (v >> 4) * 4 + (v & 3) : -1;
+      }
+      if (__ballot(at >= 0) != 0ull) {
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TP * 4; ++i) x = at == i ? acc[i / 4][j][i % 4] : x;
+        if (at >= 0 && pw + (at >> 2) * 16 + (at & 3) < A.n_p) A.target[row] = x;
+      }
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      // (no token here: -infinity and 0)
+      const float ref = m == -finf() ? 0.0f : m;
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += fexp2(acc[i][j][e] - ref);
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      if (lane < 16 && row < n_q)
+        A.stats[static_cast<int64_t>(row) * A.slots + A.slot0 + p_tile * TILE::WP + wp] = make_float2(m, s);
+    }
+  } else if constexpr (KIND == CE_DL) {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
+      const bool there = row < n_q;
+      CeRow R = {0.0f, 0.0f, 0.0f, -1};
+      if (there) R = A.rows[row];
+      const int hot = R.token - A.v0;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        uint32_t h[4][3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = pw + 16 * i + e;
+          float x = fexp2(__builtin_fmaf(acc[i][j][e], LOG2E, -R.lse_hi) - R.lse_lo);
+          x = R.weight * (v == hot ? x - 1.0f : x);
+          if (!there || v >= A.n_p) x = 0.0f;
+          if constexpr (THREE) ce_parts(x, h[e]);
+          else h[e][0] = f32_to_bf16_bits(x);
+        }
+#pragma unroll
+        for (int s = 0; s < (THREE ? 3 : 1); ++s) {
+          const uint2 w = make_uint2(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16);
+          *reinterpret_cast<uint2*>(A.dl + s * A.dl_plane + row * A.ld_dl + pw + 16 * i) = w;
+        }
+      }
+    }
+  } else if constexpr (KIND == CE_DX) {
+    float* const sums = A.sums + split * A.split_stride;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int row = qw + 16 * j;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        if (row >= n_q || pw + 16 * i >= A.n_p) continue;
+        ce_f32x4* const to = reinterpret_cast<ce_f32x4*>(sums + row * A.ld_sums + pw + 16 * i);
+        *to = A.add ? *to + acc[i][j] : acc[i][j];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      const int64_t v = qw + 16 * j;
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        if (v >= n_q || pw + 16 * i >= A.n_p) continue;
+        const ce_f32x4 x = acc[i][j] * A.scale;
+        if constexpr (THREE) {
+          *reinterpret_cast<ce_f32x4*>(static_cast<float*>(A.grad) + v * A.ld_grad + pw + 16 * i) = x;
+        } else {
+          const uint2 w = make_uint2(f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16,
+                                     f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16);
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i) = w;
+        }
+      }
+    }
+  }
+}
+
+enum CeChoice { CE_LARGE, CE_MIDDLE, CE_FEW, CE_DIRECT };
+
 template <int KIND, typename TILE, bool THREE>
 __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGemm A) {
   constexpr int PT = TILE::PT, QT = TILE::QT, NS = TILE::NS, TP = TILE::TP, TQ = TILE::TQ;
@@ -227,19 +349,8 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wp = wave % TILE::WP, wq = wave / TILE::WP;
-  // Workgroups go round the eight dies: each die gets a run of tiles, splits one after the other (whose slices of both
-  // operands its L2 then holds), in columns of eight q, so that those at work on it at a time (32) share 4 + 8 tiles.
   int p_tile, q_tile, split;
-  {
-    const int tiles = A.p_tiles * A.q_tiles, n = gridDim.x, die = blockIdx.x & 7, i = blockIdx.x >> 3;
-    const int each = n >> 3, more = n & 7;
-    int t = die * each + min(die, more) + i;
-    split = t / tiles;
-    t -= split * tiles;
-    const int column = 8 * A.p_tiles, c0 = t / column * 8, wide = min(8, A.q_tiles - c0), in = t - c0 * A.p_tiles;
-    p_tile = in / wide;
-    q_tile = c0 + in % wide;
-  }
+  ce_place(A, &p_tile, &q_tile, &split);
   const int rows = A.count ? __builtin_amdgcn_readfirstlane(*A.count) : KIND == CE_DW ? A.n_k : A.n_q;
   const int n_q = KIND == CE_DW ? A.n_q : rows, n_k = KIND == CE_DW ? rows : A.n_k;
   const int p0 = p_tile * PT, q0 = q_tile * QT;
@@ -353,104 +464,129 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
     ce_wait<0>();  // no transfer is under way when the workgroup ends
   }
 
-  // entry (p, q): p = pw + 16 i + e, q = qw + 16 j
-  const int pw = p0 + wp * TP * 16 + (lane >> 4) * 4, qw = q0 + wq * TQ * 16 + (lane & 15);
-  if constexpr (KIND == CE_LSE) {
+  ce_finish<KIND, TILE, THREE>(A, acc, p_tile, p0 + wp * TP * 16 + (lane >> 4) * 4, q0 + wq * TQ * 16 + (lane & 15), wp, split, n_q, lane);
+}
+
+// Few rows in 32 bits: memory bounds them, so the weight (P) is read as it is and taken apart where its fragments are
+// read from LDS, 44 instructions for 8 numbers, instead of being written as three parts and read six times.  Q lies in
+// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.1 ms.
+struct CeSplit {
+  ce_bf16x8 part[3];
+};
+typedef __bf16 ce_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float ce_f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ CeSplit ce_split(const float (&x)[8]) {
+  uint32_t h[3][4];
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      const int row = qw + 16 * j;
-      float m = -finf();
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
 #pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[i][j][e] = pw + 16 * i + e < A.n_p ? acc[i][j][e] * LOG2E : -finf();
-          m = fmaxf(m, acc[i][j][e]);
-        }
-      // The token's logit: the very number that the sum has, so that a row which is certain of its token has a log-probability as
-      // exact as its other logits' shares.
-      int at = -1;  // place of the token among this lane's 4 TP, if it is there
-      if (row < n_q) {
-        const int v = A.token[A.count ? A.source[row] : row] - A.v0 - pw;
-        at = v >= 0 && v < TP * 16 && (v & 12) == 0 ? (v >> 4) * 4 + (v & 3) : -1;
-      }
-      if (__ballot(at >= 0) != 0ull) {
-        float x = 0.0f;
-#pragma unroll
-        for (int i = 0; i < TP * 4; ++i) x = at == i ? acc[i / 4][j][i % 4] : x;
-        if (at >= 0 && pw + (at >> 2) * 16 + (at & 3) < A.n_p) A.target[row] = x;
-      }
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      // (no token here: -infinity and 0)
-      const float ref = m == -finf() ? 0.0f : m;
-      float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < TP; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s += fexp2(acc[i][j][e] - ref);
-      s += __shfl_xor(s, 16);
-      s += __shfl_xor(s, 32);
-      if (lane < 16 && row < n_q)
-        A.stats[static_cast<int64_t>(row) * A.slots + A.slot0 + p_tile * TILE::WP + wp] = make_float2(m, s);
-    }
-  } else if constexpr (KIND == CE_DL) {
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      const int row = qw + 16 * j;
-      const bool there = row < n_q;
-      CeRow R = {0.0f, 0.0f, 0.0f, -1};
-      if (there) R = A.rows[row];
-      const int hot = R.token - A.v0;
-#pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        uint32_t h[4][3];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int v = pw + 16 * i + e;
-          float x = fexp2(__builtin_fmaf(acc[i][j][e], LOG2E, -R.lse_hi) - R.lse_lo);
-          x = R.weight * (v == hot ? x - 1.0f : x);
-          if (!there || v >= A.n_p) x = 0.0f;
-          if constexpr (THREE) ce_parts(x, h[e]);
-          else h[e][0] = f32_to_bf16_bits(x);
-        }
-#pragma unroll
-        for (int s = 0; s < (THREE ? 3 : 1); ++s) {
-          const uint2 w = make_uint2(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16);
-          *reinterpret_cast<uint2*>(A.dl + s * A.dl_plane + row * A.ld_dl + pw + 16 * i) = w;
-        }
-      }
-    }
-  } else if constexpr (KIND == CE_DX) {
-    float* const sums = A.sums + split * A.split_stride;
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      const int row = qw + 16 * j;
-#pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        if (row >= n_q || pw + 16 * i >= A.n_p) continue;
-        ce_f32x4* const to = reinterpret_cast<ce_f32x4*>(sums + row * A.ld_sums + pw + 16 * i);
-        *to = A.add ? *to + acc[i][j] : acc[i][j];
-      }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-      const int64_t v = qw + 16 * j;
-#pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        if (v >= n_q || pw + 16 * i >= A.n_p) continue;
-        const ce_f32x4 x = acc[i][j] * A.scale;
-        if constexpr (THREE) {
-          *reinterpret_cast<ce_f32x4*>(static_cast<float*>(A.grad) + v * A.ld_grad + pw + 16 * i) = x;
-        } else {
-          const uint2 w = make_uint2(f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16,
-                                     f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16);
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i) = w;
-        }
-      }
+    for (int s = 0; s < 3; ++s) {
+      h[s][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(ce_f32x2{a, b}, ce_bf16x2));
+      a -= __uint_as_float(h[s][i] << 16);
+      b -= __uint_as_float(h[s][i] & 0xffff0000u);
     }
   }
+  CeSplit r;
+#pragma unroll
+  for (int s = 0; s < 3; ++s) __builtin_memcpy(&r.part[s], h[s], 16);
+  return r;
+}
+
+using CeDirect = CeTile<64, 64, 4, 1, 2>;
+
+template <int KIND>
+__global__ __launch_bounds__(CeDirect::NT, 2) void ce_direct_kernel(CeGemm A) {
+  static_assert(KIND != CE_DW, "the weight is not an operand");
+  constexpr int PT = CeDirect::PT, QT = CeDirect::QT, NS = CeDirect::NS, TQ = CeDirect::TQ;
+  constexpr bool PKC = KIND != CE_DX;
+  using PSide = CeSide<PKC, PT, CeDirect::WAVES, 4>;
+  using QSide = CeSide<true, QT, CeDirect::WAVES>;
+  constexpr int LOADS = PSide::LOADS + 3 * QSide::LOADS, STAGE = PSide::BYTES + 3 * QSide::BYTES;
+  __shared__ alignas(1024) char tiles[NS * STAGE];
+  const int lane = threadIdx.x & (WAVE - 1), c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  int p_tile, q_tile, split;
+  ce_place(A, &p_tile, &q_tile, &split);
+  const int n_q = A.count ? __builtin_amdgcn_readfirstlane(*A.count) : A.n_q;
+  const int p0 = p_tile * PT, q0 = q_tile * QT;
+  if (q0 >= n_q) return;
+  int kt = (A.n_k + CE_BK - 1) / CE_BK, k_first = 0;
+  const int k_last = kt - 1;
+  if (KIND == CE_DX) {
+    k_first = split * A.k_split;
+    kt = min(kt - k_first, A.k_split);
+  }
+  PSide ps;
+  QSide qs;
+  ps.init(A.p, A.ldp, p0, A.n_p, A.n_k, wave, lane);
+  qs.init(A.q, A.ldq, q0, n_q, 0, wave, lane);
+  ps.base += ps.step() * k_first;
+  qs.base += qs.step() * k_first;
+  const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)tiles));
+  int k_next = 0;
+  auto transfer = [&](int stage) __attribute__((always_inline)) {
+    const uint32_t to = lds + stage * STAGE;
+#pragma unroll
+    for (int i = 0; i < PSide::LOADS; ++i) ps.transfer(i, to, k_first + k_next == k_last, wave);
+    QSide part = qs;
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+#pragma unroll
+      for (int i = 0; i < QSide::LOADS; ++i) part.transfer(i, to + PSide::BYTES + s * QSide::BYTES, false, wave);
+      part.base += static_cast<uint64_t>(A.q_plane * 2);
+    }
+    if (k_next + 1 < kt) {  // (behind the last tile: the last again, which nobody reads)
+      ++k_next;
+      ps.base += ps.step();
+      qs.base += qs.step();
+    }
+  };
+  CeFrag<true, QT, TQ> qf;
+  qf.init(tiles + PSide::BYTES, 0, lane);
+  ce_f32x4 acc[1][TQ];
+#pragma unroll
+  for (int j = 0; j < TQ; ++j) acc[0][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (kt > 0) {
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) transfer(s);
+    int now = 0;
+    for (int t = 0; t < kt; ++t) {
+      ce_wait<(NS - 2) * LOADS>();  // this tile is there, and nobody reads the one before it any more
+      transfer(now + NS - 1 >= NS ? now - 1 : now + NS - 1);
+      const int at = now * STAGE;
+      now = now + 1 == NS ? 0 : now + 1;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        float x[8];
+        if constexpr (PKC) {
+          const int row = wave * 16 + c, piece = kk * 8 + 2 * g;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            __builtin_memcpy(x + 4 * h, tiles + at + row * (CE_BK * 4) + ((piece + h) ^ (row & 15)) * 16, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int row = kk * 32 + 8 * g + e, p = wave * 16 + c;
+            x[e] = *reinterpret_cast<const float*>(tiles + at + row * (PT * 4) + ((p >> 2) ^ (g << 2)) * 16 + (p & 3) * 4);
+          }
+        }
+        const CeSplit p = ce_split(x);
+#pragma unroll
+        for (int s = 2; s >= 0; --s) {  // q's parts, the smallest first, with those of p that matter beside them
+          ce_bf16x8 q[TQ];
+#pragma unroll
+          for (int j = 0; j < TQ; ++j) q[j] = qf.read(at + s * QSide::BYTES, j, kk);
+#pragma unroll
+          for (int h = 2 - s; h >= 0; --h)
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p.part[h], q[j], acc[0][j], 0, 0, 0);
+        }
+      }
+    }
+    ce_wait<0>();  // no transfer is under way when the workgroup ends
+  }
+  ce_finish<KIND, CeDirect, true>(A, acc, p_tile, p0 + wave * 16 + g * 4, q0 + c, wave, split, n_q, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -546,6 +682,6 @@ __global__ __launch_bounds__(256) void ce_grad_hidden_kernel(CeRows P) {
 
 // linear_ce.hip, a unit for each part (CeKind)
 template <int KIND>
-hipError_t launch_ce_part(const CeGemm& A, int tile, bool three, int splits, hipStream_t st);
+hipError_t launch_ce_part(const CeGemm& A, int tile, bool three, int splits, hipStream_t st);  // tile: CeChoice
 
 }  // namespace saki
