@@ -203,15 +203,39 @@ int tile_of(int64_t n_p, int64_t n_q, bool rows_q) {
   return ceil_div(n_p, CeLarge::PT) * ceil_div(n_q, CeLarge::QT) >= CUS ? CE_LARGE : CE_MIDDLE;
 }
 
+// A product whose k may be split between workgroups, whose sums are added up afterwards: the tile, from `first` on, and the
+// splits that cost least, in microseconds.  A CU takes STEP for a tile of k (of two workgroups, where two fit), rounds
+// that leave CUs idle cost like others, starting and ending a tile takes 3, and a split's sums are written and read.
+void split_product(int64_t n_q, int64_t n_p, int64_t kt, bool three, int first, int* tile, int64_t* k_split, int64_t* splits) {
+  double least = -1.0;
+  for (int t = first; t <= std::max<int>(first, CE_FEW); ++t) {
+    const int64_t side = t == CE_LARGE ? CeLarge::QT : t == CE_MIDDLE ? CeMiddle::QT : CeFew::QT, per_cu = t == CE_LARGE ? 1 : 2;
+    const double step = (t == CE_LARGE ? 1.7 : t == CE_MIDDLE ? 1.1 : t == CE_FEW ? 0.6 : 1.5) * (three ? 6.0 : 1.0);
+    const int64_t tiles = ceil_div(n_q, side) * ceil_div(n_p, side);
+    for (int64_t s = 1; s <= std::min<int64_t>(MOST_SPLITS, std::max<int64_t>(kt / 4, 1)); ++s) {
+      const double rounds = static_cast<double>(ceil_div(tiles * s, per_cu * CUS));
+      const double cost = rounds * (3.0 + static_cast<double>(ceil_div(kt, s)) * step) + static_cast<double>(s) * n_q * n_p * 8 / 4.5e6;
+      if (least < 0.0 || cost < least) {
+        least = cost;
+        *tile = t;
+        *splits = s;
+      }
+    }
+  }
+  *k_split = ceil_div(kt, *splits);
+  *splits = std::max<int64_t>(ceil_div(kt, *k_split), 1);
+}
+
 // The workspace of a call, and its pieces.
 struct Plan {
   int64_t n, V, D, ld;       // ld: elements of a packed row, whole tiles of k
   int64_t rows;              // n, padded to tiles
   int planes;
-  int64_t slots, wave_p, piece, pieces, splits, k_split;  // wave_p: tokens of a slot
+  int64_t slots, wave_p, piece, pieces;     // wave_p: tokens of a slot
+  int64_t splits, k_split, w_splits, w_split;  // of dX's and dW's k, and tiles of k of each
   bool direct;               // f32 weights as they are (ce_direct_kernel)
-  int tile_s, tile_l, tile_x;  // tiles of the products for the loss, for dL and for dX
-  size_t count, source, place, row, scaled, target, stats, x, w, dl, sums, bytes;
+  int tile_s, tile_l, tile_x, tile_w;  // tiles of the products for the loss, for dL, dX and dW
+  size_t count, source, place, row, scaled, target, stats, x, w, dl, sums, w_sums, bytes;
 };
 
 Plan plan_of(const saki_head* h, bool dx, bool dw) {
@@ -239,30 +263,14 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.wave_p = tile_p / (p.tile_s == CE_LARGE ? CeLarge::WP : p.tile_s == CE_MIDDLE ? CeMiddle::WP : CeFew::WP);
   static_assert(CeDirect::PT == CeFew::PT && CeDirect::WP == CeFew::WP, "slots alike");
   p.slots = ceil_div(p.V, tile_p) * (tile_p / p.wave_p);
-  // dX: k, the piece's tokens, may be split between workgroups, whose sums are added up afterwards.  The tiles and the
-  // splits that cost least, in microseconds: a CU takes STEP for a tile of k (of two workgroups, where two fit), rounds
-  // that leave CUs idle cost like others, starting and ending a tile takes 3, and a split's sums are written and read.
+  // dX's k are the piece's tokens; dW's, where the piece is the whole vocabulary (which may be small), the rows
   const int64_t kt = p.piece / CE_BK;
-  double least = 0.0;
-  p.splits = 0;
-  for (int tile = p.direct ? CE_DIRECT : p.n <= CeFew::QT ? CE_FEW : CE_LARGE; tile <= (p.direct ? CE_DIRECT : CE_FEW); ++tile) {
-    const int64_t t = tile == CE_LARGE ? CeLarge::QT : tile == CE_MIDDLE ? CeMiddle::QT : CeFew::QT, per_cu = tile == CE_LARGE ? 1 : 2;
-    const double step = tile == CE_LARGE ? 1.7 : tile == CE_MIDDLE ? 1.1 : tile == CE_FEW ? 0.6 : 1.5;
-    const double segments = p.direct || !three ? 1.0 : 6.0;
-    const int64_t tiles = ceil_div(p.n, t) * ceil_div(p.D, t);
-    for (int64_t s = 1; s <= std::min<int64_t>(MOST_SPLITS, std::max<int64_t>(kt / 4, 1)); ++s) {
-      const double rounds = static_cast<double>(ceil_div(tiles * s, per_cu * CUS));
-      const double cost = rounds * (3.0 + static_cast<double>(ceil_div(kt, s)) * segments * step) +
-                          static_cast<double>(s) * p.n * p.D * 8 / 4.5e6;
-      if (p.splits == 0 || cost < least) {
-        least = cost;
-        p.tile_x = tile;
-        p.splits = s;
-      }
-    }
-  }
-  p.k_split = ceil_div(kt, p.splits);
-  p.splits = ceil_div(kt, p.k_split);
+  p.tile_x = p.direct ? CE_DIRECT : p.n <= CeFew::QT ? CE_FEW : CE_LARGE;
+  split_product(p.n, p.D, kt, three && !p.direct, p.tile_x, &p.tile_x, &p.k_split, &p.splits);
+  p.tile_w = tile_of(p.D, p.piece, false);
+  p.w_split = ceil_div(p.n, CE_BK);
+  p.w_splits = 1;
+  if (p.pieces == 1) split_product(p.V, p.D, p.w_split, three, CE_LARGE, &p.tile_w, &p.w_split, &p.w_splits);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -281,6 +289,7 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.w = three && !p.direct ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
   p.dl = dx || dw ? take(rows * p.piece * 2 * p.planes) : at;
   p.sums = dx ? take(static_cast<size_t>(p.splits) * n * p.D * 4) : at;
+  p.w_sums = dw && p.w_splits > 1 ? take(static_cast<size_t>(p.w_splits) * p.V * p.D * 4) : at;
   p.bytes = at;
   return p;
 }
@@ -292,7 +301,6 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   CeRows R{};
   R.n_rows = p.n;
   R.vocab = static_cast<int>(p.V);
-  R.D = static_cast<int>(p.D);
   R.token = a->token;
   R.row_weight = a->row_weight;
   R.valid = a->valid_mask;
@@ -301,18 +309,12 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   R.logp_token = a->logp_token;
   R.scaled_loss = a->loss_sum ? reinterpret_cast<double*>(ws + p.scaled) : nullptr;
   R.row_status = a->row_status;
-  R.grad_hidden = a->grad_hidden;
-  R.grad_stride = a->grad_hidden_stride;
   R.source = reinterpret_cast<int*>(ws + p.source);
   R.place = reinterpret_cast<int*>(ws + p.place);
   R.rows = reinterpret_cast<CeRow*>(ws + p.row);
   R.stats = reinterpret_cast<float2*>(ws + p.stats);
   R.target = reinterpret_cast<float*>(ws + p.target);
   R.slots = static_cast<int>(p.slots);
-  R.sums = reinterpret_cast<float*>(ws + p.sums);
-  R.ld_sums = p.D;
-  R.split_stride = p.n * p.D;
-  R.splits = static_cast<int>(p.splits);
   saki_status st;
 #define SAKI_LAUNCHED(what)                     \
   st = abi_launched(hipGetLastError(), what);   \
@@ -422,8 +424,8 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
       X.n_k = static_cast<int>(nv);
       X.k_split = static_cast<int>(p.k_split);
       X.sums = reinterpret_cast<float*>(ws + p.sums);
-      X.ld_sums = R.ld_sums;
-      X.split_stride = R.split_stride;
+      X.ld_sums = p.D;
+      X.split_stride = p.n * p.D;
       X.add = v0 > 0;
       st = abi_launched(launch_ce_part<CE_DX>(X, p.tile_x, three, static_cast<int>(p.splits), hs), "ce_gemm_kernel");
       if (st != SAKI_OK) return st;
@@ -442,15 +444,30 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
       W.grad = static_cast<T*>(a->grad_weight) + v0 * a->grad_weight_stride;
       W.ld_grad = a->grad_weight_stride;
       W.scale = a->grad_scale;
-      st = abi_launched(launch_ce_part<CE_DW>(W, tile_of(p.D, nv, false), three, 1, hs), "ce_gemm_kernel");
+      W.k_split = static_cast<int>(p.w_split);
+      if (p.w_splits > 1) {
+        W.sums = reinterpret_cast<float*>(ws + p.w_sums);
+        W.ld_sums = p.D;
+        W.split_stride = p.V * p.D;
+      }
+      st = abi_launched(launch_ce_part<CE_DW>(W, p.tile_w, three, static_cast<int>(p.w_splits), hs), "ce_gemm_kernel");
       if (st != SAKI_OK) return st;
     }
   }
+  using S = std::conditional_t<three, float, uint16_t>;
+  auto add_up = [&](const CeSums& C) {
+    const int64_t blocks = std::min<int64_t>(ceil_div(C.n_rows * p.D / 4, 256), 16384);
+    hipLaunchKernelGGL((ce_sums_kernel<S>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs, C);
+  };
   if (dx) {
-    const int64_t blocks = std::min<int64_t>(ceil_div(p.n * p.D / 4, 256), 16384);
-    using S = std::conditional_t<three, float, uint16_t>;
-    hipLaunchKernelGGL((ce_grad_hidden_kernel<S>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, hs, R);
-    SAKI_LAUNCHED("ce_grad_hidden_kernel");
+    add_up(CeSums{reinterpret_cast<float*>(ws + p.sums), p.D, p.n * p.D, static_cast<int>(p.splits), p.n, static_cast<int>(p.D),
+                  R.count ? R.place : nullptr, R.rows, a->grad_scale, a->grad_hidden, a->grad_hidden_stride});
+    SAKI_LAUNCHED("ce_sums_kernel");
+  }
+  if (dw && p.w_splits > 1) {
+    add_up(CeSums{reinterpret_cast<float*>(ws + p.w_sums), p.D, p.V * p.D, static_cast<int>(p.w_splits), p.V, static_cast<int>(p.D),
+                  nullptr, nullptr, a->grad_scale, a->grad_weight, a->grad_weight_stride});
+    SAKI_LAUNCHED("ce_sums_kernel");
   }
 #undef SAKI_LAUNCHED
   return SAKI_OK;

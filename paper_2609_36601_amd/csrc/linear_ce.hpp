@@ -54,7 +54,7 @@ struct CeGemm {
   const int* count;            // rows that take part, or NULL: all
   int planes;                  // 1 or 3
   int p_tiles, q_tiles;
-  int k_split;                 // CE_DX: tiles of k of a split
+  int k_split;                 // CE_DX, CE_DW: tiles of k of a split
   // CE_LSE
   float2* stats;               // [rows, slots] maximum and sum in units of log2
   int slots, slot0;
@@ -66,8 +66,8 @@ struct CeGemm {
   uint16_t* dl;                // [rows, ld_dl] (planes: dl_plane apart)
   int64_t ld_dl, dl_plane;
   int v0;                      // the piece's first token
-  // CE_DX
-  float* sums;                 // [splits, rows, ld_sums]
+  // CE_DX, and CE_DW where it has splits (else NULL)
+  float* sums;                 // [splits, q, ld_sums]
   int64_t ld_sums, split_stride;
   int add;                     // to the sums of the pieces before
   // CE_DW
@@ -322,6 +322,10 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
       for (int i = 0; i < TP; ++i) {
         if (v >= n_q || pw + 16 * i >= A.n_p) continue;
+        if (A.sums) {  // (k in splits)
+          *reinterpret_cast<ce_f32x4*>(A.sums + split * A.split_stride + v * A.ld_sums + pw + 16 * i) = acc[i][j];
+          continue;
+        }
         const ce_f32x4 x = acc[i][j] * A.scale;
         if constexpr (THREE) {
           *reinterpret_cast<ce_f32x4*>(static_cast<float*>(A.grad) + v * A.ld_grad + pw + 16 * i) = x;
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
   const int p0 = p_tile * PT, q0 = q_tile * QT;
   if (q0 >= n_q) return;
   int kt = (n_k + CE_BK - 1) / CE_BK, k_first = 0;
-  if (KIND == CE_DX) {
+  if (KIND == CE_DX || KIND == CE_DW) {
     k_first = split * A.k_split;
     kt = min(kt - k_first, A.k_split);
   }
@@ -469,7 +473,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 
 // Few rows in 32 bits: memory bounds them, so the weight (P) is read as it is and taken apart where its fragments are
 // read from LDS, 44 instructions for 8 numbers, instead of being written as three parts and read six times.  Q lies in
-// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.1 ms.
+// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.8 ms.
 struct CeSplit {
   ce_bf16x8 part[3];
 };
@@ -595,7 +599,6 @@ __global__ __launch_bounds__(CeDirect::NT, 2) void ce_direct_kernel(CeGemm A) {
 struct CeRows {
   int64_t n_rows;
   int vocab;
-  int D;
   const int32_t* token;
   const float* row_weight;
   const uint8_t* valid;
@@ -604,8 +607,6 @@ struct CeRows {
   float* logp_token;
   double* scaled_loss;
   uint8_t* row_status;
-  void* grad_hidden;
-  int64_t grad_stride;
   // workspace
   int* count;      // rows that take part (with a mask)
   int* source;     // [rows that take part] their place in the call
@@ -614,9 +615,6 @@ struct CeRows {
   const float2* stats;
   const float* target;
   int slots;
-  const float* sums;
-  int64_t ld_sums, split_stride;
-  int splits;
 };
 
 // Rows of T as bf16 (T = float: as three parts), 64-element pieces whole: elements behind D are 0.
@@ -648,14 +646,26 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* x, int64_t stride
   }
 }
 
-// grad_hidden from the splits' sums.  Four of a thread's loads are under way.
+// A gradient from the splits' sums, [splits, rows that take part, ld_sums].  Four of a thread's loads are under way.
+struct CeSums {
+  const float* sums;
+  int64_t ld_sums, split_stride;
+  int splits;
+  int64_t n_rows;
+  int D;
+  const int* place;   // each row's place in the sums, -1: none (0); NULL: its own
+  const CeRow* rows;  // rows without a token are NaN; NULL: none
+  float scale;
+  void* grad;
+  int64_t stride;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void ce_grad_hidden_kernel(CeRows P) {
+__global__ __launch_bounds__(256) void ce_sums_kernel(CeSums P) {
   const int pieces = P.D / 4;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < P.n_rows * pieces; i += gridDim.x * 256ll) {
     const int64_t r = i / pieces;
     const int d = static_cast<int>(i - r * pieces) * 4;
-    const int64_t at = P.count ? P.place[r] : r;
+    const int64_t at = P.place ? P.place[r] : r;
     ce_f32x4 g = {0.0f, 0.0f, 0.0f, 0.0f};
     if (at >= 0) {
       const float* from = P.sums + at * P.ld_sums + d;
@@ -668,9 +678,9 @@ __global__ __launch_bounds__(256) void ce_grad_hidden_kernel(CeRows P) {
         for (int e = 0; e < 4; ++e) g += v[e];
       }
       for (; s < P.splits; ++s) g += *reinterpret_cast<const ce_f32x4*>(from + s * P.split_stride);
-      g *= P.rows[at].token < 0 ? nanf_() : P.grad_scale;
+      g *= P.rows && P.rows[at].token < 0 ? nanf_() : P.scale;
     }
-    T* const to = static_cast<T*>(P.grad_hidden) + r * P.grad_stride + d;
+    T* const to = static_cast<T*>(P.grad) + r * P.stride + d;
     if constexpr (sizeof(T) == 4) {
       *reinterpret_cast<ce_f32x4*>(to) = g;
     } else {
