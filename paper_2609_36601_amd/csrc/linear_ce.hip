@@ -11,8 +11,13 @@ static hipError_t launch_tile(CeGemm A, bool three, int splits, hipStream_t st) 
   A.p_tiles = (A.n_p + TILE::PT - 1) / TILE::PT;
   A.q_tiles = (A.n_q + TILE::QT - 1) / TILE::QT;
   const dim3 grid(static_cast<unsigned>(A.p_tiles * A.q_tiles * splits)), block(TILE::NT);
-  if (three) hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, true>), grid, block, 0, st, A);
-  else hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, false>), grid, block, 0, st, A);
+  if constexpr (std::is_same_v<TILE, CeFew> && (KIND == CE_LSE || KIND == CE_DL)) {  // (f32: ce_direct_kernel)
+    if (three) return hipErrorInvalidValue;
+  } else if (three) {
+    hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, true>), grid, block, 0, st, A);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((ce_gemm_kernel<KIND, TILE, false>), grid, block, 0, st, A);
   return hipGetLastError();
 }
 
@@ -175,12 +180,18 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t MOST_STRIDE = int64_t{1} << 22;
 constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
 // Bytes of the gradient of a piece's logits, and of a piece of the weight in three parts: what the
-// last-level cache holds, at most.
+// last-level cache holds, at most (its pieces cost each product a start and an end).
 constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
 constexpr int64_t CUS = 256;
 constexpr int64_t MOST_SPLITS = 64;
-// f32: up to so many rows the weight is read as it is.
-constexpr int64_t DIRECT_ROWS = 128;
+// f32: up to so many rows the weight is read as it is, above them it is written as three parts first.  Loss and gradients in
+// microseconds, as it is / in parts:
+//   rows             16          128          512          768         1,024        2,048
+//   4,000 x 1,024                          145/217      204/247      243/274      439/411
+//   32,000 x 1,024   139/301     234/391   825/833    1,227/1,172  1,621/1,387  3,336/2,834
+//   50,000 x 2,048   468/1,279   748/1,865 2,597/3,173  3,827/4,076  5,072/5,202 10,002/9,009
+//   151,936 x 4,096  2.4k/7.7k   4.2k/14k   15k/20k     23k/23k      30k/34k      59k/58k
+constexpr int64_t DIRECT_ROWS = 768;
 
 saki_status check_head(const saki_head* h) {
   if (!h) return abi_fail(SAKI_E_NULLPTR, "head is NULL");

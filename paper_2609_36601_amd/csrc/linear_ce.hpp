@@ -341,6 +341,29 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 
 enum CeChoice { CE_LARGE, CE_MIDDLE, CE_FEW, CE_DIRECT };
 
+// Logits in sums of 256 k: a logit that grows to 50 along k is otherwise rounded, at that size, at each of its products.
+// A row that is certain of its token has a log-probability near 0 that is as far off as the difference of two such logits
+// (2 rows of 2,880, log-probability 1.0e-5 off relative to itself where the sums were not split).  Few rows have the
+// registers for it, and no other rows whose larger losses such an error is small beside.
+template <int KIND, typename TILE>
+constexpr bool CE_CHUNKS = (KIND == CE_LSE || KIND == CE_DL) && TILE::QT == CeFew::QT;
+template <int TQ>
+struct CeChunks {
+  ce_f32x4 sum[TQ] = {};
+  __device__ __forceinline__ void end(ce_f32x4 (&acc)[1][TQ]) const {
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) acc[0][j] += sum[j];
+  }
+  __device__ __forceinline__ void add(ce_f32x4 (&acc)[1][TQ], int t) {
+    if (t % 4 != 3) return;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+      sum[j] += acc[0][j];
+      acc[0][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+};
+
 template <int KIND, typename TILE, bool THREE>
 __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGemm A) {
   constexpr int PT = TILE::PT, QT = TILE::QT, NS = TILE::NS, TP = TILE::TP, TQ = TILE::TQ;
@@ -434,6 +457,7 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 #pragma unroll
     for (int j = 0; j < TQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(have.p[i], have.q[j], acc[i][j], 0, 0, 0);
   };
+  CeChunks<TQ> chunks;
   if (steps > 0) {
     Half a, b;
 #pragma unroll
@@ -464,8 +488,10 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
         __builtin_amdgcn_sched_barrier(0);
       }
       transferred();
+      if constexpr (CE_CHUNKS<KIND, TILE>) chunks.add(acc, t);
     }
     ce_wait<0>();  // no transfer is under way when the workgroup ends
+    if constexpr (CE_CHUNKS<KIND, TILE>) chunks.end(acc);
   }
 
   ce_finish<KIND, TILE, THREE>(A, acc, p_tile, p0 + wp * TP * 16 + (lane >> 4) * 4, q0 + wq * TQ * 16 + (lane & 15), wp, split, n_q, lane);
@@ -473,7 +499,8 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 
 // Few rows in 32 bits: memory bounds them, so the weight (P) is read as it is and taken apart where its fragments are
 // read from LDS, 44 instructions for 8 numbers, instead of being written as three parts and read six times.  Q lies in
-// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.8 ms.
+// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.8 ms.  Each workgroup takes the weight
+// apart for 64 rows, so many rows go the other way (DIRECT_ROWS).
 struct CeSplit {
   ce_bf16x8 part[3];
 };
@@ -551,6 +578,7 @@ __global__ __launch_bounds__(CeDirect::NT, 2) void ce_direct_kernel(CeGemm A) {
   ce_f32x4 acc[1][TQ];
 #pragma unroll
   for (int j = 0; j < TQ; ++j) acc[0][j] = ce_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  CeChunks<TQ> chunks;
   if (kt > 0) {
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) transfer(s);
@@ -587,8 +615,10 @@ __global__ __launch_bounds__(CeDirect::NT, 2) void ce_direct_kernel(CeGemm A) {
             for (int j = 0; j < TQ; ++j) acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p.part[h], q[j], acc[0][j], 0, 0, 0);
         }
       }
+      if constexpr (CE_CHUNKS<KIND, CeDirect>) chunks.add(acc, t);
     }
     ce_wait<0>();  // no transfer is under way when the workgroup ends
+    if constexpr (CE_CHUNKS<KIND, CeDirect>) chunks.end(acc);
   }
   ce_finish<KIND, CeDirect, true>(A, acc, p_tile, p0 + wave * 16 + g * 4, q0 + c, wave, split, n_q, lane);
 }
