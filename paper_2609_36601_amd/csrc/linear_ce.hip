@@ -182,6 +182,13 @@ constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
 // Bytes of the gradient of a piece's logits, and of a piece of the weight in three parts: what the
 // last-level cache holds, at most (its pieces cost each product a start and an end).
 constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
+// Bytes of logits that a training call keeps, at most; above it, it computes them a second time, in pieces.  Loss and gradients
+// in microseconds, kept / again (bf16; 1,024 rows of 4,096 in f32):
+//   rows             16         64         200          400          1,024
+//   32,000 x 512     49/53      54/57      77/79        111/115      169/177
+//   50,000 x 2,048   189/222    204/234    293/329      408/474      719/848
+//   151,936 x 4,096  1.05k/1.25k 1.13k/1.34k 1.39k/1.69k  1.98k/2.43k  f32: 50,000 x 2,048 3.79k/5.01k
+constexpr int64_t KEEP_BYTES = int64_t{1} << 30;
 constexpr int64_t CUS = 256;
 constexpr int64_t MOST_SPLITS = 64;
 // f32: up to so many rows the weight is read as it is, above them it is written as three parts first.  Loss and gradients in
@@ -246,7 +253,8 @@ struct Plan {
   int64_t splits, k_split, w_splits, w_split;  // of dX's and dW's k, and tiles of k of each
   bool direct;               // f32 weights as they are (ce_direct_kernel)
   int tile_s, tile_l, tile_x, tile_w;  // tiles of the products for the loss, for dL, dX and dW
-  size_t count, source, place, row, scaled, target, stats, x, w, dl, sums, w_sums, bytes;
+  bool keep;                 // the logits, between the loss and dL
+  size_t count, source, place, row, scaled, target, stats, x, w, dl, logits, sums, w_sums, bytes;
 };
 
 Plan plan_of(const saki_head* h, bool dx, bool dw) {
@@ -282,6 +290,9 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.w_split = ceil_div(p.n, CE_BK);
   p.w_splits = 1;
   if (p.pieces == 1) split_product(p.V, p.D, p.w_split, three, CE_LARGE, &p.tile_w, &p.w_split, &p.w_splits);
+  // Logits kept: written, read, 8 bytes each.  Computed again: their products, or where there are few rows the weight's reading.
+  const double again = std::max((three ? 6.0 : 1.0) * 2.0 * p.n * p.D / 1.0e9, (three ? 4.0 : 2.0) * p.D / 4.5e6);
+  p.keep = (dx || dw) && p.n * padded * 4 <= KEEP_BYTES && p.n * 8 / 5.0e6 < again;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -299,6 +310,7 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.x = take(n * p.ld * 2 * p.planes);
   p.w = three && !p.direct ? take(static_cast<size_t>(p.piece) * p.ld * 2 * p.planes) : at;
   p.dl = dx || dw ? take(rows * p.piece * 2 * p.planes) : at;
+  p.logits = p.keep ? take(static_cast<size_t>(padded) * n * 4) : at;
   p.sums = dx ? take(static_cast<size_t>(p.splits) * n * p.D * 4) : at;
   p.w_sums = dw && p.w_splits > 1 ? take(static_cast<size_t>(p.w_splits) * p.V * p.D * 4) : at;
   p.bytes = at;
@@ -392,6 +404,8 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   G.source = R.source;
   G.target = reinterpret_cast<float*>(ws + p.target);
   G.slots = static_cast<int>(p.slots);
+  float* const logits = p.keep ? reinterpret_cast<float*>(ws + p.logits) : nullptr;
+  G.ld_logits = round_up(p.V, CE_PAD);
   const int64_t step = three && !p.direct ? p.piece : p.V;
   for (int64_t v0 = 0; v0 < p.V; v0 += step) {
     const int64_t nv = std::min(step, p.V - v0);
@@ -401,6 +415,7 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     G.n_p = static_cast<int>(nv);
     G.slot0 = static_cast<int>(v0 / p.wave_p);
     G.v0 = static_cast<int>(v0);
+    G.logits = logits ? logits + v0 : nullptr;
     st = abi_launched(launch_ce_part<CE_LSE>(G, p.tile_s, three, 1, hs), "ce_gemm_kernel");
     if (st != SAKI_OK) return st;
   }
@@ -415,8 +430,10 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
   const int64_t dl_plane = p.rows * p.piece;
   for (int64_t v0 = 0; v0 < p.V; v0 += p.piece) {
     const int64_t nv = std::min(p.piece, p.V - v0);
-    st = abi_launched(weight(v0, nv), "ce_pack_kernel");
-    if (st != SAKI_OK) return st;
+    if (dx || !logits) {
+      st = abi_launched(weight(v0, nv), "ce_pack_kernel");
+      if (st != SAKI_OK) return st;
+    }
     rows_q();
     G.n_p = static_cast<int>(nv);
     G.rows = R.rows;
@@ -424,8 +441,15 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     G.ld_dl = p.piece;
     G.dl_plane = dl_plane;
     G.v0 = static_cast<int>(v0);
-    st = abi_launched(launch_ce_part<CE_DL>(G, p.tile_l, three, 1, hs), "ce_gemm_kernel");
-    if (st != SAKI_OK) return st;
+    if (logits) {
+      G.logits = logits + v0;
+      const dim3 grid(static_cast<unsigned>(ceil_div(nv, 2048)), static_cast<unsigned>(std::min<int64_t>(round_up(p.n, CE_BK), 4096)));
+      hipLaunchKernelGGL((ce_share_kernel<three>), grid, dim3(256), 0, hs, G);
+      SAKI_LAUNCHED("ce_share_kernel");
+    } else {
+      st = abi_launched(launch_ce_part<CE_DL>(G, p.tile_l, three, 1, hs), "ce_gemm_kernel");
+      if (st != SAKI_OK) return st;
+    }
     if (dx) {
       CeGemm X = G;
       X.q = dl;

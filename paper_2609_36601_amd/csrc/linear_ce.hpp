@@ -61,6 +61,8 @@ struct CeGemm {
   const int32_t* token;        // the call's; of the rows that take part, source[row] where there is a count
   const int* source;
   float* target;               // [rows] the token's logit in units of log2
+  float* logits;               // [rows, ld_logits] kept for the gradient, or NULL
+  int64_t ld_logits;           // at least p_tiles whole tiles
   // CE_DL
   const CeRow* rows;
   uint16_t* dl;                // [rows, ld_dl] (planes: dl_plane apart)
@@ -232,6 +234,16 @@ __device__ __forceinline__ void ce_place(const CeGemm& A, int* p_tile, int* q_ti
   *q_tile = c0 + in % wide;
 }
 
+// A logit's gradient, as the products take it.
+template <bool THREE>
+__device__ __forceinline__ void ce_share(const CeRow& R, float logit, bool hot, bool there, uint32_t (&h)[3]) {
+  float x = fexp2(__builtin_fmaf(logit, LOG2E, -R.lse_hi) - R.lse_lo);
+  x = R.weight * (hot ? x - 1.0f : x);
+  if (!there) x = 0.0f;
+  if constexpr (THREE) ce_parts(x, h);
+  else h[0] = f32_to_bf16_bits(x);
+}
+
 // What a wave does with its products: entry (p, q) of acc[i][j][e] is p = pw + 16 i + e, q = qw + 16 j.
 template <int KIND, typename TILE, bool THREE>
 __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE::TP][TILE::TQ], int p_tile, int pw, int qw, int wp,
@@ -241,6 +253,11 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
       const int row = qw + 16 * j;
+      if (A.logits && row < n_q) {
+        float* const to = A.logits + row * A.ld_logits + pw;
+#pragma unroll
+        for (int i = 0; i < TP; ++i) *reinterpret_cast<ce_f32x4*>(to + 16 * i) = acc[i][j];
+      }
       float m = -finf();
 #pragma unroll
       for (int i = 0; i < TP; ++i)
@@ -290,11 +307,7 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int v = pw + 16 * i + e;
-          float x = fexp2(__builtin_fmaf(acc[i][j][e], LOG2E, -R.lse_hi) - R.lse_lo);
-          x = R.weight * (v == hot ? x - 1.0f : x);
-          if (!there || v >= A.n_p) x = 0.0f;
-          if constexpr (THREE) ce_parts(x, h[e]);
-          else h[e][0] = f32_to_bf16_bits(x);
+          ce_share<THREE>(R, acc[i][j][e], v == hot, there && v < A.n_p, h[e]);
         }
 #pragma unroll
         for (int s = 0; s < (THREE ? 3 : 1); ++s) {
@@ -673,6 +686,33 @@ __global__ __launch_bounds__(256) void ce_pack_kernel(const T* x, int64_t stride
       for (int s = 0; s < 3; ++s)
         out[s * (plane / 8)] = make_uint4(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16, h[4][s] | h[5][s] << 16, h[6][s] | h[7][s] << 16);
     }
+  }
+}
+
+// dL where the log-sum-exp's product kept its logits, in whole tiles of k of the products that read it.  A thread takes 8
+// tokens.  It reads 4 bytes and writes 2 (three parts: 6) a logit, mostly in the last-level cache.
+template <bool THREE>
+__global__ __launch_bounds__(256) void ce_share_kernel(CeGemm A) {
+  const int rows = A.count ? *A.count : A.n_q;
+  const int v = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (v >= (A.n_p + CE_BK - 1) / CE_BK * CE_BK) return;
+  for (int row = blockIdx.y; row < (rows + CE_BK - 1) / CE_BK * CE_BK; row += gridDim.y) {
+    const bool there = row < rows;
+    CeRow R = {0.0f, 0.0f, 0.0f, -1};
+    ce_f32x4 x[2] = {};
+    if (there) {
+      R = A.rows[row];
+      const float* const from = A.logits + row * A.ld_logits + v;
+      x[0] = *reinterpret_cast<const ce_f32x4*>(from);
+      x[1] = *reinterpret_cast<const ce_f32x4*>(from + 4);
+    }
+    uint32_t h[8][3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ce_share<THREE>(R, x[e / 4][e % 4], v + e == R.token - A.v0, there && v + e < A.n_p, h[e]);
+#pragma unroll
+    for (int s = 0; s < (THREE ? 3 : 1); ++s)
+      *reinterpret_cast<uint4*>(A.dl + s * A.dl_plane + row * A.ld_dl + v) =
+          make_uint4(h[0][s] | h[1][s] << 16, h[2][s] | h[3][s] << 16, h[4][s] | h[5][s] << 16, h[6][s] | h[7][s] << 16);
   }
 }
 
