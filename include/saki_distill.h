@@ -6,7 +6,7 @@
  *   2. saki_distill_top: the divergence between a student's row and such a list, and its
  *      gradient with respect to the student's logits.
  *   3. saki_linear_ce: cross entropy of softmax(hidden weight^T) at a token of each row and the
- *      gradients of hidden and weight; the logits are never in memory as a whole.
+ *      gradients of hidden and weight, in a workspace that does not grow with rows x vocab.
  *
  * Memory, streams, layout of logit rows, alignment and errors are those of saki.h: arrays are
  * the caller's device memory, calls only enqueue on `stream`, may be captured into a graph, and
@@ -135,15 +135,16 @@ typedef struct {
   int64_t grad_weight_stride;
 } saki_ce_args;
 
-/* Cross entropy from hidden states.  The logits exist a tile at a time in registers (for the
- * loss) and a piece of the vocabulary at a time in the workspace, as the gradient of the piece's
- * logits (for the gradients).
+/* Cross entropy from hidden states.  The logits exist a tile at a time in registers; with gradients, those of calls
+ * of at most 1 GiB of them (n_rows vocab 4 bytes) are kept in the workspace in between, others are computed a second
+ * time, a piece of the vocabulary at a time.
  *   ws   ws_bytes >= saki_linear_ce_workspace_bytes(head, grads), 256-byte aligned
  * Rows of valid_mask 0 are not read: loss, logp_token and grad_hidden are 0 there, and they add
  * nothing to grad_weight, whatever they hold.  A token outside [0, vocab) or a row_weight that
  * is not finite gives the row NaN in its outputs and grad_hidden and SAKI_ROW_BAD_TARGET, and it
  * adds nothing to grad_weight.  A row whose logits' log-sum-exp is not finite gets NaN
  * and SAKI_ROW_NONFINITE, and makes grad_weight NaN.
+ * f32 elements of at least 2^128 (1 - 2^-9), about 3.396e38, count as infinite.
  * Rounding: products in 32 bits of bf16 or f32 elements; for the gradients row_weight (p - 1[..])
  * is rounded once to the inputs' type (f32: to 24 bits).  n_rows < 2^31 / 256, and rows of hidden and weight
  * below 2^22 elements apart. */

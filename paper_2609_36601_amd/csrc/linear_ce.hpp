@@ -3,9 +3,12 @@
 // With logits L = X W^T (X [n, D], W [V, D]), log-sum-exp lse_r and target y_r of row r, weight w_r:
 //   loss_r = -w_r (L[r, y_r] - lse_r),   dL[r, v] = w_r (exp(L[r, v] - lse_r) - [v = y_r]),
 //   dX = dL W,   dW = dL^T X.
-// Four products, 8 n V D operations where 6 would do with L kept: L is computed for the loss, whose
-// epilogue keeps a maximum and a sum for each row and LSE_P tokens, and again, a piece of the
-// vocabulary at a time, for dL, which is a bf16 array of the piece that both gradients read.
+// Four products, 8 n V D operations: L is computed for the loss, whose epilogue keeps a maximum and a sum for each row
+// and wave, and again, a piece of the vocabulary at a time, for dL, which is a bf16 array of the piece that both
+// gradients read.  Where L fits into the workspace (KEEP_BYTES) it is kept instead, and there are three, 6 n V D.
+// What bounds them: with many rows the matrix pipes at the clock that the power allows (8,192 x 151,936 x 4,096: 7.2 to
+// 7.5 ms for L, 1,360 to 1,420 TFLOP/s, where a large library product reaches 1,435); with few the reading of W (8 rows of
+// 1,024 x 32,000: 23 us with the launch).
 //
 // One kernel does all four (ce_gemm_kernel), C[p, q] = sum_k P(p, k) Q(q, k):
 //   CE_LSE  P = W   (tokens; k contiguous)   Q = X   (rows; k contiguous)    epilogue: maximum and sum over p

@@ -94,6 +94,14 @@ def test_sizes(saki_lib, n, V, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,D", [(128, 700, 264), (129, 700, 8), (768, 300, 328), (769, 300, 328), (769, 300, 16), (3, 2, 1024)])
+def test_the_forms_of_a_call(saki_lib, n, V, D, dtype):
+    """Both sides of: f32 weights as they are or in parts, logits kept or computed again, the rows of grad_weight's sums in splits."""
+    rng = np.random.default_rng(n + D)
+    check(*problem(n, V, D, rng), dtype, valid=rng.random(n) < 0.7)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_the_large_tiles(saki_lib, dtype):
     """Sizes of which the products fill the card with their largest tiles, none of them whole."""
     rng = np.random.default_rng(3)
