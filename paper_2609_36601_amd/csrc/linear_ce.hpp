@@ -247,6 +247,18 @@ __device__ __forceinline__ void ce_share(const CeRow& R, float logit, bool hot, 
   else h[0] = f32_to_bf16_bits(x);
 }
 
+__device__ __forceinline__ uint2 ce_bits(ce_f32x4 x) {
+  return make_uint2(f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16, f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16);
+}
+// Two lanes with 4 entries each of two runs of 16 exchange halves: 8 entries of one run each, `at` from the lane's place in the first.
+__device__ __forceinline__ uint4 ce_pair(uint2 a, uint2 b, int lane, int* at) {
+  const bool odd = (lane & 16) != 0;
+  const uint2 give = odd ? a : b;
+  const uint2 got = make_uint2(__shfl_xor(give.x, 16), __shfl_xor(give.y, 16));
+  *at = odd ? 12 : 0;
+  return odd ? make_uint4(got.x, got.y, b.x, b.y) : make_uint4(a.x, a.y, got.x, got.y);
+}
+
 // What a wave does with its products: entry (p, q) of acc[i][j][e] is p = pw + 16 i + e, q = qw + 16 j.
 template <int KIND, typename TILE, bool THREE>
 __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE::TP][TILE::TQ], int p_tile, int pw, int qw, int wp,
@@ -335,6 +347,18 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
       const int64_t v = qw + 16 * j;
+      if constexpr (!THREE && TP % 2 == 0) {
+        if (!A.sums) {
+#pragma unroll
+          for (int i = 0; i < TP; i += 2) {
+            int at;
+            const uint4 w = ce_pair(ce_bits(acc[i][j] * A.scale), ce_bits(acc[i + 1][j] * A.scale), lane, &at);
+            if (v < n_q && pw + 16 * i + at < A.n_p)
+              *reinterpret_cast<uint4*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i + at) = w;
+          }
+          continue;
+        }
+      }
 #pragma unroll
       for (int i = 0; i < TP; ++i) {
         if (v >= n_q || pw + 16 * i >= A.n_p) continue;
@@ -346,9 +370,7 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
         if constexpr (THREE) {
           *reinterpret_cast<ce_f32x4*>(static_cast<float*>(A.grad) + v * A.ld_grad + pw + 16 * i) = x;
         } else {
-          const uint2 w = make_uint2(f32_to_bf16_bits(x[0]) | f32_to_bf16_bits(x[1]) << 16,
-                                     f32_to_bf16_bits(x[2]) | f32_to_bf16_bits(x[3]) << 16);
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i) = w;
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.grad) + v * A.ld_grad + pw + 16 * i) = ce_bits(x);
         }
       }
     }
