@@ -6,7 +6,7 @@
  *   2. saki_distill_top: the divergence between a student's row and such a list, and its
  *      gradient with respect to the student's logits.
  *   3. saki_linear_ce: cross entropy of softmax(hidden weight^T) at a token of each row and the
- *      gradients of hidden and weight, in a workspace that does not grow with rows x vocab.
+ *      gradients of hidden and weight, without logits for every row and token in memory.
  *
  * Memory, streams, layout of logit rows, alignment and errors are those of saki.h: arrays are
  * the caller's device memory, calls only enqueue on `stream`, may be captured into a graph, and
@@ -142,7 +142,7 @@ typedef struct {
  * Rows of valid_mask 0 are not read: loss, logp_token and grad_hidden are 0 there, and they add
  * nothing to grad_weight, whatever they hold.  A token outside [0, vocab) or a row_weight that
  * is not finite gives the row NaN in its outputs and grad_hidden and SAKI_ROW_BAD_TARGET, and it
- * adds nothing to grad_weight.  A row whose logits' log-sum-exp is not finite gets NaN
+ * adds nothing to grad_weight if its hidden state is finite.  A row whose logits' log-sum-exp is not finite gets NaN
  * and SAKI_ROW_NONFINITE, and makes grad_weight NaN.
  * f32 elements of at least 2^128 (1 - 2^-9), about 3.396e38, count as infinite.
  * Rounding: products in 32 bits of bf16 or f32 elements; for the gradients row_weight (p - 1[..])

@@ -312,9 +312,9 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
       const int row = qw + 16 * j;
-      const bool there = row < n_q;
       CeRow R = {0.0f, 0.0f, 0.0f, -1};
-      if (there) R = A.rows[row];
+      if (row < n_q) R = A.rows[row];
+      const bool there = R.token >= 0;  // (a row without a token adds nothing, whatever its logits are)
       const int hot = R.token - A.v0;
 #pragma unroll
       for (int i = 0; i < TP; ++i) {
@@ -722,11 +722,11 @@ __global__ __launch_bounds__(256) void ce_share_kernel(CeGemm A) {
   const int v = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (v >= (A.n_p + CE_BK - 1) / CE_BK * CE_BK) return;
   for (int row = blockIdx.y; row < (rows + CE_BK - 1) / CE_BK * CE_BK; row += gridDim.y) {
-    const bool there = row < rows;
     CeRow R = {0.0f, 0.0f, 0.0f, -1};
     ce_f32x4 x[2] = {};
+    if (row < rows) R = A.rows[row];
+    const bool there = R.token >= 0;
     if (there) {
-      R = A.rows[row];
       const float* const from = A.logits + row * A.ld_logits + v;
       x[0] = *reinterpret_cast<const ce_f32x4*>(from);
       x[1] = *reinterpret_cast<const ce_f32x4*>(from + 4);

@@ -171,6 +171,32 @@ def test_a_row_that_is_not_finite(saki_lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,D", [(8, 512), (70, 64), (800, 24)])
+def test_rows_of_no_use_among_others(saki_lib, n, D, dtype):
+    """Logits kept and computed again: a row without a token adds nothing though its logits are infinite; a row that is not
+    finite leaves the other rows' outputs alone."""
+    rng = np.random.default_rng(13)
+    x, w, token = problem(n, 300, D, rng)
+    x[3] = 3e38 * np.sign(w[7])
+    token[3] = -1
+    xd, wd, td = matrix(x, dtype), matrix(w, dtype), torch.as_tensor(token, device=DEV).int()
+    out = saki_lib.linear_ce(xd, wd, td)
+    x[3] = 0
+    plain = saki_lib.linear_ce(matrix(x, dtype), wd, td)
+    xd[5, 3] = float("nan")
+    td[3] = 2
+    none = saki_lib.linear_ce(xd, wd, td)
+    torch.cuda.synchronize()
+    assert out["row_status"].tolist() == [4 if r == 3 else 0 for r in range(n)]
+    assert bool(out["grad_weight"].isfinite().all()) and torch.equal(out["grad_weight"], plain["grad_weight"])
+    assert bool(out["grad_hidden"][3].isnan().all())
+    others = [r for r in range(n) if r not in (3, 5)]
+    assert torch.equal(out["grad_hidden"][others], plain["grad_hidden"][others])
+    assert none["row_status"].tolist() == [1 if r in (3, 5) else 0 for r in range(n)]
+    assert torch.equal(none["grad_hidden"][others], out["grad_hidden"][others]) and torch.equal(none["row_loss"][others], out["row_loss"][others])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_logits_of_all_sizes(saki_lib, dtype):
     """Rows that are certain (log p near 0), rows whose logits are near 1e30, rows of logits that are all alike."""
     rng = np.random.default_rng(11)
