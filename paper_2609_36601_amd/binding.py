@@ -685,6 +685,9 @@ def saki_top_logits(logits, k, top_logit, top_token, rest_logit=None, row_status
 
 def top_logits(logits, k, temperature=1.0, stream=None):
     """The k largest logits of each row and the others' log-sum-exp; allocates its outputs and workspace."""
+    if stream is not None:  # what is allocated here is that stream's
+        with torch.cuda.stream(stream):
+            return top_logits(logits, k, temperature)
     n, V = logits.shape
     dev = logits.device
     out = dict(top_logit=torch.empty(n, k, dtype=torch.float32, device=dev),
@@ -729,6 +732,10 @@ def saki_distill_top(student, top_token, top_logit, rest_logit=None, temperature
 def distill_top(student, top_token, top_logit, rest_logit=None, temperature=1.0, direction=SAKI_KL_FORWARD, valid_mask=None,
                 grad_scale=1.0, grad_dtype=torch.float32, stream=None):
     """Divergence from a teacher's top logits and its gradient (grad_dtype None: none); allocates its outputs."""
+    if stream is not None:  # what is allocated here is that stream's
+        with torch.cuda.stream(stream):
+            return distill_top(student, top_token, top_logit, rest_logit, temperature, direction, valid_mask, grad_scale,
+                               grad_dtype)
     n, V = student.shape
     dev = student.device
     out = dict(row_loss=torch.empty(n, dtype=torch.float32, device=dev),
@@ -782,6 +789,9 @@ def saki_linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad
 
 def linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad_scale=1.0, train=True, stream=None):
     """Cross entropy from hidden states and (train) the gradients of hidden and weight; allocates its outputs."""
+    if stream is not None:  # what is allocated here is that stream's
+        with torch.cuda.stream(stream):
+            return linear_ce(hidden, weight, token, row_weight, valid_mask, grad_scale, train)
     n, dev = hidden.shape[0], hidden.device
     out = dict(row_loss=torch.empty(n, dtype=torch.float32, device=dev),
                logp_token=torch.empty(n, dtype=torch.float32, device=dev),

@@ -182,7 +182,7 @@ constexpr int64_t MOST_ROWS = (int64_t{1} << 31) / 256;
 // last-level cache holds, at most (its pieces cost each product a start and an end).
 constexpr int64_t PIECE_BYTES = int64_t{256} << 20;
 // Bytes of logits that a training call keeps, at most; above it, it computes them a second time, in pieces.  Loss and gradients
-// in microseconds, kept / again (bf16; 1,024 rows of 4,096 in f32):
+// in microseconds, kept / again (bf16 but for the one in f32):
 //   rows             16         64         200          400          1,024
 //   32,000 x 512     49/53      54/57      77/79        111/115      169/177
 //   50,000 x 2,048   189/222    204/234    293/329      408/474      719/848

@@ -7,8 +7,8 @@
 // and wave, and again, a piece of the vocabulary at a time, for dL, which is a bf16 array of the piece that both
 // gradients read.  Where L fits into the workspace (KEEP_BYTES) it is kept instead, and there are three, 6 n V D.
 // What bounds them: with many rows the matrix pipes at the clock that the power allows (8,192 x 151,936 x 4,096: 7.2 to
-// 7.5 ms for L, 1,360 to 1,420 TFLOP/s, where a large library product reaches 1,435); with few the reading of W (8 rows of
-// 1,024 x 32,000: 23 us with the launch).
+// 7.8 ms for L, 1,310 to 1,420 TFLOP/s, where a library product of this size reaches 1,435 to 1,509); with few the reading of
+// W (8 rows of 2,048, 32,000 tokens, 131 MB: 23 us with the launch).
 //
 // One kernel does all four (ce_gemm_kernel), C[p, q] = sum_k P(p, k) Q(q, k):
 //   CE_LSE  P = W   (tokens; k contiguous)   Q = X   (rows; k contiguous)    epilogue: maximum and sum over p
@@ -537,7 +537,8 @@ __global__ __launch_bounds__(TILE::NT, TILE::PER_SIMD) void ce_gemm_kernel(CeGem
 
 // Few rows in 32 bits: memory bounds them, so the weight (P) is read as it is and taken apart where its fragments are
 // read from LDS, 44 instructions for 8 numbers, instead of being written as three parts and read six times.  Q lies in
-// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.8 ms.  Each workgroup takes the weight
+// three parts as above.  120 rows of 3,888, 106,276 tokens, loss and gradients: 9.1 -> 2.8 ms (2.2 with
+// the logits kept).  Each workgroup takes the weight
 // apart for 64 rows, so many rows go the other way (DIRECT_ROWS).
 struct CeSplit {
   ce_bf16x8 part[3];

@@ -89,3 +89,29 @@ def test_two_calls_at_once(saki_lib):
                 step()
     torch.cuda.synchronize()
     assert _same(a[1], want[0]) and _same(b[1], want[1])
+
+
+def test_calls_on_another_stream(saki_lib):
+    """Outputs and workspaces of a call belong to its stream: allocations of the current one do not touch them while it runs."""
+    torch.manual_seed(3)
+    n, V, D = 300, 20001, 256
+    logits = saki_lib.alloc_rows(n, V, torch.bfloat16, DEV)
+    logits.copy_(3 * torch.randn(n, V, device=DEV))
+    x, w = torch.randn(n, D, device=DEV).bfloat16(), (torch.randn(V, D, device=DEV) / 16).bfloat16()
+    token = torch.randint(0, V, (n,), dtype=torch.int32, device=DEV)
+    top = saki_lib.top_logits(logits, 20)
+    calls = [lambda **k: saki_lib.top_logits(logits, 20, **k), lambda **k: saki_lib.top_logits(logits[:3], 20, **k),
+             lambda **k: saki_lib.distill_top(logits, top["top_token"], top["top_logit"], top["rest_logit"], **k),
+             lambda **k: saki_lib.linear_ce(x, w, token, **k)]
+    want = [c() for c in calls]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        got = []
+        for c in calls:
+            got.append(c(stream=side))
+            [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for size in (1 << 12, 1 << 20, 1 << 24, 1 << 27)]
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            for key in a:
+                assert torch.equal(a[key].view(torch.uint8), b[key].view(torch.uint8)) if a[key].is_contiguous() else torch.equal(a[key], b[key]), key
