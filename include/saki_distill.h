@@ -12,8 +12,9 @@
  * the caller's device memory, calls only enqueue on `stream`, may be captured into a graph, and
  * allocate nothing; workspaces have any contents before and after a call, and calls that may run
  * at the same time need separate ones.  Results do not depend on how rows are split into
- * calls (saki_linear_ce's grad_weight, a sum over the rows of a call, apart) and are the same
- * bits for the same call.  n_rows == 0: sums over the rows (loss_sum, grad_weight) are 0,
+ * calls and are the same bits for the same call, apart from saki_linear_ce's grad_weight, which is a sum over the
+ * rows of a call, and from the order of 32-bit sums: how many rows a call has decides how its products are split, and
+ * how long rows of few are read (rest_logit).  n_rows == 0: sums over the rows (loss_sum, grad_weight) are 0,
  * nothing else is written.
  */
 #ifndef SAKI_DISTILL_H

@@ -29,13 +29,22 @@ saki_status check_logits(const void* x, int32_t dtype, int64_t n_rows, int64_t v
 
 float log2_scale(float temperature) { return static_cast<float>(1.4426950408889634074 / static_cast<double>(temperature)); }
 
-// Parts of a row: one where the rows alone fill the card; otherwise so many that about TOP_ITEMS
-// workgroups run, of at least TOP_PART_CHUNKS chunks each.
-constexpr int64_t TOP_ITEMS = 1024, TOP_PART_CHUNKS = 8, TOP_MOST_PARTS = 64;
+// Parts of a row: several, of at least TOP_PART_CHUNKS chunks, where rows are longer than TOP_LONG and so few that two parts of
+// each leave CUs idle: about TOP_ITEMS workgroups.  The second launch, which joins them, costs what shorter rows would gain.
+// Microseconds whole / in parts, bf16:
+//   rows            1            16           64           128          255
+//   65,536          17.0/19.8    18.5/20.0    19.4/21.0    19.6/21.5    19.8/26.7
+//   98,304          22.0/22.8    22.4/23.1    22.7/21.7    23.8/22.5    25.4/29.0
+//   151,936         27.8/25.0    32.4/27.1    32.7/23.2    37.4/27.4    36.7/34.2
+//   262,144         36.1/31.4    42.5/33.5    43.6/26.1    50.0/31.1    49.6/42.4
+// (up to 64 parts; 8 at most, which the second launch joins sooner: 151,936, 1 / 16 rows 24.5 / 27.1 -> 20.2 / 20.8, 262,144
+// 27.3 / 33.4 -> 23.0 / 23.8, 1,000,000 35.7 / 38.7 -> 32.2 / 38.6)
+constexpr int64_t TOP_ITEMS = 512, TOP_LONG = 98304, TOP_PART_CHUNKS = 8, TOP_MOST_PARTS = 8;
 int64_t top_parts(int64_t n_rows, int64_t vocab) {
   const int64_t chunks = (vocab + SAKI_CHUNK - 1) / SAKI_CHUNK;
+  if (n_rows < 1 || n_rows >= TOP_ITEMS / 2 || vocab <= TOP_LONG) return 1;
   const int64_t want = std::min({(TOP_ITEMS + n_rows - 1) / n_rows, chunks / TOP_PART_CHUNKS, TOP_MOST_PARTS});
-  return n_rows > TOP_ITEMS / 2 || want < 2 ? 1 : want;
+  return want < 2 ? 1 : want;
 }
 
 // Workgroups of distill_kernel: of 512 threads, two a CU, where a row is long (read and written, over

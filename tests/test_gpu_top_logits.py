@@ -135,3 +135,33 @@ def test_many_rows_in_one_call_and_split(saki_lib):
         assert torch.equal(whole[f], torch.cat([p[f] for p in parts]))
     # (few rows are read in parts, whose sums are added in another order)
     assert torch.allclose(whole["rest_logit"], torch.cat([p["rest_logit"] for p in parts]), rtol=2.0**-20, atol=2.0**-20)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V,k", [(1, 98305, 1), (3, 110003, 256), (40, 98304, 20), (40, 98311, 20), (255, 100001, 7), (256, 100001, 7),
+                                   (1, 600001, 64)])
+def test_long_rows_in_few_and_many(saki_lib, n, V, k, dtype):
+    """Both sides of what is read in parts."""
+    rng = np.random.default_rng(n + V + k)
+    check(rows(rng.normal(size=(n, V)) * 3, dtype), k, 1.3)
+
+
+@pytest.mark.parametrize("kind", ["equal", "two_values", "rising", "falling", "blocks", "peak", "sampled", "sampled_ties"])
+def test_orders_and_ties_of_long_rows(saki_lib, kind):
+    V = 120011
+    i = np.arange(V)
+    x = {"equal": np.full(V, 2.5), "two_values": (i % 3 == 0) * 1.0, "rising": i * 0.0625, "falling": -i * 0.0625,
+         "blocks": np.floor(i / 700) % 5, "peak": np.where(i == 75000, 30.0, 0.0),
+         "sampled": np.where((i % 16384 < 512) & (i % 8 == 0), 5.0 + i / 4096, i * -0.001),
+         "sampled_ties": np.where((i % 16384 < 512) & (i % 8 == 0), 5.0, (i % 11) * 0.25)}[kind]
+    for dtype in (torch.bfloat16, torch.float32):
+        check(rows(np.tile(x, (2, 1)), dtype), 90)
+
+
+def test_long_rows_far_below_the_list(saki_lib):
+    test_a_rest_far_below_the_list(saki_lib, 120000, 200)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_long_rows_that_are_not_finite(saki_lib, bad):
+    test_rows_that_are_not_finite(saki_lib, 120000, bad)
