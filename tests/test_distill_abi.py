@@ -39,8 +39,8 @@ def top(lib, **kw):
     (SHAPE, dict(k=8, V=7)), (SHAPE, dict(top_stride=7)), (VALUE, dict(tau=0.0)), (VALUE, dict(tau=-1.0)),
     (VALUE, dict(tau=float("nan"))), (VALUE, dict(tau=float("inf"))), (VALUE, dict(tau=2.0**-65)), (NULLPTR, dict(logits=None)),
     (NULLPTR, dict(top_logit=None)), (NULLPTR, dict(top_token=None)), (ALIGN, dict(logits=264)), (ALIGN, dict(stride=1004)),
-    (ALIGN, dict(top_logit=258)), (ALIGN, dict(rest=258)), (WORKSPACE, dict(V=50000, stride=50000)),
-    (WORKSPACE, dict(V=50000, stride=50000, ws=256, ws_bytes=100)), (ALIGN, dict(V=50000, stride=50000, ws=264, ws_bytes=1 << 30)),
+    (ALIGN, dict(top_logit=258)), (ALIGN, dict(rest=258)), (WORKSPACE, dict(V=120000, stride=120000)),
+    (WORKSPACE, dict(V=120000, stride=120000, ws=256, ws_bytes=100)), (ALIGN, dict(V=120000, stride=120000, ws=264, ws_bytes=1 << 30)),
     (OK, dict(n=0, logits=None, top_logit=None, top_token=None))])
 def test_top_logits(lib, code, kw):
     assert top(lib, **kw) == code
