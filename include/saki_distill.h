@@ -147,7 +147,8 @@ typedef struct {
  * and SAKI_ROW_NONFINITE, and makes grad_weight NaN.
  * f32 elements of at least 2^128 (1 - 2^-9), about 3.396e38, count as infinite.
  * Rounding: products in 32 bits of bf16 or f32 elements; for the gradients row_weight (p - 1[..])
- * is rounded once to the inputs' type (f32: to 24 bits).  n_rows < 2^31 / 256, and rows of hidden and weight
+ * is rounded once to the inputs' type (f32: to 24 bits).  Where p_r(token[r]) is near 1, log p and p - 1 come from
+ * the other tokens' sum: their errors are relative to themselves, beside what the logits' rounding makes.  n_rows < 2^31 / 256, and rows of hidden and weight
  * below 2^22 elements apart. */
 saki_status saki_linear_ce(const saki_head *head, const saki_ce_args *args, void *ws,
                            size_t ws_bytes, saki_stream_t stream);

@@ -92,7 +92,9 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRows P) {
   if (threadIdx.x == 0) *P.count = base;
 }
 
-// A workgroup a row that takes part: its log-sum-exp from the tiles' maxima and sums, and the row's outputs.  What bounds it: latency; every thread has four of its row's loads under way.
+// A workgroup a row that takes part: its log-sum-exp from the tiles' maxima and sums, and the row's outputs.  With u the other
+// tokens' sum relative to the token's exponential, log p = -log(1 + u) and 1 - p = u / (1 + u): both relatively exact where u is
+// small.  What bounds it: latency; every thread has four of its row's loads under way.
 __global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
   constexpr int DEEP = 4;
   __shared__ float part_m[4];
@@ -137,15 +139,18 @@ __global__ __launch_bounds__(256) void ce_loss_kernel(CeRows P) {
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) sum += part_m[w] == -finf() ? part_s[w] : part_s[w] * static_cast<double>(fexp2(part_m[w] - m));
-  // (a row of -infinity alone: m and so the result)
-  const double lse2 = static_cast<double>(m) + log2(sum);
-  const double logp = (static_cast<double>(target) - lse2) / static_cast<double>(LOG2E);
+  // (a row of -infinity alone: m and so the result; a token's logit that is not finite: NaN, or log p)
+  const double own = good ? exp2(static_cast<double>(target) - static_cast<double>(m)) : 0.0, all = own + sum;
+  const double lse2 = static_cast<double>(m) + log2(all);
+  const double logp = own >= 0.25 ? -log1p(sum / own) / (LN2_D * static_cast<double>(LOG2E))
+                                  : (static_cast<double>(target) - lse2) / static_cast<double>(LOG2E);
   const bool finite = isfinite(lse2) && (!good || isfinite(logp));
   CeRow R;
   R.lse_hi = finite ? static_cast<float>(lse2) : nanf_();
   R.lse_lo = finite ? static_cast<float>(lse2 - static_cast<double>(R.lse_hi)) : nanf_();
   R.weight = good ? weight : 0.0f;
   R.token = good ? token : -1;
+  R.rest = finite ? static_cast<float>(sum / all) : nanf_();
   P.rows[i] = R;
   const bool ok = good && finite;
   const double loss = ok ? -static_cast<double>(weight) * logp : __builtin_nan("");

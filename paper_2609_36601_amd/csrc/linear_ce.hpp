@@ -46,6 +46,7 @@ struct CeRow {
   float lse_hi, lse_lo;  // log-sum-exp / ln 2, in two floats
   float weight;
   int token;
+  float rest;            // 1 - p at the token, from the other tokens' sum
 };
 
 struct CeGemm {
@@ -59,7 +60,7 @@ struct CeGemm {
   int p_tiles, q_tiles;
   int k_split;                 // CE_DX, CE_DW: tiles of k of a split
   // CE_LSE
-  float2* stats;               // [rows, slots] maximum and sum in units of log2
+  float2* stats;               // [rows, slots] maximum in units of log2, and sum without the row's token
   int slots, slot0;
   const int32_t* token;        // the call's; of the rows that take part, source[row] where there is a count
   const int* source;
@@ -237,11 +238,20 @@ __device__ __forceinline__ void ce_place(const CeGemm& A, int* p_tile, int* q_ti
   *q_tile = c0 + in % wide;
 }
 
-// A logit's gradient, as the products take it.
+// A logit in units of log2: rounded, so that a difference of two is that of the numbers the sum is made of.
+__device__ __forceinline__ float ce_log2(float logit) {
+#pragma clang fp contract(off)
+  return logit * LOG2E;
+}
+
+// A logit's gradient, as the products take it: the row's weight times p, and at the token p - 1, which is not taken from p: of a
+// row that is certain of its token the difference would be rounding alone (1,000 tokens, 1 - p = 5e-7: off by 150%, 30% of
+// the rows with the wrong sign).  bf16 heads round it to bf16, by 2^-8 of itself at most, since both products that
+// read it multiply bf16 numbers; two parts would make them twice as long.  It shows in the gradients' distance from 64 bits: 1.84e-3 of
+// their size instead of the 1.65e-3 that the rounding of the result alone makes (8,192 x 4,096 x 151,936).
 template <bool THREE>
 __device__ __forceinline__ void ce_share(const CeRow& R, float logit, bool hot, bool there, uint32_t (&h)[3]) {
-  float x = fexp2(__builtin_fmaf(logit, LOG2E, -R.lse_hi) - R.lse_lo);
-  x = R.weight * (hot ? x - 1.0f : x);
+  float x = R.weight * (hot ? -R.rest : fexp2((ce_log2(logit) - R.lse_hi) - R.lse_lo));
   if (!there) x = 0.0f;
   if constexpr (THREE) ce_parts(x, h);
   else h[0] = f32_to_bf16_bits(x);
@@ -278,11 +288,11 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
       for (int i = 0; i < TP; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          acc[i][j][e] = pw + 16 * i + e < A.n_p ? acc[i][j][e] * LOG2E : -finf();
+          acc[i][j][e] = pw + 16 * i + e < A.n_p ? ce_log2(acc[i][j][e]) : -finf();
           m = fmaxf(m, acc[i][j][e]);
         }
-      // The token's logit: the very number that the sum has, so that a row which is certain of its token has a log-probability as
-      // exact as its other logits' shares.
+      // The token's logit, which the sum leaves out: a row that is certain of its token has a log-probability and a gradient
+      // of the size of what the others have, which in a sum with the token's 1 would be rounded at 2^-24.
       int at = -1;  // place of the token among this lane's 4 TP, if it is there
       if (row < n_q) {
         const int v = A.token[A.count ? A.source[row] : row] - A.v0 - pw;
@@ -303,6 +313,12 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
       for (int i = 0; i < TP; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s += fexp2(acc[i][j][e] - ref);
+      // (the token's term left out afterwards, where there is one: left out above, it costs every tile 2% of L's time)
+      if (__ballot(at >= 0) != 0ull) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TP * 4; ++i) s += at == i ? 0.0f : fexp2(acc[i / 4][j][i % 4] - ref);
+      }
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
       if (lane < 16 && row < n_q)
@@ -312,7 +328,7 @@ __device__ __forceinline__ void ce_finish(const CeGemm& A, ce_f32x4 (&acc)[TILE:
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
       const int row = qw + 16 * j;
-      CeRow R = {0.0f, 0.0f, 0.0f, -1};
+      CeRow R = {0.0f, 0.0f, 0.0f, -1, 0.0f};
       if (row < n_q) R = A.rows[row];
       const bool there = R.token >= 0;  // (a row without a token adds nothing, whatever its logits are)
       const int hot = R.token - A.v0;
@@ -723,7 +739,7 @@ __global__ __launch_bounds__(256) void ce_share_kernel(CeGemm A) {
   const int v = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (v >= (A.n_p + CE_BK - 1) / CE_BK * CE_BK) return;
   for (int row = blockIdx.y; row < (rows + CE_BK - 1) / CE_BK * CE_BK; row += gridDim.y) {
-    CeRow R = {0.0f, 0.0f, 0.0f, -1};
+    CeRow R = {0.0f, 0.0f, 0.0f, -1, 0.0f};
     ce_f32x4 x[2] = {};
     if (row < rows) R = A.rows[row];
     const bool there = R.token >= 0;
