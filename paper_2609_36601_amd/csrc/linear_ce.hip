@@ -10,6 +10,8 @@ template <int KIND, typename TILE>
 static hipError_t launch_tile(CeGemm A, bool three, int splits, hipStream_t st) {
   A.p_tiles = (A.n_p + TILE::PT - 1) / TILE::PT;
   A.q_tiles = (A.n_q + TILE::QT - 1) / TILE::QT;
+  // (a launch of more threads is cut off without an error; see Plan::s_step)
+  if (static_cast<int64_t>(A.p_tiles) * A.q_tiles * splits * TILE::NT > CE_MOST_THREADS) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<unsigned>(A.p_tiles * A.q_tiles * splits)), block(TILE::NT);
   if constexpr (std::is_same_v<TILE, CeFew> && (KIND == CE_LSE || KIND == CE_DL)) {  // (f32: ce_direct_kernel)
     if (three) return hipErrorInvalidValue;
@@ -256,6 +258,7 @@ struct Plan {
   int64_t rows;              // n, padded to tiles
   int planes;
   int64_t slots, wave_p, piece, pieces;     // wave_p: tokens of a slot
+  int64_t s_step;            // tokens of a launch of the loss's product, at most: its threads are fewer than 2^32
   int64_t splits, k_split, w_splits, w_split;  // of dX's and dW's k, and tiles of k of each
   bool direct;               // f32 weights as they are (ce_direct_kernel)
   int tile_s, tile_l, tile_x, tile_w;  // tiles of the products for the loss, for dL, dX and dW
@@ -288,6 +291,12 @@ Plan plan_of(const saki_head* h, bool dx, bool dw) {
   p.wave_p = tile_p / (p.tile_s == CE_LARGE ? CeLarge::WP : p.tile_s == CE_MIDDLE ? CeMiddle::WP : CeFew::WP);
   static_assert(CeDirect::PT == CeFew::PT && CeDirect::WP == CeFew::WP, "slots alike");
   p.slots = ceil_div(p.V, tile_p) * (tile_p / p.wave_p);
+  // The other products stay below it: dL's tiles by its piece's size, the gradients' by what memory holds of their sums.
+  const int64_t side_q = p.tile_s == CE_LARGE ? CeLarge::QT : p.tile_s == CE_MIDDLE ? CeMiddle::QT : CeFew::QT;
+  const int64_t column = ceil_div(p.n, side_q) * (p.tile_s == CE_LARGE ? CeLarge::NT : CeFew::NT);
+  static_assert(CeMiddle::NT == CeFew::NT && CeDirect::NT == CeFew::NT && CeDirect::QT == CeFew::QT, "threads alike");
+  static_assert(MOST_ROWS / CeLarge::QT * CeLarge::NT * (CE_PAD / CeLarge::PT) < CE_MOST_THREADS, "a launch takes CE_PAD tokens");
+  p.s_step = CE_MOST_THREADS / column * tile_p / CE_PAD * CE_PAD;
   // dX's k are the piece's tokens; dW's, where the piece is the whole vocabulary (which may be small), the rows
   const int64_t kt = p.piece / CE_BK;
   p.tile_x = p.direct ? CE_DIRECT : p.n <= CeFew::QT ? CE_FEW : CE_LARGE;
@@ -418,12 +427,16 @@ saki_status run(const saki_head* h, const saki_ce_args* a, const Plan& p, char* 
     st = abi_launched(weight(v0, nv), "ce_pack_kernel");
     if (st != SAKI_OK) return st;
     rows_q();
-    G.n_p = static_cast<int>(nv);
-    G.slot0 = static_cast<int>(v0 / p.wave_p);
-    G.v0 = static_cast<int>(v0);
-    G.logits = logits ? logits + v0 : nullptr;
-    st = abi_launched(launch_ce_part<CE_LSE>(G, p.tile_s, three, 1, hs), "ce_gemm_kernel");
-    if (st != SAKI_OK) return st;
+    for (int64_t u0 = v0; u0 < v0 + nv; u0 += p.s_step) {
+      CeGemm L = G;
+      L.p = static_cast<const char*>(G.p) + (u0 - v0) * G.ldp * (p.direct ? 4 : 2);
+      L.n_p = static_cast<int>(std::min(p.s_step, v0 + nv - u0));
+      L.slot0 = static_cast<int>(u0 / p.wave_p);
+      L.v0 = static_cast<int>(u0);
+      L.logits = logits ? logits + u0 : nullptr;
+      st = abi_launched(launch_ce_part<CE_LSE>(L, p.tile_s, three, 1, hs), "ce_gemm_kernel");
+      if (st != SAKI_OK) return st;
+    }
   }
   hipLaunchKernelGGL(ce_loss_kernel, dim3(static_cast<unsigned>(p.n)), dim3(256), 0, hs, R);
   SAKI_LAUNCHED("ce_loss_kernel");

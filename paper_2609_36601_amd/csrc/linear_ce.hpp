@@ -39,6 +39,7 @@ typedef __attribute__((address_space(3))) ce_s16x4 ce_lds_s16x4;
 enum CeKind { CE_LSE, CE_DL, CE_DX, CE_DW };
 
 constexpr int CE_BK = 64;   // k of a tile
+constexpr int64_t CE_MOST_THREADS = (int64_t{1} << 32) - 1;  // of a launch
 constexpr int CE_PAD = 256;  // rows and pieces of the vocabulary are padded to it: the largest tile
 
 // What a row's gradient is made of.
