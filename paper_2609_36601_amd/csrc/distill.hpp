@@ -66,13 +66,15 @@ struct DistillRow {
 // sum 2^((x - m) c) and smallest logit lo; wrong: the entry, or rest, cannot be used.  The bucket of the other tokens is
 // the entry behind the list's last.  Writes the row's outputs but the gradient; that of the listed tokens goes to sh.patch.
 // Logarithms in natural units, in 64 bits: a divergence near 0 is a difference of large ones.  Only the waves that hold
-// entries compute with them.
+// entries compute with them; which ones these are differs from workgroup to workgroup, so sums over the list are added in the
+// list's order: a row's bits do not depend on the workgroup that takes it.
 template <typename BLOCK>
 __device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParams& P, int64_t r, int slot, bool part, bool held,
                                                     bool wrong, int token, float s_tok, float logit, float rest, float m, double S,
                                                     float lo) {
   const double c64 = static_cast<double>(P.c) * LN2_D;
-  const bool lists = uniform(slot / WAVE * WAVE <= P.k), bucket = slot == P.k;
+  const int place = __builtin_amdgcn_readfirstlane(slot / WAVE);  // this wave's in the list
+  const bool lists = place * WAVE <= P.k, bucket = slot == P.k;
   float mm[3] = {m, held ? s_tok : -finf(), held && !wrong ? logit : -finf()};
   B.max(mm);
   const float mU = mm[0], mP = fmaxf(mm[1], mU), mT = fmaxf(mm[2], rest);
@@ -80,20 +82,20 @@ __device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParam
   const bool has_t = (held || bucket) && teach > -finf() && mT > -finf();
   double v[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, z = 0.0, y = 0.0, own_p = 0.0, own_t = 0.0;
   v[0] = S > 0.0 ? S * static_cast<double>(fexp2((m - mU) * P.c)) : S;
-  v[3] = wrong ? 1.0 : 0.0;
-  v[4] = (lo > -finf() && mU < finf() ? 0.0 : 1024.0) + (held ? 1.0 : 0.0);  // (fewer than 1,024 threads)
+  v[1] = wrong ? 1.0 : 0.0;
+  v[2] = (lo > -finf() && mU < finf() ? 0.0 : 1024.0) + (held ? 1.0 : 0.0);  // (fewer than 1,024 threads)
   if (lists) {
     z = (static_cast<double>(bucket ? mU : s_tok) - mP) * c64;
     y = (static_cast<double>(teach) - mT) * c64;
     own_p = held || bucket ? exp(z) : 0.0;
     own_t = has_t ? exp(y) : 0.0;
-    v[1] = bucket ? 0.0 : own_p;
-    v[2] = own_t;
-    v[5] = bucket ? own_p : 0.0;
+    v[3] = bucket ? own_p : 0.0;
+    v[4] = bucket ? 0.0 : own_p;
+    v[5] = own_t;
   }
-  B.sum(v);
+  B.template sum_placed<4>(v, place);
   const double SU = v[0];
-  const int n_held = static_cast<int>(v[4]) & 1023;
+  const int n_held = static_cast<int>(v[2]) & 1023;
   const bool some = mT > -finf(), others = n_held < P.V;
   double lt = 0.0, lp = 0.0, log_p = 0.0, p = 0.0, t = 0.0;
   // infinite divergences: forward, a share of the teacher's where the student has no token; reverse, the
@@ -101,7 +103,7 @@ __device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParam
   double l[2] = {0.0, 0.0};
   if (lists) {
     if (bucket) own_p = others ? own_p * SU : 0.0;
-    const double all_p = v[1] + (others ? v[5] * SU : 0.0), all_t = v[2];
+    const double all_p = v[4] + (others ? v[3] * SU : 0.0), all_t = v[5];
     const double log_t = log(all_t);
     log_p = log(all_p);
     lt = y - log_t;
@@ -118,11 +120,11 @@ __device__ __forceinline__ DistillRow distill_solve(BLOCK& B, const DistillParam
     }
     if (some && bucket && !others && !P.reverse) l[1] = rest > -finf() ? 1.0 : 0.0;
   }
-  B.sum(l);
+  B.template sum_placed<0>(l, place);
   if (lists) {
     double loss = l[0];
-    const bool bad = v[3] != 0.0 || l[1] != 0.0;
-    const bool finite = v[4] < 1024.0 && SU == SU && isfinite(log_p);
+    const bool bad = v[1] != 0.0 || l[1] != 0.0;
+    const bool finite = v[2] < 1024.0 && SU == SU && isfinite(log_p);
     const bool take = part && some && !bad && finite, nan = part && (bad || !finite);
     if (!take) loss = nan ? __builtin_nan("") : 0.0;
     const double scale = static_cast<double>(P.grad_scale) * P.inv_tau;

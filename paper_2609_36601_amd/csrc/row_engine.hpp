@@ -137,6 +137,30 @@ struct Block {
     __syncthreads();
   }
 
+  // As sum, with the numbers from FIRST on added in the order of the waves' `place`s (a permutation of them).
+  template <int FIRST, int N>
+  __device__ __forceinline__ void sum_placed(double (&v)[N], int place) {
+    static_assert(FIRST % 4 == 0 && N > FIRST && N <= RED_MAX && RED_MAX % 4 == 0, "block reduction wider than the LDS buffer");
+    if constexpr (FIRST > 0) {
+      double own[FIRST];
+#pragma unroll
+      for (int i = 0; i < FIRST; ++i) own[i] = v[i];
+      wave_sums_post(own, sh.red_d[wave], lane);
+    }
+    double placed[N - FIRST];
+#pragma unroll
+    for (int i = FIRST; i < N; ++i) placed[i - FIRST] = v[i];
+    wave_sums_post(placed, sh.red_d[place] + FIRST, lane);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      double acc = 0.0;
+      for (int w = 0; w < NW; ++w) acc += sh.red_d[w][i];
+      v[i] = acc;
+    }
+    __syncthreads();
+  }
+
   // Sums N doubles over the block for wave 0 alone (the other waves get
   // partial sums); a barrier must follow before the next reduction.
   template <int N>
