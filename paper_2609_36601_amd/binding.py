@@ -613,8 +613,16 @@ def saki_kv_attention(table, pool, layer, tokens, q, out, lse=None, scale=1.0, w
 # ---------------------------------------------------------------------------
 # A teacher's top logits, distillation from them, cross entropy from hidden states.
 # ---------------------------------------------------------------------------
+def _hold(stream, *tensors):
+    """What a call on `stream` reads or writes stays allocated until it has run, also if the caller lets go of it."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device == stream.device:
+            t.record_stream(stream)
+
+
 def _on(device, stream, **tensors):
-    """The arguments of one call lie on one device, the current one, and take no part in autograd."""
+    """The arguments of one call lie on one device, the current one, and take no part in autograd; those of a call on a
+    stream that is named are held for it."""
     for name, t in tensors.items():
         if t is None:
             continue
@@ -629,6 +637,8 @@ def _on(device, stream, **tensors):
         raise ValueError(f"a stream of {stream.device} for tensors on {device}")
     if torch.cuda.current_device() != device.index:
         raise ValueError(f"the call's tensors are on {device}, the current device is {torch.cuda.current_device()}")
+    if stream is not None:
+        _hold(stream, *tensors.values())
 
 
 def _typed(n, **tensors):
@@ -686,6 +696,7 @@ def saki_top_logits(logits, k, top_logit, top_token, rest_logit=None, row_status
 def top_logits(logits, k, temperature=1.0, stream=None):
     """The k largest logits of each row and the others' log-sum-exp; allocates its outputs and workspace."""
     if stream is not None:  # what is allocated here is that stream's
+        _hold(stream, logits)
         with torch.cuda.stream(stream):
             return top_logits(logits, k, temperature)
     n, V = logits.shape
@@ -733,6 +744,7 @@ def distill_top(student, top_token, top_logit, rest_logit=None, temperature=1.0,
                 grad_scale=1.0, grad_dtype=torch.float32, stream=None):
     """Divergence from a teacher's top logits and its gradient (grad_dtype None: none); allocates its outputs."""
     if stream is not None:  # what is allocated here is that stream's
+        _hold(stream, student, top_token, top_logit, rest_logit, valid_mask)
         with torch.cuda.stream(stream):
             return distill_top(student, top_token, top_logit, rest_logit, temperature, direction, valid_mask, grad_scale,
                                grad_dtype)
@@ -790,6 +802,7 @@ def saki_linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad
 def linear_ce(hidden, weight, token, row_weight=None, valid_mask=None, grad_scale=1.0, train=True, stream=None):
     """Cross entropy from hidden states and (train) the gradients of hidden and weight; allocates its outputs."""
     if stream is not None:  # what is allocated here is that stream's
+        _hold(stream, hidden, weight, token, row_weight, valid_mask)
         with torch.cuda.stream(stream):
             return linear_ce(hidden, weight, token, row_weight, valid_mask, grad_scale, train)
     n, dev = hidden.shape[0], hidden.device
