@@ -49,7 +49,8 @@ int64_t top_parts(int64_t n_rows, int64_t vocab) {
 
 // Workgroups of distill_kernel: of 512 threads, two a CU, where a row is long (read and written, over
 // DISTILL_LONG bytes): then few rows are under way at a time, and the last-level cache holds more of what the second sweep
-// reads again; else of 256, whose steps between the sweeps take less.  8,192 rows, microseconds of 512 / 256: bf16 of
+// reads again; else of 256, four a CU, whose steps between the sweeps take less (a fifth beside them: bf16 of 4,096 111.9 us
+// for 110.6, of 9,000 124.5 for 120.8, of 14,000 134.9 for 139.4; f32 alike).  8,192 rows, microseconds of 512 / 256: bf16 of
 // 32,000 329 / 259, of 100,000 716 / 726, f32 of 16,384 263 / 250, of 32,000 474 / 491, bf16 of 50,000 with a gradient in f32
 // (a third as many rows) 161 / 214.
 constexpr int64_t DISTILL_LONG = 224 << 10;
@@ -198,7 +199,7 @@ saki_status saki_distill_top(const void* student, int32_t dtype, int64_t n_rows,
   const bool bf16 = dtype == SAKI_BF16;
   const int64_t row_bytes = vocab * ((bf16 ? 2 : 4) + (!grad ? 0 : grad_dtype == SAKI_BF16 ? 2 : 4));
   const int threads = row_bytes <= DISTILL_LONG && list->k < 256 ? 256 : 512;  // (a thread for each token, and one for the others)
-  const int64_t slots = static_cast<int64_t>(cus) * (threads == 512 ? 2 : row_bytes <= DISTILL_LONG / 4 ? 5 : 4);
+  const int64_t slots = static_cast<int64_t>(cus) * (threads == 512 ? 2 : 4);
   const dim3 grid(static_cast<unsigned>(std::min(n_rows, slots)));
   if (n_rows > slots) {
     P.next_row = static_cast<unsigned int*>(ws);
