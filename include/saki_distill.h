@@ -11,7 +11,8 @@
  * Memory, streams, layout of logit rows, alignment and errors are those of saki.h: arrays are
  * the caller's device memory, calls only enqueue on `stream`, may be captured into a graph, and
  * allocate nothing; workspaces have any contents before and after a call, and calls that may run
- * at the same time need separate ones.  Results do not depend on how rows are split into
+ * at the same time need separate ones.  Their sizes are those of a call's own shapes: one of fewer rows may need more
+ * (rows that are read in parts, logits that are kept), so a workspace for several shapes is as large as the largest of them.  Results do not depend on how rows are split into
  * calls and are the same bits for the same call, apart from saki_linear_ce's grad_weight, which is a sum over the
  * rows of a call, and from the order of 32-bit sums: how many rows a call has decides how its products are split, and
  * how long rows of few are read (rest_logit).  n_rows == 0: sums over the rows (loss_sum, grad_weight) are 0,
@@ -144,7 +145,8 @@ typedef struct {
  * nothing to grad_weight, whatever they hold.  A token outside [0, vocab) or a row_weight that
  * is not finite gives the row NaN in its outputs and grad_hidden and SAKI_ROW_BAD_TARGET, and it
  * adds nothing to grad_weight if its hidden state is finite.  A row whose logits' log-sum-exp is not finite gets NaN
- * and SAKI_ROW_NONFINITE, and makes grad_weight NaN.
+ * and SAKI_ROW_NONFINITE, and makes grad_weight NaN.  An element of weight that is not finite may do so to every row,
+ * those whose logit there would be -infinity among them.
  * f32 elements of at least 2^128 (1 - 2^-9), about 3.396e38, count as infinite.
  * Rounding: products in 32 bits of bf16 or f32 elements; for the gradients row_weight (p - 1[..])
  * is rounded once to the inputs' type (f32: to 24 bits).  Where p_r(token[r]) is near 1, log p and p - 1 come from

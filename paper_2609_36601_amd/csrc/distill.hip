@@ -37,7 +37,12 @@ float log2_scale(float temperature) { return static_cast<float>(1.44269504088896
 //   98,304          22.0/22.8    22.4/23.1    22.7/21.7    23.8/22.5    25.4/29.0
 //   151,936         27.8/25.0    32.4/27.1    32.7/23.2    37.4/27.4    36.7/34.2
 //   262,144         36.1/31.4    42.5/33.5    43.6/26.1    50.0/31.1    49.6/42.4
-// (up to 64 parts; 8 at most, which the second launch joins sooner: 151,936, 1 / 16 rows 24.5 / 27.1 -> 20.2 / 20.8, 262,144
+// and f32, the rule's 8 parts at most:
+//   65,536          22.3/22.7    24.2/23.6    24.7/26.1    25.6/29.0    28.7/36.1
+//   98,304          24.8/24.7    27.8/25.7    28.3/28.4    32.9/32.5    33.1/42.3
+//   151,936         33.1/25.7    34.0/27.1    46.1/30.9    48.0/38.0    48.8/49.2
+//   262,144         44.3/27.5    53.7/30.4    64.1/36.1    63.5/46.4    68.0/66.6
+// (bf16 up to 64 parts; 8 at most, which the second launch joins sooner: 151,936, 1 / 16 rows 24.5 / 27.1 -> 20.2 / 20.8, 262,144
 // 27.3 / 33.4 -> 23.0 / 23.8, 1,000,000 35.7 / 38.7 -> 32.2 / 38.6)
 constexpr int64_t TOP_ITEMS = 512, TOP_LONG = 98304, TOP_PART_CHUNKS = 8, TOP_MOST_PARTS = 8;
 int64_t top_parts(int64_t n_rows, int64_t vocab) {

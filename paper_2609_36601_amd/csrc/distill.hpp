@@ -9,7 +9,7 @@
 // reference, hence neither p_R nor a gradient entry is a difference of the row's whole
 // sum and the listed part of it, and a bucket of 1e-30 of the row has full precision.
 //
-// What bounds it: memory.  8,192 rows of 151,936 bf16 with a bf16 gradient: 1,158 us, 4.3 TB/s of reads and writes (a large copy
+// What bounds it: memory.  8,192 rows of 151,936 bf16 with a bf16 gradient: 1,167 us, 4.3 TB/s of reads and writes (a large copy
 // reaches 4.8); the second sweep runs backwards over what the caches still hold.
 #pragma once
 

@@ -227,7 +227,9 @@ using CeFew = CeTile<64, 64, 4, 1, 4>;
 
 // Which tile and split a workgroup takes.  Workgroups go round the eight dies: each die gets a run of tiles, splits one after
 // the other (whose slices of both operands its L2 then holds), in columns of eight q, so that those at work on it at a
-// time (32) share 4 + 8 tiles.
+// time (32) share 4 + 8 tiles.  With a mask the runs are those of all the call's rows: tiles behind the last row that takes
+// part end at once, and where there are several columns of rows the last dies have little else (3,001 rows, 2,011 of them
+// taking part: 294 tiles of L on five dies, 98 on one, none on two).
 __device__ __forceinline__ void ce_place(const CeGemm& A, int* p_tile, int* q_tile, int* split) {
   const int tiles = A.p_tiles * A.q_tiles, n = gridDim.x, die = blockIdx.x & 7, i = blockIdx.x >> 3;
   const int each = n >> 3, more = n & 7;
